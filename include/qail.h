@@ -402,6 +402,126 @@ int qail_lsq_backward(const float* v, const float* dout, size_t n, const float* 
 int qail_qbc_loss(const float* logits_q, const float* logits_fp, int32_t B, int32_t D, float* loss,
                   float* grad_q, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------- serving: between a decoder's linears --
+ * The appendix "Analysis" times the prefill and the decode stage of the whole backbone.  These calls are what
+ * a decoder layer does between its quantised linears when several requests are served at once: norms, a cache of
+ * keys and values in pages, attention over it, and adapters that differ from request to request. */
+
+/* Root-mean-square norm of rows, with the residual's addition before it:
+ *     h = x (+ residual)                             fp32, one rounding
+ *     r[m] = 1 / sqrt(mean_k h[m][k]^2 + eps)        fp32 sums
+ *     y[m][k] = bf16(h[m][k] * r[m] * weight[k])
+ * and, for 8-bit linears, codes with one step per row:
+ *     u = h * weight                                 fp32, one rounding
+ *     s = max_k |u[m][k]| / 127                      fp32, correctly rounded; 1 for an all-zero row
+ *     q[m][k] = clamp(rint(u / s), -127, 127);       y_scale[m] = s * r[m]
+ * so q * y_scale stands for y; r is in the scale alone and decides no code.  Codes are packed as by qail_quantize_act_s8:
+ * a row is the a_s8 of a qail_w8a8_gemm with H = W = 1, whose int32 sums are scaled by y_scale[m] and the weight's scale.
+ *   x, residual  bf16 [M][K] (residual may be NULL); weight bf16 [K]; eps > 0
+ *   h_out        bf16 [M][K], the rounded h, or NULL; may be x or residual itself
+ *   y            bf16 [M][K] or NULL; may be x or residual itself, when h_out is not
+ *   y_s8, y_scale  uint32 [M][K/4] and fp32 [M], both or neither
+ * At least one of h_out (with a residual), y and y_s8 is required.  K % 8 == 0, M * K < 2^31. */
+int qail_rmsnorm(const uint16_t* x, const uint16_t* residual, const uint16_t* weight, float eps, int32_t M, int32_t K,
+                 uint16_t* h_out, uint16_t* y, uint32_t* y_s8, float* y_scale, void* stream);
+
+/* Its gradient.  h: bf16 [M][K], what was normalised (h_out of the forward call, or x where there is no residual);
+ * dy: the gradient of y; dres: the gradient that reaches h_out on its other way, or NULL; both bf16 [M][K].  With n = h * r:
+ *     dx = bf16(r * (dy * weight - n * mean_k(dy * weight * n)) + dres)     the gradient of x and of residual; [M][K]
+ *     dweight[k] = sum_m dy * n                                             fp32 [K], a fixed order of summation
+ * (for codes the straight-through gradient is that of y).  dx may be h, dy or dres itself.  The workspace is 16-byte aligned. */
+int qail_rmsnorm_backward_workspace(int32_t M, int32_t K, size_t* bytes);
+int qail_rmsnorm_backward(const uint16_t* h, const uint16_t* weight, float eps, const uint16_t* dy, const uint16_t* dres,
+                          int32_t M, int32_t K, uint16_t* dx, float* dweight, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* How a cache holds keys and values. */
+typedef enum {
+    QAIL_KV_BF16 = 0,
+    QAIL_KV_S8 = 1    /* signed codes -127..127 with one fp32 step per token and head: max|t| / 127, 1 for an all-zero row */
+} qail_kv_type;
+
+/* The keys and values of one layer in pages that requests are given as they grow.  k and v (and their steps) are
+ * [num_pages][heads][page_size][head_dim] (steps without the last dimension); device memory, 16-byte aligned. */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;      /* QAIL_KV_S8 only */
+    float* v_scale;
+    int32_t num_pages, heads, page_size;   /* page_size: a power of two, 16 to 1024 */
+    int32_t head_dim;                      /* 64 or 128 */
+    int32_t type;                          /* qail_kv_type */
+} qail_kv_cache;
+
+/* Byte sizes of k (and of v), and of k_scale (and of v_scale); pointers in `c` are not looked at. */
+int qail_kv_cache_sizes(const qail_kv_cache* c, size_t* data_bytes, size_t* scale_bytes);
+
+/* The requests of a step.  Their new tokens are packed: request r has rows q_start[r] .. q_start[r + 1] - 1 of the step's tensors,
+ * any number of them (0: it waits).  kv_len[r] counts its tokens with the new ones, so that row i of them has position
+ * kv_len[r] - (q_start[r + 1] - q_start[r]) + i; a token at position p lies in slot p % page_size of page page_table[r][p / page_size].
+ * page_table, q_start and kv_len are device memory (4-byte aligned), read when the kernels run, so that a captured graph can be
+ * replayed with other contents: q_start ascends from 0 to `tokens`.
+ * max_new and max_len are upper bounds on a request's new tokens and its kv_len that the launches are planned by; contents
+ * beyond them cost speed, not results. */
+typedef struct {
+    const int32_t* page_table;   /* [requests][max_pages]; entries that no token lies in are not used */
+    const int32_t* q_start;      /* [requests + 1] */
+    const int32_t* kv_len;       /* [requests] */
+    int32_t requests, max_pages;
+    int32_t tokens;              /* rows of the step's tensors, >= 0 */
+    int32_t max_new, max_len;
+} qail_requests;
+
+/* `errors` (device, one uint32, may be NULL; not cleared) of the two calls below is incremented at least once if the contents of the
+ * three arrays are bad: a page outside 0 .. num_pages - 1 for a token in use, a kv_len beyond max_pages * page_size, a q_start that descends
+ * or leaves 0 .. tokens, for qail_kv_append a negative position or one beyond `positions`.  Nothing outside the given
+ * buffers is read or written then; the outputs of the requests concerned are unspecified. */
+
+/* Rotates the new tokens' keys and queries and writes keys and values to their slots.  With half = head_dim / 2, position p, i < half,
+ * each product and sum one fp32 operation (no fused multiply-add):
+ *     t'[i] = t[i] * cos[p][i] - t[i + half] * sin[p][i],   t'[i + half] = t[i + half] * cos[p][i] + t[i] * sin[p][i]
+ * rounded once, to bf16 or to the cache's codes.
+ *   k, v      bf16, token t and head h at t * k_stride + h * head_dim (elements; strides are multiples of 8, >= heads * head_dim)
+ *   q, q_out  bf16, q_heads heads of each; q as k with q_stride, q_out contiguous [tokens][q_heads][head_dim] (may be q where that is
+ *             contiguous); both NULL where there are no queries to rotate
+ *   cos, sin  fp32 [positions][half], both or neither: without them nothing is rotated and q must be NULL
+ * The pages that requests write to must differ. */
+int qail_kv_append(const qail_kv_cache* c, const qail_requests* b, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                   int64_t v_stride, const uint16_t* q, int64_t q_stride, int32_t q_heads, uint16_t* q_out, const float* cos,
+                   const float* sin, int32_t positions, uint32_t* errors, void* stream);
+
+/* Causal attention of the new tokens over their requests' cache, which holds their own keys and values already:
+ *     out[t][a] = sum_j p_j v[j],  p = softmax_j(scale * q[t][a] . k[j]),  j = 0 .. position of t, head a / (q_heads / heads) of the cache
+ * (q_heads is a multiple of the cache's heads).  A chunk may be one token, a few, or a whole prompt.  Scores, maxima and sums are fp32; p is
+ * rounded to bf16 for its product with v (one that is below 2^-126 of its row's largest may count as zero).  A token whose position is negative (more new tokens than kv_len) sees no key: its
+ * rows are zero.  Slots behind a request's last token may hold anything.
+ *   q         bf16, token t and head a at t * q_stride + a * head_dim; q_stride % 8 == 0
+ *   out       bf16 [tokens][q_heads][head_dim]
+ *   scale     finite
+ * The workspace (256-byte aligned; may be NULL where the query says 0) holds the partial results of keys that are divided among blocks. */
+int qail_paged_attention_workspace(const qail_kv_cache* c, const qail_requests* b, int32_t q_heads, size_t* bytes);
+int qail_paged_attention(const qail_kv_cache* c, const qail_requests* b, const uint16_t* q, int64_t q_stride, int32_t q_heads, float scale,
+                         uint16_t* out, uint32_t* errors, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters of many requests beside a shared 4-bit linear: `count` linears as for qail_w4a16_linear_batch, and for each a stack
+ * of `n` adapters of one rank, of which row m of x uses row_adapter[m]:
+ *     y[m] = x[m] w_hat^T + scaling[a] (x[m] A[a]^T) B[a]^T,  a = row_adapter[m];  without the second term where a is not in 0 .. n - 1
+ * A: bf16 [n][r][K], B: bf16 [n][N][r], scaling: fp32 [n]; device memory, 16-byte aligned; 8 <= r <= 64, r % 8 == 0, n >= 1; an
+ * adapter of a lower rank is filled up with zeros.  row_adapter: int32 [M], device, 4-byte aligned, the same for all linears.
+ * The linear is rounded to bf16 as by qail_w4a16_linear_batch, the adapter's fp32 part is added and rounded again; a row without an adapter
+ * keeps the linear's bits.  What one adapter holds reaches no row of another. */
+typedef struct {
+    const uint16_t* A;
+    const uint16_t* B;
+    const float* scaling;
+    int32_t n, r;
+} qail_adapters;
+
+/* Workspace (256-byte aligned): the linears' own and the down-projections x A^T in fp32.  Errors as for qail_w4a16_linear_lora_batch. */
+int qail_w4a16_adapters_workspace(const qail_w4a16_item* items, const qail_adapters* adapters, int32_t count, int32_t M, size_t* bytes);
+int qail_w4a16_linear_adapters_batch(const qail_w4a16_item* items, const qail_adapters* adapters, const int32_t* row_adapter, int32_t count,
+                                     int32_t M, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

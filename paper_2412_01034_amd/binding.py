@@ -40,6 +40,8 @@ EXPORTS = (
     "qail_act_scale_s8", "qail_quantize_act_s8", "qail_w8a8_gemm", "qail_w8a16_linear",
     "qail_w8a16_linear_batch", "qail_w8a16_workspace", "qail_w8a16_batch_workspace",
     "qail_fake_quant_w4", "qail_lsq_forward", "qail_lsq_backward_workspace", "qail_lsq_backward", "qail_qbc_loss",
+    "qail_rmsnorm", "qail_rmsnorm_backward_workspace", "qail_rmsnorm_backward", "qail_kv_cache_sizes", "qail_kv_append",
+    "qail_paged_attention_workspace", "qail_paged_attention", "qail_w4a16_adapters_workspace", "qail_w4a16_linear_adapters_batch",
 )
 
 
@@ -77,6 +79,22 @@ class qail_w4a16_item(ctypes.Structure):
 class qail_w8a16_item(ctypes.Structure):
     _fields_ = [("d", qail_wdesc), ("qweight", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("x", ctypes.c_void_p), ("y", ctypes.c_void_p)]
+
+
+class qail_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int32), ("heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
+class qail_requests(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("requests", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_len", ctypes.c_int32)]
+
+
+class qail_adapters(ctypes.Structure):
+    _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scaling", ctypes.c_void_p), ("n", ctypes.c_int32), ("r", ctypes.c_int32)]
 
 
 _lib = None
@@ -130,6 +148,16 @@ def lib() -> ctypes.CDLL:
         L.qail_w4a4_conv_batch.argtypes = [ctypes.POINTER(qail_conv_item), i32, vp]
         L.qail_w4a4_conv_u4.argtypes = [ctypes.POINTER(qail_conv_desc), vp, vp, vp, vp, ctypes.c_float, vp,
                                         ctypes.c_float, vp, vp, vp, sz, vp]
+        pc, pb, i64, f32 = ctypes.POINTER(qail_kv_cache), ctypes.POINTER(qail_requests), ctypes.c_int64, ctypes.c_float
+        L.qail_rmsnorm.argtypes = [vp, vp, vp, f32, i32, i32, vp, vp, vp, vp, vp]
+        L.qail_rmsnorm_backward_workspace.argtypes = [i32, i32, psz]
+        L.qail_rmsnorm_backward.argtypes = [vp, vp, f32, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+        L.qail_kv_cache_sizes.argtypes = [pc, psz, psz]
+        L.qail_kv_append.argtypes = [pc, pb, vp, i64, vp, i64, vp, i64, i32, vp, vp, vp, i32, vp, vp]
+        L.qail_paged_attention_workspace.argtypes = [pc, pb, i32, psz]
+        L.qail_paged_attention.argtypes = [pc, pb, vp, i64, i32, f32, vp, vp, vp, sz, vp]
+        L.qail_w4a16_adapters_workspace.argtypes = [ctypes.POINTER(qail_w4a16_item), ctypes.POINTER(qail_adapters), i32, i32, psz]
+        L.qail_w4a16_linear_adapters_batch.argtypes = [ctypes.POINTER(qail_w4a16_item), ctypes.POINTER(qail_adapters), vp, i32, i32, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("qail_status_string",):
                 getattr(L, name).restype = ctypes.c_int
@@ -589,3 +617,174 @@ def qail_qbc_loss(logits_q: torch.Tensor, logits_fp: torch.Tensor, loss: torch.T
         _need(grad_q, Bn * D * 4, "grad_q")
     _check(lib().qail_qbc_loss(_ptr(logits_q), _ptr(logits_fp), Bn, D, _ptr(loss), _ptr(grad_q), _ptr(workspace),
                                workspace.numel() * workspace.element_size(), _stream()), "qail_qbc_loss")
+
+
+# ------------------------------------------------------------------ serving: between a decoder's linears --
+
+QAIL_KV_BF16 = 0
+QAIL_KV_S8 = 1
+
+
+def _typed(t: torch.Tensor, what: str, *dtypes) -> None:
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: {' or '.join(str(d).replace('torch.', '') for d in dtypes)} expected, {t.dtype} given")
+
+
+def _bf16(t: Optional[torch.Tensor], count: int, what: str) -> Optional[int]:
+    """The address of an optional bf16 tensor (or one of 16-bit integers with the same bits) of at least `count` values."""
+    if t is None:
+        return None
+    _typed(t, what, torch.bfloat16, torch.int16)
+    return _arg(t, 2 * count, what)
+
+
+def _fp32(t: Optional[torch.Tensor], count: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    _typed(t, what, torch.float32)
+    return _arg(t, 4 * count, what)
+
+
+def _int32(t: torch.Tensor, count: int, what: str) -> int:
+    _typed(t, what, torch.int32)
+    return _arg(t, 4 * count, what)
+
+
+def _errors(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else _int32(t, 1, "errors")
+
+
+def qail_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                 residual_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, y_s8: Optional[torch.Tensor] = None,
+                 y_scale: Optional[torch.Tensor] = None) -> None:
+    """x, residual: bf16 [M, K]; residual_out (the rounded sum), y: bf16 [M, K]; y_s8: M * K bytes of codes; y_scale: fp32 [M]."""
+    M, K = x.shape
+    n = M * K
+    if y_s8 is not None:
+        _need(y_s8, n, "y_s8")
+    _check(lib().qail_rmsnorm(_bf16(x, n, "x"), _bf16(residual, n, "residual"), _bf16(weight, K, "weight"), eps, M, K,
+                              _bf16(residual_out, n, "residual_out"), _bf16(y, n, "y"), _ptr(y_s8), _fp32(y_scale, M, "y_scale"), _stream()),
+           "qail_rmsnorm")
+
+
+def qail_rmsnorm_backward_workspace(M: int, K: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_rmsnorm_backward_workspace(M, K, ctypes.byref(b)), "qail_rmsnorm_backward_workspace")
+    return b.value
+
+
+def qail_rmsnorm_backward(h: torch.Tensor, weight: torch.Tensor, eps: float, dy: torch.Tensor, dx: torch.Tensor, dweight: torch.Tensor,
+                          workspace: torch.Tensor, dres: Optional[torch.Tensor] = None) -> None:
+    """h, dy, dres, dx: bf16 [M, K]; dweight: fp32 [K]."""
+    M, K = h.shape
+    n = M * K
+    _check(lib().qail_rmsnorm_backward(_bf16(h, n, "h"), _bf16(weight, K, "weight"), eps, _bf16(dy, n, "dy"), _bf16(dres, n, "dres"), M, K,
+                                       _bf16(dx, n, "dx"), _fp32(dweight, K, "dweight"), _ptr(workspace), workspace.nbytes, _stream()),
+           "qail_rmsnorm_backward")
+
+
+def make_kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                  v_scale: Optional[torch.Tensor] = None) -> qail_kv_cache:
+    """k, v: [num_pages, heads, page_size, head_dim], bf16 or int8; with int8 the steps, fp32 [num_pages, heads, page_size].  The
+    result can be passed to any number of calls (the tensors must be kept alive by the caller)."""
+    pages, heads, size, dim = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v of one shape and type expected")
+    _typed(k, "k", torch.bfloat16, torch.int8)
+    eight = k.dtype == torch.int8
+    if eight != (k_scale is not None) or eight != (v_scale is not None):
+        raise ValueError("k_scale and v_scale belong to an int8 cache")
+    c = qail_kv_cache(_ptr(k), _ptr(v), _fp32(k_scale, pages * heads * size, "k_scale"), _fp32(v_scale, pages * heads * size, "v_scale"),
+                      pages, heads, size, dim, QAIL_KV_S8 if eight else QAIL_KV_BF16)
+    qail_kv_cache_sizes(pages, heads, size, dim, c.type)   # raises for a shape that is not supported
+    return c
+
+
+def qail_kv_cache_sizes(num_pages: int, heads: int, page_size: int, head_dim: int, type: int) -> Tuple[int, int]:
+    """Bytes of k (and of v), and of k_scale (and of v_scale)."""
+    c = qail_kv_cache(None, None, None, None, num_pages, heads, page_size, head_dim, type)
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().qail_kv_cache_sizes(ctypes.byref(c), ctypes.byref(a), ctypes.byref(b)), "qail_kv_cache_sizes")
+    return a.value, b.value
+
+
+def make_requests(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, tokens: int, max_new: int, max_len: int) -> qail_requests:
+    """page_table: int32 [requests, max_pages]; q_start: int32 [requests + 1]; kv_len: int32 [requests].  The result can be passed to
+    any number of calls, also after the tensors' contents have changed (they must be kept alive by the caller)."""
+    requests, max_pages = page_table.shape
+    return qail_requests(_int32(page_table, requests * max_pages, "page_table"), _int32(q_start, requests + 1, "q_start"),
+                         _int32(kv_len, requests, "kv_len"), requests, max_pages, tokens, max_new, max_len)
+
+
+def _heads(t: torch.Tensor, tokens: int, dim: int, what: str) -> Tuple[int, int, int]:
+    """Address, stride between tokens and heads of a bf16 tensor [tokens, heads, dim] whose tokens may lie apart."""
+    _typed(t, what, torch.bfloat16, torch.int16)
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    n, heads, d = t.shape
+    if n < tokens or d != dim:
+        raise ValueError(f"{what}: [{tokens}, heads, {dim}] expected, {list(t.shape)} given")
+    across, between, within = t.stride()
+    if (within != 1 and d > 1) or (between != d and heads > 1):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return t.data_ptr(), across if n > 1 else heads * d, heads
+
+
+def qail_kv_append(cache: qail_kv_cache, requests: qail_requests, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                   q_out: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                   errors: Optional[torch.Tensor] = None) -> None:
+    """k, v: bf16 [tokens, heads, head_dim], q: bf16 [tokens, q_heads, head_dim], views of a wider tensor among them; q_out: contiguous;
+    cos, sin: fp32 [positions, head_dim / 2]."""
+    T, D = requests.tokens, cache.head_dim
+    ka, ks, kh = _heads(k, T, D, "k")
+    va, vs, vh = _heads(v, T, D, "v")
+    if kh != cache.heads or vh != cache.heads:
+        raise ValueError(f"k and v of {cache.heads} heads expected")
+    qa, qs, qh = _heads(q, T, D, "q") if q is not None else (None, 0, 0)
+    positions = cos.shape[0] if cos is not None else 0
+    _check(lib().qail_kv_append(ctypes.byref(cache), ctypes.byref(requests), ka, ks, va, vs, qa, qs, qh, _bf16(q_out, T * qh * D, "q_out"),
+                                _fp32(cos, positions * D // 2, "cos"), _fp32(sin, positions * D // 2, "sin"), positions, _errors(errors), _stream()),
+           "qail_kv_append")
+
+
+def qail_paged_attention_workspace(cache: qail_kv_cache, requests: qail_requests, q_heads: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_paged_attention_workspace(ctypes.byref(cache), ctypes.byref(requests), q_heads, ctypes.byref(b)),
+           "qail_paged_attention_workspace")
+    return b.value
+
+
+def qail_paged_attention(cache: qail_kv_cache, requests: qail_requests, q: torch.Tensor, out: torch.Tensor, scale: float,
+                         workspace: Optional[torch.Tensor] = None, errors: Optional[torch.Tensor] = None) -> None:
+    """q: bf16 [tokens, q_heads, head_dim], a view of a wider tensor among them; out: contiguous."""
+    T, D = requests.tokens, cache.head_dim
+    qa, qs, qh = _heads(q, T, D, "q")
+    ws, wsb = (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
+    _check(lib().qail_paged_attention(ctypes.byref(cache), ctypes.byref(requests), qa, qs, qh, scale, _bf16(out, T * qh * D, "out"), _errors(errors),
+                                      ws, wsb, _stream()), "qail_paged_attention")
+
+
+def make_adapters(entries: Sequence[dict]):
+    """entries: dicts with A (bf16 [n, r, K]), B (bf16 [n, N, r]) and scaling (fp32 [n]), one for each linear of a list.  The tensors must
+    be kept alive by the caller."""
+    arr = (qail_adapters * max(1, len(entries)))()
+    for i, e in enumerate(entries):
+        n, r, K = e["A"].shape
+        if tuple(e["B"].shape) != (n, e["N"], r) or K != e["K"]:
+            raise ValueError(f"A [n, r, {e['K']}] and B [n, {e['N']}, r] expected, {list(e['A'].shape)} and {list(e['B'].shape)} given")
+        arr[i] = qail_adapters(_bf16(e["A"], n * r * K, "A"), _bf16(e["B"], n * e["N"] * r, "B"), _fp32(e["scaling"], n, "scaling"), n, r)
+    return arr
+
+
+def qail_w4a16_adapters_workspace(items, adapters, count: int, M: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_w4a16_adapters_workspace(items, adapters, count, M, ctypes.byref(b)), "qail_w4a16_adapters_workspace")
+    return b.value
+
+
+def qail_w4a16_linear_adapters_batch(items, adapters, row_adapter: torch.Tensor, count: int, M: int, workspace: torch.Tensor,
+                                     stream: Optional[int] = None) -> None:
+    """items: make_w4a16_items, adapters: make_adapters of the same list; row_adapter: int32 [M], -1 for a row without an adapter."""
+    wsb = workspace.nbytes if workspace is not None else 0
+    _check(lib().qail_w4a16_linear_adapters_batch(items, adapters, _int32(row_adapter, M, "row_adapter"), count, M, _ptr(workspace), wsb,
+                                                  _stream() if stream is None else stream), "qail_w4a16_linear_adapters_batch")

@@ -1,0 +1,226 @@
+// Low-rank adapters of many requests beside a shared 4-bit linear: row m of x goes through adapter a = row_adapter[m],
+//   t[m][j] = sum_k x[m][k] A[a][j][k],   y[m][n] += scaling[a] sum_j t[m][j] B[a][n][j].
+// Two launches around the linears': both contractions run on the matrix cores, 16 rows of x at a time.  A tile's rows may belong to
+// any number of adapters: each distinct one is multiplied with all 16 rows and only its own rows' columns are kept, by selection, so that
+// nothing an adapter holds (an infinity included) reaches another's rows.  At decode sizes, where every row may have its own,
+// the distinct adapters of a tile are spread over blocks (`slots`), since one after the other they would be a chain of round
+// trips to memory.  The bytes are those of the adapters in use, r (K + N) bf16 each.
+#include "qail_internal.h"
+
+namespace qail {
+
+namespace {
+
+constexpr int kMaxItems = 8;    // linears that share the two launches
+constexpr int kMaxSplits = 8;   // shares of K
+constexpr int kDownWaves = 8, kUpWaves = 4;
+
+struct AdapterItem {
+    const uint16_t *x, *A, *B;
+    const float* scaling;
+    float* t;      // fp32 [splits][M][r]
+    uint16_t* y;
+    int N, K, n, r;
+};
+struct AdapterArgs {
+    AdapterItem it[kMaxItems];
+    const int32_t* rows;
+    int M, slots, splits;
+};
+
+// Calls f(a, mine) for the distinct adapters of the tile that are this slot's; `mine`: whether the lane's column (row m0 + lane % 16) uses it.
+template <typename F>
+__device__ __forceinline__ void each_adapter(const AdapterArgs& a, const AdapterItem& it, int m0, int slot, F f) {
+    const int m = m0 + (int)threadIdx.x % 16;
+    const int id = m < a.M ? a.rows[m] : -1;
+    unsigned long long left = __ballot(id >= 0 && id < it.n) & 0xFFFFull;   // the first 16 lanes hold the tile's rows
+    for (int i = 0; left; ++i) {
+        const int of = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const bool mine = id == of;
+        left &= ~__ballot(mine);
+        if (i % a.slots == slot) f(of, mine);
+    }
+}
+
+__global__ __launch_bounds__(kDownWaves* kWave) void adapters_down_kernel(const AdapterArgs a) {
+    __shared__ f32x4_t red[kDownWaves][kWave];
+    const int item = blockIdx.z, slot = blockIdx.y;
+    const AdapterItem& it = a.it[item];
+    const int tiles_j = (it.r + 15) / 16;
+    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
+    const int j0 = tile % 4 * 16, m0 = tile / 4 * 16;   // four tiles of j for every item: a rank of 64
+    if (j0 / 16 >= tiles_j) return;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane % 16, g = lane / 16;
+    const int K = it.K, r = it.r, M = a.M;
+    const uint16_t* xr = it.x + (size_t)min(m0 + col, M - 1) * K + 8 * g;
+    each_adapter(a, it, m0, slot, [&](int of, bool mine) {
+        const uint16_t* ar = it.A + ((size_t)of * r + min(j0 + col, r - 1)) * K + 8 * g;
+        constexpr int kAhead = 4;
+        const int round = 32 * kDownWaves * a.splits;
+        f32x4_t part[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) part[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int kb = (wave * a.splits + split) * 32; kb < K; kb += kAhead * round) {
+            uint4 xv[kAhead], av[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {   // past the end of K element 0 is read again and counts as 0
+                const bool in = kb + u * round + 8 * g < K;
+                xv[u] = *reinterpret_cast<const uint4*>(xr + (in ? kb + u * round : -8 * g));
+                av[u] = *reinterpret_cast<const uint4*>(ar + (in ? kb + u * round : -8 * g));
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (kb + u * round + 8 * g >= K) xv[u] = av[u] = uint4{0u, 0u, 0u, 0u};
+                part[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, av[u]), __builtin_bit_cast(bf16x8_t, xv[u]), part[u], 0, 0, 0);
+            }
+        }
+        __syncthreads();   // the sums of the adapter before have been read
+        red[wave][lane] = (part[0] + part[1]) + (part[2] + part[3]);
+        __syncthreads();
+        if (wave == 0 && mine) {   // (mine: the row exists)
+            f32x4_t sum = red[0][lane];
+#pragma unroll
+            for (int w = 1; w < kDownWaves; ++w) sum += red[w][lane];
+            if (j0 + 4 * g < r) *reinterpret_cast<f32x4_t*>(it.t + ((size_t)split * M + m0 + col) * r + j0 + 4 * g) = sum;   // r % 8 == 0
+        }
+    });
+}
+
+// A wave adds to 16 rows of 64 columns.  Row i of tile t of the product is column 16 (i / 4) + 4 t + i % 4, so that a lane ends up with 16
+// consecutive columns of one row.  t is split into two bf16 values (a relative 2^-17 is lost, where one alone would lose 2^-9).
+template <bool kWide>   // N % 8 == 0: rows of y are 16-byte aligned
+__device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& it, int m0, int n0, int slot) {
+    const int lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
+    const int N = it.N, r = it.r, M = a.M, m = m0 + col;
+    each_adapter(a, it, m0, slot, [&](int of, bool mine) {
+        f32x4_t acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int j0 = 0; j0 < r; j0 += 32) {
+            const bool in = j0 + 8 * g < r;
+            uint4 bv[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int n = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
+                bv[t] = in ? *reinterpret_cast<const uint4*>(it.B + ((size_t)of * N + n) * r + j0 + 8 * g) : uint4{0u, 0u, 0u, 0u};
+            }
+            float s[8] = {};
+            if (in && mine)
+                for (int k = 0; k < a.splits; ++k) {
+                    const float4* p = reinterpret_cast<const float4*>(it.t + ((size_t)k * M + m) * r + j0 + 8 * g);
+                    const float4 lo = p[0], hi = p[1];
+                    s[0] += lo.x; s[1] += lo.y; s[2] += lo.z; s[3] += lo.w;
+                    s[4] += hi.x; s[5] += hi.y; s[6] += hi.z; s[7] += hi.w;
+                }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                hi[e] = f32x2_to_bf16x2_rne(s[2 * e], s[2 * e + 1]);
+                lo[e] = f32x2_to_bf16x2_rne(s[2 * e] - __builtin_bit_cast(float, hi[e] << 16), s[2 * e + 1] - __builtin_bit_cast(float, hi[e] & 0xFFFF0000u));
+            }
+            const bf16x8_t th = __builtin_bit_cast(bf16x8_t, uint4{hi[0], hi[1], hi[2], hi[3]}), tl = __builtin_bit_cast(bf16x8_t, uint4{lo[0], lo[1], lo[2], lo[3]});
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const bf16x8_t b = __builtin_bit_cast(bf16x8_t, bv[t]);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tl, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, th, acc[t], 0, 0, 0);
+            }
+        }
+        const int n = n0 + 16 * g;
+        if (!mine || n >= N) return;
+        const float scaling = it.scaling[of];
+        uint16_t* y = it.y + (size_t)m * N + n;
+        if (kWide) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (n + 8 * half >= N) break;
+                uint4 v = reinterpret_cast<uint4*>(y)[half];
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4_t& d = acc[2 * half + e / 2];
+                    w[e] = f32x2_to_bf16x2_rne(fmaf(scaling, d[e % 2 * 2], __builtin_bit_cast(float, w[e] << 16)),
+                                               fmaf(scaling, d[e % 2 * 2 + 1], __builtin_bit_cast(float, w[e] & 0xFFFF0000u)));
+                }
+                reinterpret_cast<uint4*>(y)[half] = uint4{w[0], w[1], w[2], w[3]};
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (n + e < N) y[e] = (uint16_t)f32x2_to_bf16x2_rne(fmaf(scaling, acc[e / 4][e % 4], bf16_bits_to_f32(y[e])), 0.f);
+        }
+    });
+}
+
+__global__ __launch_bounds__(kUpWaves* kWave) void adapters_up_kernel(const AdapterArgs a) {
+    const AdapterItem& it = a.it[blockIdx.z];
+    const int row_tiles = (a.M + 15) / 16;
+    const int m0 = blockIdx.x % row_tiles * 16, n0 = (blockIdx.x / row_tiles * kUpWaves + (int)threadIdx.x / kWave) * 64;
+    if (n0 >= it.N) return;   // whole waves; no barrier below
+    if (it.N % 8 == 0) add_up<true>(a, it, m0, n0, blockIdx.y);
+    else add_up<false>(a, it, m0, n0, blockIdx.y);
+}
+
+// Shares of K: more where the tiles alone leave the chip empty.
+int k_splits(int M, int count) {
+    const long long blocks = 2ll * ((M + 15) / 16) * count;   // of a rank of 32
+    const long long s = device_cu_count() / blocks;
+    return s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : (int)s;
+}
+
+}  // namespace
+
+// fp32 values of workspace: the down-projections of every linear.
+size_t adapters_workspace(const qail_adapters* ad, int count, int M) {
+    size_t n = 0;
+    for (int i = 0; i < count; ++i) {
+        const int first = i / kMaxItems * kMaxItems;
+        n += (size_t)k_splits(M, count - first < kMaxItems ? count - first : kMaxItems) * M * ad[i].r;
+    }
+    return n;
+}
+
+namespace {
+
+template <typename F>
+hipError_t in_groups(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, F launch) {
+    for (int i0 = 0; i0 < count; i0 += kMaxItems) {
+        const int c = count - i0 < kMaxItems ? count - i0 : kMaxItems;
+        AdapterArgs a{};
+        int widest = 0, most = 1;
+        a.rows = rows;
+        a.M = M;
+        a.splits = k_splits(M, c);
+        for (int i = 0; i < c; ++i) {
+            const qail_w4a16_item& s = items[i0 + i];
+            const qail_adapters& l = ad[i0 + i];
+            a.it[i] = AdapterItem{s.x, l.A, l.B, l.scaling, t, s.y, s.d.N, s.d.K, l.n, l.r};
+            t += (size_t)a.splits * M * l.r;
+            widest = s.d.N > widest ? s.d.N : widest;
+            most = l.n > most ? l.n : most;
+        }
+        const int in_tile = M < 16 ? M : 16;   // distinct adapters of a tile, at most
+        a.slots = most < in_tile ? most : in_tile;
+        if (M > 64) a.slots = 1;
+        launch(a, c, widest);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st) {
+    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int) {
+        hipLaunchKernelGGL(adapters_down_kernel, dim3((M + 15) / 16 * 4 * a.splits, a.slots, c), dim3(kDownWaves * kWave), 0, st, a);
+    });
+}
+
+hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st) {
+    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int widest) {
+        hipLaunchKernelGGL(adapters_up_kernel, dim3((M + 15) / 16 * ((widest + 64 * kUpWaves - 1) / (64 * kUpWaves)), a.slots, c), dim3(kUpWaves * kWave), 0, st, a);
+    });
+}
+
+}  // namespace qail

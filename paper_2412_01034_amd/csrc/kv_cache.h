@@ -1,0 +1,89 @@
+// The cache of keys and values and the requests of a step, as the kernels see them.
+#pragma once
+
+#include "qail_internal.h"
+
+namespace qail {
+
+struct CacheArgs {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    const int32_t *table, *starts, *lens;
+    uint32_t* errors;
+    int num_pages, heads, page_shift, max_pages, requests, tokens;
+};
+
+inline CacheArgs cache_args(const qail_kv_cache& c, const qail_requests& b, uint32_t* errors) {
+    return CacheArgs{c.k, c.v, c.k_scale, c.v_scale, b.page_table, b.q_start, b.kv_len, errors,
+                     c.num_pages, c.heads, __builtin_ctz((unsigned)c.page_size), b.max_pages, b.requests, b.tokens};
+}
+
+__device__ __forceinline__ void report(const CacheArgs& a) {
+    if (a.errors) atomicAdd(a.errors, 1u);
+}
+
+// A request's rows of the step's tensors and its length, with what the arrays may hold turned into something that stays inside
+// the buffers: n = 0 where q_start is bad, len cut to what the page table can hold.  (This and what follows is for the host
+// too, which walks through it in the tests.)
+struct Request {
+    int start, n, len;
+};
+__host__ __device__ __forceinline__ Request request(const CacheArgs& a, int r, bool& bad) {
+    const int s = a.starts[r], e = a.starts[r + 1], len = a.lens[r];
+    const long long room = (long long)a.max_pages << a.page_shift;
+    const bool rows = s >= 0 && e >= s && e <= a.tokens, keys = len >= 0 && (long long)len <= room;
+    bad = !rows || !keys;
+    Request q{0, 0, 0};
+    if (rows) q = Request{s, e - s, keys ? len : len < 0 ? 0 : (int)room};   // room < len fits 31 bits
+    return q;
+}
+
+// The request that has row t: the last one whose rows start at or before it.  A wave looks at 64 starts at a time, with no load waiting
+// for another (a binary search would wait for eight in a row at 256 requests).
+__device__ __forceinline__ int request_of(const CacheArgs& a, int t) {
+    int before = 0;
+    for (int i = 0; i < a.requests; i += kWave) {
+        const int r = i + (int)threadIdx.x % kWave;
+        before += __popcll(__ballot(r < a.requests && a.starts[r] <= t));
+    }
+    return before - 1;
+}
+
+// Whether a token of a request can be written: its position is one that the page table and the table of angles (positions; 0: none) reach.
+__host__ __device__ __forceinline__ bool has_slot(const Request& q, int t, int positions, int& at) {
+    at = q.len - q.n + (t - q.start);   // below len: inside the page table
+    return t >= q.start && t < q.start + q.n && at >= 0 && (positions == 0 || at < positions);
+}
+
+// Keys that rows row0 .. row0 + count - 1 of a request see (its last row's), `group` rows a token.
+__host__ __device__ __forceinline__ int keys_of(const Request& q, int group, int row0, int count) {
+    const int rows = q.n * group, last = row0 + count < rows ? row0 + count - 1 : rows - 1;
+    const int keys = q.len - q.n + last / group + 1;
+    return keys > 0 ? keys : 0;
+}
+
+// Shares that `keys` are divided into: `chunk` each, at most `most` of them, of which the last takes what is left.
+__host__ __device__ __forceinline__ int shares(int keys, int chunk, int most) {
+    const int n = (keys + chunk - 1) / chunk;
+    return n < 1 ? 1 : n > most ? most : n;
+}
+struct Range {
+    int begin, end;
+};
+__host__ __device__ __forceinline__ Range share_of(int keys, int chunk, int count, int i) {
+    return Range{i * chunk, i == count - 1 ? keys : (i + 1) * chunk};
+}
+
+__host__ __device__ __forceinline__ bool is_page(int p, int num_pages) { return (unsigned)p < (unsigned)num_pages; }
+
+// A page's number in the cache; one that is not in it becomes page 0 and is reported.
+__device__ __forceinline__ int page_of(const CacheArgs& a, int r, int index) {
+    int p = a.table[(size_t)r * a.max_pages + index];
+    if (!is_page(p, a.num_pages)) {
+        report(a);
+        p = 0;
+    }
+    return p;
+}
+
+}  // namespace qail

@@ -1,0 +1,355 @@
+// Causal attention of new tokens over a paged cache.
+//
+// Scores are computed transposed, S^T = K Q^T, so that a lane of the result holds one row's (query's) scores for several keys: a row's maximum
+// and sum are a few exchanges between the lanes that share a column, its rescaling factor is where its output column
+// O^T = V^T P^T is, and the scores' registers are the second product's operand as they are.  The keys that a lane holds are
+// chosen by the order in which rows of K enter the first product, which is free.
+//
+// Rows of one request and one head of the cache: row i is token i / group, head i % group, so grouped heads share every key that is loaded.
+#include <algorithm>
+
+#include "kv_cache.h"
+
+namespace qail {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+
+struct AttentionArgs {
+    CacheArgs c;
+    const uint16_t* q;
+    uint16_t* out;
+    float* part_o;      // [tokens][q_heads][splits][D]: outputs of a share of the keys, not yet divided by their sum
+    float2* part_ml;    // [tokens][q_heads][splits]: their maximum and sum
+    long long q_stride;
+    float scale;        // times log2(e)
+    int q_heads, group;
+    int splits, chunk;  // keys of a tile of rows are divided into shares of `chunk`, at most `splits`
+};
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
+
+// Eight signed bytes as bf16 (exact).
+__device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t src = i < 2 ? lo : hi;
+        const int sh = i % 2 * 16;
+        const float x = (float)(int)(int8_t)(src >> sh), y = (float)(int)(int8_t)(src >> (sh + 8));
+        w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);   // upper halves
+    }
+    return __builtin_bit_cast(bf16x8_t, uint4{w[0], w[1], w[2], w[3]});
+}
+
+// ---------------------------------------------------------------------------- few rows: a stream of keys --
+//
+// Up to 16 rows (a decode step: the heads that share a head of the cache) against all keys: bound by the cache's bytes, each read
+// once.  A wave takes 32 keys at a time, on its own: K goes from memory into the registers that the first product reads,
+// V through the wave's part of LDS, which is read transposed.  The four waves of a block take tiles in turn and add up at the end.
+// Rows past the last key repeat it (its slot holds a token, which slots behind it need not) and get a score of minus infinity.
+constexpr int kStreamWaves = 4, kStreamKeys = 32, kStreamRows = 16;
+
+template <int D, bool kEight>
+struct Stream {
+    static constexpr int kRowBytes = kEight ? D : 2 * D;
+    static constexpr int kSteps = D / 32;                          // of the first product
+    static constexpr int kLoadsK = kEight ? D / 64 : D / 32;       // 16-byte loads of a lane per tile of 16 keys
+    static constexpr int kLanesV = kRowBytes / 16;                 // lanes that load a row of V
+    static constexpr int kSlots = kWave / kLanesV;                 // rows a load instruction covers
+    static constexpr int kLoadsV = kStreamKeys / kSlots;
+    static constexpr int kPadO = D + 4;
+    static constexpr int kLds = kStreamWaves * (kStreamKeys * kRowBytes > 16 * kPadO * 4 ? kStreamKeys * kRowBytes : 16 * kPadO * 4);
+
+    // V's rows lie in LDS with their 16-byte pieces exchanged so that the rows read together lie in different banks.
+    __device__ static __forceinline__ int swizzle(int row, int piece) {
+        if constexpr (kEight) return kRowBytes == 128 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
+        else return kRowBytes == 256 ? piece ^ (((row & 3) | ((row >> 1) & 4)) << 1) : piece ^ ((((row >> 1) & 1) | ((row >> 2) & 2)) << 1);
+    }
+};
+
+template <int D, bool kEight>
+__global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(const AttentionArgs a) {
+    using S = Stream<D, kEight>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
+    __shared__ float2 ml[kStreamWaves][16];
+    const int H = a.c.heads, R = a.c.requests;
+    const int h = blockIdx.x % H, r = blockIdx.x / H % R, split = blockIdx.x / H / R;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
+    bool bad;
+    const Request rq = request(a.c, r, bad);
+    if (bad && h == 0 && split == 0 && threadIdx.x == 0) report(a.c);
+    const int rows = rq.n * a.group;
+    uint8_t* const lds_v = lds + wave * kStreamKeys * S::kRowBytes;
+    float* const lds_o = reinterpret_cast<float*>(lds);
+
+    for (int row0 = 0; row0 < rows; row0 += kStreamRows) {
+        const int before = rq.len - rq.n;                            // keys in front of the new ones; may be negative
+        const int keys = keys_of(rq, a.group, row0, kStreamRows), count = shares(keys, a.chunk, a.splits);
+        if (split >= count) continue;   // uniform
+        const int k0 = share_of(keys, a.chunk, count, split).begin, k1 = share_of(keys, a.chunk, count, split).end;
+        const int row = row0 + col, token = row / a.group, head = h * a.group + row % a.group;
+        const int pos = row < rows ? before + token : -1;
+
+        bf16x8_t q[S::kSteps];
+#pragma unroll
+        for (int s = 0; s < S::kSteps; ++s) {   // bytes: a lane's 16 codes of K are two steps
+            const int d = kEight ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+            q[s] = as_bf16x8(row < rows ? *reinterpret_cast<const uint4*>(a.q + (rq.start + token) * a.q_stride + head * D + d) : uint4{0u, 0u, 0u, 0u});
+        }
+        f32x4_t o[D / 16];
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+
+        // Of the 32 keys from `kt`, lane group g has keys 8 g .. 8 g + 7 after the first product: row 4 g' + i of tile t is key 8 g' + 4 t + i.
+        const int key_k = 8 * (col / 4) + col % 4;
+        const int slot_v = lane / S::kLanesV, row_v = 8 * (slot_v / (S::kSlots / 4)) + slot_v % (S::kSlots / 4) * S::kLoadsV;
+        uint4 kv[2][S::kLoadsK], vv[S::kLoadsV];
+        float ks[8], vs[8];
+        int page_k, page_v, page_s;
+        auto pages = [&](int kt) {   // eight keys never lie in two pages
+            page_k = page_of(a.c, r, min(kt + 8 * (col / 4), k1 - 1) >> a.c.page_shift);
+            page_v = page_of(a.c, r, min(kt + row_v / 8 * 8, k1 - 1) >> a.c.page_shift);
+            if constexpr (kEight) page_s = page_of(a.c, r, min(kt + 8 * g, k1 - 1) >> a.c.page_shift);
+        };
+        const int slots = 1 << a.c.page_shift;
+        auto load_k = [&](int kt) {
+            const uint8_t* base = static_cast<const uint8_t*>(a.c.k) + ((((size_t)page_k * H + h) << a.c.page_shift) * S::kRowBytes);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint8_t* p = base + (min(kt + key_k + 4 * t, k1 - 1) & (slots - 1)) * S::kRowBytes;
+#pragma unroll
+                for (int s = 0; s < S::kLoadsK; ++s) kv[t][s] = *reinterpret_cast<const uint4*>(p + 64 * s + 16 * g);
+            }
+        };
+        auto load_v = [&](int kt) {
+            const uint8_t* base = static_cast<const uint8_t*>(a.c.v) + ((((size_t)page_v * H + h) << a.c.page_shift) * S::kRowBytes) + lane % S::kLanesV * 16;
+#pragma unroll
+            for (int n = 0; n < S::kLoadsV; ++n)
+                vv[n] = *reinterpret_cast<const uint4*>(base + (min(kt + row_v + n, k1 - 1) & (slots - 1)) * S::kRowBytes);
+        };
+        auto load_steps = [&](int kt) {
+            const size_t base = (((size_t)page_s * H + h) << a.c.page_shift);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = base + (min(kt + 8 * g + i, k1 - 1) & (slots - 1));
+                ks[i] = a.c.k_scale[at];
+                vs[i] = a.c.v_scale[at];
+            }
+        };
+        constexpr int kStride = kStreamWaves * kStreamKeys;
+        int kt = k0 + wave * kStreamKeys;
+        if (kt < k1) {
+            pages(kt);
+            load_k(kt);
+            load_v(kt);
+            if constexpr (kEight) load_steps(kt);
+        }
+        for (; kt < k1; kt += kStride) {
+            const bool more = kt + kStride < k1;
+            if (more) pages(kt + kStride);
+#pragma unroll
+            for (int n = 0; n < S::kLoadsV; ++n)
+                *reinterpret_cast<uint4*>(lds_v + (row_v + n) * S::kRowBytes + S::swizzle(row_v + n, lane % S::kLanesV) * 16) = vv[n];
+            if (more) load_v(kt + kStride);
+            f32x4_t sc[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s) {
+                    bf16x8_t kf;
+                    if constexpr (kEight) kf = s % 2 ? codes_to_bf16(kv[t][s / 2].z, kv[t][s / 2].w) : codes_to_bf16(kv[t][s / 2].x, kv[t][s / 2].y);
+                    else kf = as_bf16x8(kv[t][s]);
+                    sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[s], sc[t], 0, 0, 0);
+                }
+            }
+            if (more) load_k(kt + kStride);
+            float p[8], top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = sc[i / 4][i % 4];
+                if constexpr (kEight) p[i] *= ks[i];
+                const int key = kt + 8 * g + i;
+                p[i] = key <= pos && key < k1 ? p[i] : -INFINITY;
+                top = fmaxf(top, p[i]);
+            }
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float m_new = fmaxf(m, top), off = m_new == -INFINITY ? 0.f : m_new * a.scale;
+            if (__any(m_new > m)) {
+                const float alpha = __builtin_amdgcn_exp2f(m * a.scale - off);   // 0 where there was no key yet
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) o[d] *= alpha;
+                m = m_new;
+            }
+            uint32_t pw[4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.scale, -off));
+                l += p[i];
+                if constexpr (kEight) p[i] *= vs[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pw[i] = f32x2_to_bf16x2_rne(p[2 * i], p[2 * i + 1]);
+            const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, uint4{pw[0], pw[1], pw[2], pw[3]});
+            if (kEight && more) load_steps(kt + kStride);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                bf16x8_t vf;
+                if constexpr (kEight) {
+                    const int rv = 8 * g + col / 2;
+                    const i32x2_t c = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (__attribute__((address_space(3))) i32x2_t*)(lds_v + rv * S::kRowBytes + S::swizzle(rv, d) * 16 + col % 2 * 8));
+                    vf = codes_to_bf16((uint32_t)c[0], (uint32_t)c[1]);
+                } else {
+                    s16x4_t part[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int rv = 8 * g + 4 * t + col / 4;
+                        part[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(
+                            lds_v + rv * S::kRowBytes + S::swizzle(rv, 2 * d + col % 4 / 2) * 16 + col % 2 * 8));
+                    }
+                    typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+                    const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    vf = __builtin_bit_cast(bf16x8_t, both);
+                }
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[d], 0, 0, 0);
+            }
+        }
+        l += __shfl_xor(l, 16, kWave);
+        l += __shfl_xor(l, 32, kWave);
+
+        // the waves' shares, added up: o[d][i] of lane (col, g) is output 16 d + 4 g + i of row col
+        __syncthreads();   // no wave reads V any more
+        if (g == 0) ml[wave][col] = make_float2(m, l);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4_t*>(lds_o + (wave * 16 + col) * S::kPadO + 16 * d + 4 * g) = o[d];
+        __syncthreads();
+        constexpr int kLanesO = D / 8;   // of an output row, eight values each
+        for (int i = threadIdx.x / kLanesO; i < min(kStreamRows, rows - row0); i += kStreamWaves * kWave / kLanesO) {
+            const int d = threadIdx.x % kLanesO * 8;
+            float top = ml[0][i].x;
+#pragma unroll
+            for (int w = 1; w < kStreamWaves; ++w) top = fmaxf(top, ml[w][i].x);
+            float sum = 0.f, acc[8] = {};
+#pragma unroll
+            for (int w = 0; w < kStreamWaves; ++w) {
+                const float f = ml[w][i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[w][i].x - top) * a.scale);
+                sum = fmaf(f, ml[w][i].y, sum);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = fmaf(f, lds_o[(w * 16 + i) * S::kPadO + d + e], acc[e]);
+            }
+            const size_t at = (size_t)(rq.start + (row0 + i) / a.group) * a.q_heads + h * a.group + (row0 + i) % a.group;
+            if (count == 1) {
+                const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
+                uint4 w;
+                w.x = f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv);
+                w.y = f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv);
+                w.z = f32x2_to_bf16x2_rne(acc[4] * inv, acc[5] * inv);
+                w.w = f32x2_to_bf16x2_rne(acc[6] * inv, acc[7] * inv);
+                *reinterpret_cast<uint4*>(a.out + at * D + d) = w;
+            } else {
+                float4* out = reinterpret_cast<float4*>(a.part_o + (at * a.splits + split) * D + d);
+                out[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                out[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                if (d == 0) a.part_ml[at * a.splits + split] = make_float2(top, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Adds up the shares of the keys: a wave per output row.
+template <int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a) {
+    const int lane = threadIdx.x % kWave;
+    const long long at = (long long)blockIdx.x * 4 + threadIdx.x / kWave;
+    if (at >= (long long)a.c.tokens * a.q_heads) return;   // whole waves
+    const int t = (int)(at / a.q_heads), head = (int)(at % a.q_heads);
+    const int r = request_of(a.c, t);
+    if (r < 0) return;
+    bool bad;
+    const Request rq = request(a.c, r, bad);
+    if (t >= rq.start + rq.n) return;   // not a row of this request: q_start is bad
+    const int row0 = ((t - rq.start) * a.group + head % a.group) / kStreamRows * kStreamRows;
+    const int count = shares(keys_of(rq, a.group, row0, kStreamRows), a.chunk, a.splits);
+    if (count == 1) return;
+    const float2 mine = lane < count ? a.part_ml[at * a.splits + lane] : make_float2(-INFINITY, 0.f);
+    float top = mine.x;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - top) * a.scale);
+    float sum = f * mine.y;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    const float w = sum > 0.f ? f / sum : sum == 0.f ? 0.f : sum;
+    constexpr int kPer = D / kWave;
+    float acc[kPer] = {};
+    for (int s = 0; s < count; ++s) {
+        const float ws = __shfl(w, s, kWave);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ws, a.part_o[(at * a.splits + s) * D + lane * kPer + e], acc[e]);
+    }
+    if constexpr (kPer == 2) reinterpret_cast<uint32_t*>(a.out + at * D)[lane] = f32x2_to_bf16x2_rne(acc[0], acc[1]);
+    else a.out[at * D + lane] = (uint16_t)f32x2_to_bf16x2_rne(acc[0], acc[0]);
+}
+
+// How a step is divided among blocks.
+struct Plan {
+    int splits, chunk;
+};
+Plan plan_for(const qail_kv_cache& c, const qail_requests& b) {
+    const long long units = (long long)b.requests * c.heads;
+    const long long most = std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size);   // at most 2^30
+    long long s = (3ll * device_cu_count() + units - 1) / units;
+    s = std::min<long long>({s, 64, (most + 255) / 256});
+    s = std::max<long long>(s, 1);
+    const int chunk = (int)(((most + s - 1) / s + 127) / 128 * 128);
+    return Plan{(int)s, std::max(chunk, 128)};
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
+    const Plan p = plan_for(c, b);
+    if (p.splits == 1) return 0;
+    const size_t rows = (size_t)b.tokens * q_heads * p.splits;
+    return align256(rows * c.head_dim * sizeof(float)) + align256(rows * sizeof(float2));
+}
+
+hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
+                                  uint16_t* out, uint32_t* errors, void* ws, hipStream_t st) {
+    const Plan p = plan_for(c, b);
+    AttentionArgs a{};
+    a.c = cache_args(c, b, errors);
+    a.q = q;
+    a.out = out;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256((size_t)b.tokens * q_heads * p.splits * c.head_dim * sizeof(float)));
+    a.q_stride = q_stride;
+    a.scale = scale * 1.44269504088896340736f;
+    a.q_heads = q_heads;
+    a.group = q_heads / c.heads;
+    a.splits = p.splits;
+    a.chunk = p.chunk;
+    const bool eight = c.type == QAIL_KV_S8, wide = c.head_dim == 128;
+    const dim3 grid((unsigned)(b.requests * c.heads * p.splits));
+    auto* const stream = wide ? (eight ? attend_stream_kernel<128, true> : attend_stream_kernel<128, false>)
+                              : (eight ? attend_stream_kernel<64, true> : attend_stream_kernel<64, false>);
+    hipLaunchKernelGGL(stream, grid, dim3(kStreamWaves * kWave), 0, st, a);
+    if (p.splits > 1) {
+        const long long rows = (long long)b.tokens * q_heads;
+        auto* const join = wide ? attend_join_kernel<128> : attend_join_kernel<64>;
+        hipLaunchKernelGGL(join, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace qail

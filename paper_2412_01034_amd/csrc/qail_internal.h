@@ -125,4 +125,22 @@ hipError_t launch_w4a4_conv_u4(const qail_conv_desc& d, const uint32_t* a, const
                                const float* bias, float s_out, const uint32_t* res_u4, float res_scale,
                                const float* res_f32, uint32_t* out_u4, hipStream_t st);
 
+// Serving: between a decoder's linears.
+bool rmsnorm_supports(int K);
+hipError_t launch_rmsnorm(const uint16_t* x, const uint16_t* residual, const uint16_t* weight, float eps, int M, int K, uint16_t* h_out,
+                          uint16_t* y, uint32_t* y_s8, float* y_scale, hipStream_t st);
+size_t rmsnorm_back_workspace(int M, int K);
+hipError_t launch_rmsnorm_back(const uint16_t* h, const uint16_t* weight, float eps, const uint16_t* dy, const uint16_t* dres, int M, int K,
+                               uint16_t* dx, float* dweight, float* ws, hipStream_t st);
+hipError_t launch_kv_append(const qail_kv_cache& c, const qail_requests& b, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                            const uint16_t* q, int64_t q_stride, int q_heads, uint16_t* q_out, const float* cos, const float* sin, int positions,
+                            uint32_t* errors, hipStream_t st);
+size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b, int q_heads);
+hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
+                                  uint16_t* out, uint32_t* errors, void* ws, hipStream_t st);
+// fp32 values of workspace for the down-projections of a list; `t` of the two launches has as many
+size_t adapters_workspace(const qail_adapters* ad, int count, int M);
+hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
+hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
+
 }  // namespace qail
