@@ -49,6 +49,36 @@ __device__ __forceinline__ int request_of(const CacheArgs& a, int t) {
     return before - 1;
 }
 
+// Tiles of `height` rows that a request's new tokens make, `group` rows each; none for fewer than min_rows.
+__host__ __device__ __forceinline__ int tiles_of(const Request& q, int group, int min_rows, int height) {
+    const int rows = q.n * group;
+    return rows < min_rows ? 0 : (rows + height - 1) / height;
+}
+
+// The request and the first row of tile `tile` of all of them, counted in the order of the requests; false past the last one.
+__device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_rows, int height, int tile, int& r, int& row0) {
+    const int lane = threadIdx.x % kWave;
+    for (int r0 = 0; r0 < a.requests; r0 += kWave) {
+        bool bad;
+        const int mine = r0 + lane < a.requests ? tiles_of(request(a, r0 + lane, bad), group, min_rows, height) : 0;
+        int sum = mine;   // of this lane's request and those before it
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int left = __shfl_up(sum, o, kWave);
+            if (lane >= o) sum += left;
+        }
+        const unsigned long long past = __ballot(sum > tile);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            r = r0 + at;
+            row0 = (tile - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at))) * height;
+            return true;
+        }
+        tile -= __builtin_amdgcn_readlane(sum, kWave - 1);
+    }
+    return false;
+}
+
 // Whether a token of a request can be written: its position is one that the page table and the table of angles (positions; 0: none) reach.
 __host__ __device__ __forceinline__ bool has_slot(const Request& q, int t, int positions, int& at) {
     at = q.len - q.n + (t - q.start);   // below len: inside the page table

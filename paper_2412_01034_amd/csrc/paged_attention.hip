@@ -7,6 +7,7 @@
 //
 // Rows of one request and one head of the cache: row i is token i / group, head i % group, so grouped heads share every key that is loaded.
 #include <algorithm>
+#include <atomic>
 
 #include "kv_cache.h"
 
@@ -15,7 +16,9 @@ namespace qail {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short s16x8_t;
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;   // (arrays of HIP's own uint4 end up in scratch memory)
 
 struct AttentionArgs {
     CacheArgs c;
@@ -26,10 +29,15 @@ struct AttentionArgs {
     long long q_stride;
     float scale;        // times log2(e)
     int q_heads, group;
-    int splits, chunk;  // keys of a tile of rows are divided into shares of `chunk`, at most `splits`
+    int splits;         // places for partial results of a row
+    int chunk, most;    // keys of a tile of rows are divided into shares of `chunk`, at most `most`
+    int min_rows, max_rows;   // requests with fewer or more rows are left to the other kernel (stream: max_rows, tiles: min_rows)
+    int tiles;          // of rows, at most
+    // the join's: where requests go, and how the tiles' keys are divided
+    int stream_rows, tile_rows, tile_chunk, tile_most;
 };
 
-__device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
+__device__ __forceinline__ bf16x8_t as_bf16x8(const u32x4_t& v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 // Eight signed bytes as bf16 (exact).
 __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
@@ -41,7 +49,7 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
         const float x = (float)(int)(int8_t)(src >> sh), y = (float)(int)(int8_t)(src >> (sh + 8));
         w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);   // upper halves
     }
-    return __builtin_bit_cast(bf16x8_t, uint4{w[0], w[1], w[2], w[3]});
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
 }
 
 // ---------------------------------------------------------------------------- few rows: a stream of keys --
@@ -82,12 +90,13 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
     const Request rq = request(a.c, r, bad);
     if (bad && h == 0 && split == 0 && threadIdx.x == 0) report(a.c);
     const int rows = rq.n * a.group;
+    if (rows > a.max_rows) return;
     uint8_t* const lds_v = lds + wave * kStreamKeys * S::kRowBytes;
     float* const lds_o = reinterpret_cast<float*>(lds);
 
     for (int row0 = 0; row0 < rows; row0 += kStreamRows) {
         const int before = rq.len - rq.n;                            // keys in front of the new ones; may be negative
-        const int keys = keys_of(rq, a.group, row0, kStreamRows), count = shares(keys, a.chunk, a.splits);
+        const int keys = keys_of(rq, a.group, row0, kStreamRows), count = shares(keys, a.chunk, a.most);
         if (split >= count) continue;   // uniform
         const int k0 = share_of(keys, a.chunk, count, split).begin, k1 = share_of(keys, a.chunk, count, split).end;
         const int row = row0 + col, token = row / a.group, head = h * a.group + row % a.group;
@@ -97,7 +106,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) {   // bytes: a lane's 16 codes of K are two steps
             const int d = kEight ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
-            q[s] = as_bf16x8(row < rows ? *reinterpret_cast<const uint4*>(a.q + (rq.start + token) * a.q_stride + head * D + d) : uint4{0u, 0u, 0u, 0u});
+            q[s] = as_bf16x8(row < rows ? *reinterpret_cast<const u32x4_t*>(a.q + (rq.start + token) * a.q_stride + head * D + d) : u32x4_t{0u, 0u, 0u, 0u});
         }
         f32x4_t o[D / 16];
 #pragma unroll
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
         // Of the 32 keys from `kt`, lane group g has keys 8 g .. 8 g + 7 after the first product: row 4 g' + i of tile t is key 8 g' + 4 t + i.
         const int key_k = 8 * (col / 4) + col % 4;
         const int slot_v = lane / S::kLanesV, row_v = 8 * (slot_v / (S::kSlots / 4)) + slot_v % (S::kSlots / 4) * S::kLoadsV;
-        uint4 kv[2][S::kLoadsK], vv[S::kLoadsV];
+        u32x4_t kv[2][S::kLoadsK], vv[S::kLoadsV];
         float ks[8], vs[8];
         int page_k, page_v, page_s;
         auto pages = [&](int kt) {   // eight keys never lie in two pages
@@ -122,14 +131,14 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             for (int t = 0; t < 2; ++t) {
                 const uint8_t* p = base + (min(kt + key_k + 4 * t, k1 - 1) & (slots - 1)) * S::kRowBytes;
 #pragma unroll
-                for (int s = 0; s < S::kLoadsK; ++s) kv[t][s] = *reinterpret_cast<const uint4*>(p + 64 * s + 16 * g);
+                for (int s = 0; s < S::kLoadsK; ++s) kv[t][s] = *reinterpret_cast<const u32x4_t*>(p + 64 * s + 16 * g);
             }
         };
         auto load_v = [&](int kt) {
             const uint8_t* base = static_cast<const uint8_t*>(a.c.v) + ((((size_t)page_v * H + h) << a.c.page_shift) * S::kRowBytes) + lane % S::kLanesV * 16;
 #pragma unroll
             for (int n = 0; n < S::kLoadsV; ++n)
-                vv[n] = *reinterpret_cast<const uint4*>(base + (min(kt + row_v + n, k1 - 1) & (slots - 1)) * S::kRowBytes);
+                vv[n] = *reinterpret_cast<const u32x4_t*>(base + (min(kt + row_v + n, k1 - 1) & (slots - 1)) * S::kRowBytes);
         };
         auto load_steps = [&](int kt) {
             const size_t base = (((size_t)page_s * H + h) << a.c.page_shift);
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             if (more) pages(kt + kStride);
 #pragma unroll
             for (int n = 0; n < S::kLoadsV; ++n)
-                *reinterpret_cast<uint4*>(lds_v + (row_v + n) * S::kRowBytes + S::swizzle(row_v + n, lane % S::kLanesV) * 16) = vv[n];
+                *reinterpret_cast<u32x4_t*>(lds_v + (row_v + n) * S::kRowBytes + S::swizzle(row_v + n, lane % S::kLanesV) * 16) = vv[n];
             if (more) load_v(kt + kStride);
             f32x4_t sc[2];
 #pragma unroll
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) pw[i] = f32x2_to_bf16x2_rne(p[2 * i], p[2 * i + 1]);
-            const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, uint4{pw[0], pw[1], pw[2], pw[3]});
+            const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[0], pw[1], pw[2], pw[3]});
             if (kEight && more) load_steps(kt + kStride);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
@@ -214,7 +223,6 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
                         part[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(
                             lds_v + rv * S::kRowBytes + S::swizzle(rv, 2 * d + col % 4 / 2) * 16 + col % 2 * 8));
                     }
-                    typedef __attribute__((ext_vector_type(8))) short s16x8_t;
                     const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
                     vf = __builtin_bit_cast(bf16x8_t, both);
                 }
@@ -247,12 +255,12 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             const size_t at = (size_t)(rq.start + (row0 + i) / a.group) * a.q_heads + h * a.group + (row0 + i) % a.group;
             if (count == 1) {
                 const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
-                uint4 w;
+                u32x4_t w;
                 w.x = f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv);
                 w.y = f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv);
                 w.z = f32x2_to_bf16x2_rne(acc[4] * inv, acc[5] * inv);
                 w.w = f32x2_to_bf16x2_rne(acc[6] * inv, acc[7] * inv);
-                *reinterpret_cast<uint4*>(a.out + at * D + d) = w;
+                *reinterpret_cast<u32x4_t*>(a.out + at * D + d) = w;
             } else {
                 float4* out = reinterpret_cast<float4*>(a.part_o + (at * a.splits + split) * D + d);
                 out[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -261,6 +269,241 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             }
         }
         __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------- many rows: tiles on the matrix cores --
+//
+// A block takes kTileRows rows against 64 keys at a time, which its four waves stage in LDS together (bytes as bf16 codes; their steps beside
+// them) while they work on the tile before.  Bound by the matrix cores in principle: 4 D operations per score, against about five vector
+// instructions per score and the bytes of both operands from LDS.
+constexpr int kTileWaves = 4, kTileKeys = 64;
+
+template <int D, bool kEight, int kMT>
+struct Tile {
+    static constexpr int kRows = kTileWaves * 32 * kMT;
+    static constexpr int kRowBytes = 2 * D;                        // of LDS
+    static constexpr int kPieces = kEight ? D / 16 : D / 8;        // 16-byte pieces of a row in memory
+    static constexpr int kPass = kTileWaves * kWave / kPieces;     // rows that the block loads at once
+    static constexpr int kLoads = kTileKeys / kPass;
+    static constexpr int kBuffer = 2 * kTileKeys * kRowBytes + (kEight ? 2 * kTileKeys * 4 : 0);   // K, V, their steps
+    static constexpr int kLds = 2 * kBuffer;
+
+    // Pieces of a row are exchanged so that what is read together lies in different banks: K by 16 rows and one piece, V by
+    // four rows and two neighbouring pieces of 32 bytes.
+    __device__ static __forceinline__ int swizzle_k(int row, int piece) { return D == 128 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7); }
+    __device__ static __forceinline__ int swizzle_v(int row, int piece) { return D == 128 ? piece ^ ((row & 3) << 2) : piece ^ ((row & 2) << 1); }
+};
+
+// The larger of a value and its counterpart in the other half of the wave.
+__device__ __forceinline__ float max_of_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = r[0], b = r[1];   // (a bit cast of r[1] itself gives r[0])
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+template <int D, bool kEight, int kMT>
+__global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_tile_kernel(const AttentionArgs a) {
+    using T = Tile<D, kEight, kMT>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int H = a.c.heads;
+    const int h = blockIdx.x % H, split = blockIdx.x / H % a.most, tile = a.tiles - 1 - blockIdx.x / H / a.most;   // the longest first
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, col = lane % 32, half = lane / 32;
+    int r, row0;
+    if (!tile_of(a.c, a.group, a.min_rows, T::kRows, tile, r, row0)) return;
+    bool bad;
+    const Request rq = request(a.c, r, bad);
+    if (bad && h == 0 && split == 0 && row0 == 0 && threadIdx.x == 0) report(a.c);
+    const int rows = rq.n * a.group, before = rq.len - rq.n;
+    const int keys = keys_of(rq, a.group, row0, T::kRows), count = shares(keys, a.chunk, a.most);
+    if (split >= count) return;
+    const Range range = share_of(keys, a.chunk, count, split);
+    const int k1 = range.end;
+
+    bf16x8_t q[kMT][D / 16];
+    int lim[kMT];
+    float m[kMT], l[kMT];
+    f32x16_t o[kMT][D / 32];
+#pragma unroll
+    for (int t = 0; t < kMT; ++t) {
+        const int row = row0 + (wave * kMT + t) * 32 + col, token = row / a.group, head = h * a.group + row % a.group;
+        lim[t] = row < rows ? min(before + token, k1 - 1) : k1 - 1;   // the last key that the row sees; rows past the end are not stored
+        const uint16_t* p = a.q + (rq.start + (row < rows ? token : 0)) * a.q_stride + head * D + 8 * half;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) q[t][s] = as_bf16x8(row < rows ? *reinterpret_cast<const u32x4_t*>(p + 16 * s) : u32x4_t{0u, 0u, 0u, 0u});
+        m[t] = -INFINITY;
+        l[t] = 0.f;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][d][e] = 0.f;
+    }
+
+    // Staging: the block's threads cover kPass rows at a time; 16 rows never lie in two pages.
+    const int piece = threadIdx.x % T::kPieces, row_in = threadIdx.x / T::kPieces, group_in = wave * (kWave / T::kPieces) / 16;
+    const int slots = 1 << a.c.page_shift;
+    u32x4_t kv[T::kLoads], vv[T::kLoads];
+    float step;
+    auto load = [&](int kt) {
+#pragma unroll
+        for (int n = 0; n < T::kLoads; ++n) {
+            const int first = __builtin_amdgcn_readfirstlane(min(kt + n * T::kPass + 16 * group_in, k1 - 1));
+            const size_t base = ((size_t)page_of(a.c, r, first >> a.c.page_shift) * H + h) << a.c.page_shift;
+            const size_t at = (base + (min(kt + n * T::kPass + row_in, k1 - 1) & (slots - 1))) * (T::kPieces * 16) + piece * 16;
+            kv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.k) + at);
+            vv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.v) + at);
+        }
+        if constexpr (kEight) {
+            if (threadIdx.x < 2 * kTileKeys) {   // threads 0 .. 63 a step of K each, 64 .. 127 of V
+                const int key = min(kt + (int)threadIdx.x % kTileKeys, k1 - 1);
+                const size_t at = (((size_t)page_of(a.c, r, key >> a.c.page_shift) * H + h) << a.c.page_shift) + (key & (slots - 1));
+                step = (threadIdx.x < kTileKeys ? a.c.k_scale : a.c.v_scale)[at];
+            }
+        }
+    };
+    auto store = [&](int buffer) {
+        uint8_t* const kb = lds + buffer * T::kBuffer;
+        uint8_t* const vb = kb + kTileKeys * T::kRowBytes;
+#pragma unroll
+        for (int n = 0; n < T::kLoads; ++n) {
+            const int row = n * T::kPass + row_in;
+            if constexpr (kEight) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16x8_t kc = i ? codes_to_bf16(kv[n].z, kv[n].w) : codes_to_bf16(kv[n].x, kv[n].y);
+                    const bf16x8_t vc = i ? codes_to_bf16(vv[n].z, vv[n].w) : codes_to_bf16(vv[n].x, vv[n].y);
+                    *reinterpret_cast<bf16x8_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, 2 * piece + i) * 16) = kc;
+                    *reinterpret_cast<bf16x8_t*>(vb + row * T::kRowBytes + T::swizzle_v(row, 2 * piece + i) * 16) = vc;
+                }
+            } else {
+                *reinterpret_cast<u32x4_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, piece) * 16) = kv[n];
+                *reinterpret_cast<u32x4_t*>(vb + row * T::kRowBytes + T::swizzle_v(row, piece) * 16) = vv[n];
+            }
+        }
+        if constexpr (kEight)
+            if (threadIdx.x < 2 * kTileKeys) reinterpret_cast<float*>(vb + kTileKeys * T::kRowBytes)[threadIdx.x] = step;
+    };
+
+    int kt = range.begin, buffer = 0;
+    if (kt < k1) {
+        load(kt);
+        store(0);
+    }
+    for (; kt < k1; kt += kTileKeys, buffer ^= 1) {
+        __syncthreads();
+        const bool more = kt + kTileKeys < k1;
+        if (more) load(kt + kTileKeys);
+        const uint8_t* const kb = lds + buffer * T::kBuffer;
+        const uint8_t* const vb = kb + kTileKeys * T::kRowBytes;
+        const float* const steps = reinterpret_cast<const float*>(vb + kTileKeys * T::kRowBytes);
+        if (kt <= __builtin_amdgcn_readlane(lim[kMT - 1], 31)) {   // some row of the wave sees a key of the tile
+            f32x16_t sc[kMT][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int t = 0; t < kMT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[t][u][e] = 0.f;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const int row = 32 * u + col;
+                    const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, 2 * s + half) * 16);
+#pragma unroll
+                    for (int t = 0; t < kMT; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[t][s], sc[t][u], 0, 0, 0);
+                }
+            }
+            bf16x8_t pf[kMT][4];
+#pragma unroll
+            for (int t = 0; t < kMT; ++t) {
+                // element e of half u is key kt + 32 u + 8 (e / 4) + 4 half + e % 4
+                if constexpr (kEight) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sc[t][u][e] *= steps[32 * u + 8 * (e / 4) + 4 * half + e % 4];
+                }
+                if (kt + kTileKeys - 1 > __builtin_amdgcn_readfirstlane(lim[t])) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (kt + 32 * u + 8 * (e / 4) + 4 * half + e % 4 > lim[t]) sc[t][u][e] = -INFINITY;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][u][e]);
+                top = max_of_halves(top);
+                // the maximum is followed only where it has grown by more than 2^8: p stays far from overflow, and a tile rarely rescales
+                if (__any((top - m[t]) * a.scale > 8.f)) {
+                    const float m_new = fmaxf(m[t], top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[t] - m_new) * a.scale);
+                    m[t] = m_new;
+                    l[t] *= alpha;
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) o[t][d] *= alpha;
+                }
+                const float off = m[t] == -INFINITY ? 0.f : m[t] * a.scale;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        sc[t][u][e] = __builtin_amdgcn_exp2f(fmaf(sc[t][u][e], a.scale, -off));
+                        l[t] += sc[t][u][e];
+                        if constexpr (kEight) sc[t][u][e] *= steps[kTileKeys + 32 * u + 8 * (e / 4) + 4 * half + e % 4];
+                    }
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = f32x2_to_bf16x2_rne(sc[t][st / 2][8 * (st % 2) + 2 * e], sc[t][st / 2][8 * (st % 2) + 2 * e + 1]);
+                    pf[t][st] = as_bf16x8(u32x4_t{w[0], w[1], w[2], w[3]});
+                }
+            }
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    s16x4_t part[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int row = 16 * st + 8 * j + 4 * half + lane % 16 / 4;
+                        const int piece_v = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
+                        part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(
+                            vb + row * T::kRowBytes + T::swizzle_v(row, piece_v) * 16 + lane % 2 * 8));
+                    }
+                    const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, both);
+#pragma unroll
+                    for (int t = 0; t < kMT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][st], o[t][d], 0, 0, 0);
+                }
+        }
+        if (more) store(buffer ^ 1);
+    }
+
+#pragma unroll
+    for (int t = 0; t < kMT; ++t) {
+        const float sum = l[t] + __shfl_xor(l[t], 32, kWave);
+        const int row = row0 + (wave * kMT + t) * 32 + col;
+        if (row >= rows) continue;
+        const size_t at = (size_t)(rq.start + row / a.group) * a.q_heads + h * a.group + row % a.group;
+        if (count == 1) {
+            const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
+                        uint2{f32x2_to_bf16x2_rne(o[t][d][e] * inv, o[t][d][e + 1] * inv), f32x2_to_bf16x2_rne(o[t][d][e + 2] * inv, o[t][d][e + 3] * inv)};
+        } else {
+            float* out = a.part_o + (at * a.splits + split) * D;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[t][d][e], o[t][d][e + 1], o[t][d][e + 2], o[t][d][e + 3]);
+            if (half == 0) a.part_ml[at * a.splits + split] = make_float2(m[t], sum);
+        }
     }
 }
 
@@ -276,8 +519,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a)
     bool bad;
     const Request rq = request(a.c, r, bad);
     if (t >= rq.start + rq.n) return;   // not a row of this request: q_start is bad
-    const int row0 = ((t - rq.start) * a.group + head % a.group) / kStreamRows * kStreamRows;
-    const int count = shares(keys_of(rq, a.group, row0, kStreamRows), a.chunk, a.splits);
+    const bool tiled = rq.n * a.group > a.stream_rows;
+    const int height = tiled ? a.tile_rows : kStreamRows, row0 = ((t - rq.start) * a.group + head % a.group) / height * height;
+    const int count = shares(keys_of(rq, a.group, row0, height), tiled ? a.tile_chunk : a.chunk, tiled ? a.tile_most : a.most);
     if (count == 1) return;
     const float2 mine = lane < count ? a.part_ml[at * a.splits + lane] : make_float2(-INFINITY, 0.f);
     float top = mine.x;
@@ -299,26 +543,64 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a)
     else a.out[at * D + lane] = (uint16_t)f32x2_to_bf16x2_rne(acc[0], acc[0]);
 }
 
-// How a step is divided among blocks.
+// How a step is divided among blocks: which kernels run (both where requests of few rows and of many may come together) and how
+// the keys are shared.
 struct Plan {
-    int splits, chunk;
+    bool stream, tiles;
+    int row_tiles;
+    int splits, most, tile_most;
+    int chunk, tile_chunk;
+    int stream_rows;   // requests of up to so many rows are the stream's
 };
-Plan plan_for(const qail_kv_cache& c, const qail_requests& b) {
-    const long long units = (long long)b.requests * c.heads;
-    const long long most = std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size);   // at most 2^30
-    long long s = (3ll * device_cu_count() + units - 1) / units;
-    s = std::min<long long>({s, 64, (most + 255) / 256});
-    s = std::max<long long>(s, 1);
-    const int chunk = (int)(((most + s - 1) / s + 127) / 128 * 128);
-    return Plan{(int)s, std::max(chunk, 128)};
+constexpr int kMT = 1;
+int share_size(long long keys, long long count, int unit) { return (int)std::max<long long>((keys + count - 1) / count + unit - 1, unit) / unit * unit; }
+
+Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
+    Plan p{};
+    const int group = q_heads / c.heads, tile_rows = Tile<128, false, kMT>::kRows;
+    const long long keys = std::max<long long>(1, std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size));   // at most 2^30
+    const long long most_rows = (long long)std::min(b.max_new, b.tokens) * group;
+    p.stream = most_rows <= kStreamRows;
+    p.tiles = !p.stream;
+    if (p.tiles && b.requests > 1 && (long long)b.requests * b.max_new != b.tokens && group <= kStreamRows) p.stream = true;
+    p.stream_rows = p.tiles ? (p.stream ? kStreamRows : 0) : INT32_MAX;
+    const long long cus = device_cu_count(), units = (long long)b.requests * c.heads;
+    long long s = 1, ts = 1;
+    if (p.stream) s = std::max(1ll, std::min({(3 * cus + units - 1) / units, 64ll, (keys + 255) / 256}));
+    if (p.tiles) {
+        p.row_tiles = (int)((long long)b.tokens * group / tile_rows) + b.requests;
+        const long long work = std::max(1ll, (long long)b.tokens * group / tile_rows) * c.heads;
+        ts = std::max(1ll, std::min({(2 * cus + work - 1) / work, 64ll, (keys + 511) / 512}));
+    }
+    p.most = (int)s;
+    p.tile_most = (int)ts;
+    p.splits = std::max(p.most, p.tile_most);
+    p.chunk = share_size(keys, s, 128);
+    p.tile_chunk = share_size(keys, ts, kTileKeys);
+    return p;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
+// More than 64 KB of LDS needs an opt-in; the call is idempotent, so two host threads that both find the flag clear may both make it.
+template <int D, bool kEight>
+hipError_t launch_tiles(const AttentionArgs& a, unsigned blocks, hipStream_t st) {
+    using T = Tile<D, kEight, kMT>;
+    static std::atomic<bool> done{false};
+    if (T::kLds > 65536 && !done.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_tile_kernel<D, kEight, kMT>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
+        if (e != hipSuccess) return e;
+        done.store(true, std::memory_order_release);
+    }
+    hipLaunchKernelGGL((attend_tile_kernel<D, kEight, kMT>), dim3(blocks), dim3(kTileWaves * kWave), T::kLds, st, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
-    const Plan p = plan_for(c, b);
+    const Plan p = plan_for(c, b, q_heads);
     if (p.splits == 1) return 0;
     const size_t rows = (size_t)b.tokens * q_heads * p.splits;
     return align256(rows * c.head_dim * sizeof(float)) + align256(rows * sizeof(float2));
@@ -326,7 +608,7 @@ size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b,
 
 hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
                                   uint16_t* out, uint32_t* errors, void* ws, hipStream_t st) {
-    const Plan p = plan_for(c, b);
+    const Plan p = plan_for(c, b, q_heads);
     AttentionArgs a{};
     a.c = cache_args(c, b, errors);
     a.q = q;
@@ -338,12 +620,29 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
     a.q_heads = q_heads;
     a.group = q_heads / c.heads;
     a.splits = p.splits;
-    a.chunk = p.chunk;
+    a.max_rows = p.stream_rows;
+    a.min_rows = p.stream_rows + 1;
+    a.tiles = p.row_tiles;
+    a.stream_rows = p.stream_rows;
+    a.tile_rows = Tile<128, false, kMT>::kRows;
+    a.tile_chunk = p.tile_chunk;
+    a.tile_most = p.tile_most;
     const bool eight = c.type == QAIL_KV_S8, wide = c.head_dim == 128;
-    const dim3 grid((unsigned)(b.requests * c.heads * p.splits));
-    auto* const stream = wide ? (eight ? attend_stream_kernel<128, true> : attend_stream_kernel<128, false>)
-                              : (eight ? attend_stream_kernel<64, true> : attend_stream_kernel<64, false>);
-    hipLaunchKernelGGL(stream, grid, dim3(kStreamWaves * kWave), 0, st, a);
+    if (p.tiles) {   // the longer kernel first
+        a.chunk = p.tile_chunk;
+        a.most = p.tile_most;
+        const unsigned blocks = (unsigned)((long long)p.row_tiles * c.heads * p.tile_most);
+        const hipError_t e = wide ? (eight ? launch_tiles<128, true>(a, blocks, st) : launch_tiles<128, false>(a, blocks, st))
+                                  : (eight ? launch_tiles<64, true>(a, blocks, st) : launch_tiles<64, false>(a, blocks, st));
+        if (e != hipSuccess) return e;
+    }
+    a.chunk = p.chunk;
+    a.most = p.most;
+    if (p.stream) {
+        auto* const stream = wide ? (eight ? attend_stream_kernel<128, true> : attend_stream_kernel<128, false>)
+                                  : (eight ? attend_stream_kernel<64, true> : attend_stream_kernel<64, false>);
+        hipLaunchKernelGGL(stream, dim3((unsigned)((long long)b.requests * c.heads * p.most)), dim3(kStreamWaves * kWave), 0, st, a);
+    }
     if (p.splits > 1) {
         const long long rows = (long long)b.tokens * q_heads;
         auto* const join = wide ? attend_join_kernel<128> : attend_join_kernel<64>;

@@ -66,6 +66,13 @@ void walk(const Arrays& s, bool good) {
         int same;
         CHECK(at == 0 || !has_slot(q, t, at, same), "row %d beyond the angles", t);
     }
+    for (int group : {1, 7, 16, 24})   // the grid has so many tiles of rows
+        for (int height : {128, 256}) {
+            long long tiles = 0;
+            bool bad;
+            for (int r = 0; r < a.requests; ++r) tiles += tiles_of(request(a, r, bad), group, 1, height);
+            CHECK(!good || tiles <= (long long)s.tokens * group / height + a.requests, "%lld tiles of %d", tiles, height);
+        }
     for (int r = 0; r < a.requests; ++r) {
         bool bad;
         const Request q = request(a, r, bad);
