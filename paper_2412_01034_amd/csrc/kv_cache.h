@@ -106,14 +106,14 @@ __host__ __device__ __forceinline__ Range share_of(int keys, int chunk, int coun
 
 __host__ __device__ __forceinline__ bool is_page(int p, int num_pages) { return (unsigned)p < (unsigned)num_pages; }
 
-// A page's number in the cache; one that is not in it becomes page 0 and is reported.
-__device__ __forceinline__ int page_of(const CacheArgs& a, int r, int index) {
-    int p = a.table[(size_t)r * a.max_pages + index];
-    if (!is_page(p, a.num_pages)) {
-        report(a);
-        p = 0;
-    }
-    return p;
+// The entry of the page table, as it is; looked at (below) when it is used, so that no load waits for the one before.
+__device__ __forceinline__ int page_entry(const CacheArgs& a, int r, int index) { return a.table[(size_t)r * a.max_pages + index]; }
+
+// A page's number in the cache: page 0, and `bad`, where an entry is none.
+__device__ __forceinline__ int page_of(const CacheArgs& a, int entry, bool& bad) {
+    const bool in = is_page(entry, a.num_pages);
+    bad = bad || !in;
+    return in ? entry : 0;
 }
 
 }  // namespace qail

@@ -88,9 +88,10 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
     bool bad;
     const Request rq = request(a.c, r, bad);
-    if (bad && h == 0 && split == 0 && threadIdx.x == 0) report(a.c);
     const int rows = rq.n * a.group;
+    if (bad && h == 0 && split == 0 && threadIdx.x == 0) report(a.c);
     if (rows > a.max_rows) return;
+    bad = false;   // from here on: a page
     uint8_t* const lds_v = lds + wave * kStreamKeys * S::kRowBytes;
     float* const lds_o = reinterpret_cast<float*>(lds);
 
@@ -118,15 +119,15 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
         const int slot_v = lane / S::kLanesV, row_v = 8 * (slot_v / (S::kSlots / 4)) + slot_v % (S::kSlots / 4) * S::kLoadsV;
         u32x4_t kv[2][S::kLoadsK], vv[S::kLoadsV];
         float ks[8], vs[8];
-        int page_k, page_v, page_s;
-        auto pages = [&](int kt) {   // eight keys never lie in two pages
-            page_k = page_of(a.c, r, min(kt + 8 * (col / 4), k1 - 1) >> a.c.page_shift);
-            page_v = page_of(a.c, r, min(kt + row_v / 8 * 8, k1 - 1) >> a.c.page_shift);
-            if constexpr (kEight) page_s = page_of(a.c, r, min(kt + 8 * g, k1 - 1) >> a.c.page_shift);
+        int entry_k, entry_v, entry_s;   // of the page table, for the tile that is loaded next
+        auto entries = [&](int kt) {     // eight keys never lie in two pages
+            entry_k = page_entry(a.c, r, min(kt + 8 * (col / 4), k1 - 1) >> a.c.page_shift);
+            entry_v = page_entry(a.c, r, min(kt + row_v / 8 * 8, k1 - 1) >> a.c.page_shift);
+            if constexpr (kEight) entry_s = page_entry(a.c, r, min(kt + 8 * g, k1 - 1) >> a.c.page_shift);
         };
         const int slots = 1 << a.c.page_shift;
         auto load_k = [&](int kt) {
-            const uint8_t* base = static_cast<const uint8_t*>(a.c.k) + ((((size_t)page_k * H + h) << a.c.page_shift) * S::kRowBytes);
+            const uint8_t* base = static_cast<const uint8_t*>(a.c.k) + ((((size_t)page_of(a.c, entry_k, bad) * H + h) << a.c.page_shift) * S::kRowBytes);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const uint8_t* p = base + (min(kt + key_k + 4 * t, k1 - 1) & (slots - 1)) * S::kRowBytes;
@@ -135,13 +136,13 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
             }
         };
         auto load_v = [&](int kt) {
-            const uint8_t* base = static_cast<const uint8_t*>(a.c.v) + ((((size_t)page_v * H + h) << a.c.page_shift) * S::kRowBytes) + lane % S::kLanesV * 16;
+            const uint8_t* base = static_cast<const uint8_t*>(a.c.v) + ((((size_t)page_of(a.c, entry_v, bad) * H + h) << a.c.page_shift) * S::kRowBytes) + lane % S::kLanesV * 16;
 #pragma unroll
             for (int n = 0; n < S::kLoadsV; ++n)
                 vv[n] = *reinterpret_cast<const u32x4_t*>(base + (min(kt + row_v + n, k1 - 1) & (slots - 1)) * S::kRowBytes);
         };
         auto load_steps = [&](int kt) {
-            const size_t base = (((size_t)page_s * H + h) << a.c.page_shift);
+            const size_t base = (((size_t)page_of(a.c, entry_s, bad) * H + h) << a.c.page_shift);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const size_t at = base + (min(kt + 8 * g + i, k1 - 1) & (slots - 1));
@@ -152,14 +153,14 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
         constexpr int kStride = kStreamWaves * kStreamKeys;
         int kt = k0 + wave * kStreamKeys;
         if (kt < k1) {
-            pages(kt);
-            load_k(kt);
+            entries(kt);
             load_v(kt);
+            load_k(kt);
             if constexpr (kEight) load_steps(kt);
+            entries(kt + kStride);   // (the last key's beyond the end)
         }
         for (; kt < k1; kt += kStride) {
             const bool more = kt + kStride < k1;
-            if (more) pages(kt + kStride);
 #pragma unroll
             for (int n = 0; n < S::kLoadsV; ++n)
                 *reinterpret_cast<u32x4_t*>(lds_v + (row_v + n) * S::kRowBytes + S::swizzle(row_v + n, lane % S::kLanesV) * 16) = vv[n];
@@ -206,7 +207,10 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
 #pragma unroll
             for (int i = 0; i < 4; ++i) pw[i] = f32x2_to_bf16x2_rne(p[2 * i], p[2 * i + 1]);
             const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[0], pw[1], pw[2], pw[3]});
-            if (kEight && more) load_steps(kt + kStride);
+            if (more) {
+                if constexpr (kEight) load_steps(kt + kStride);
+                entries(kt + 2 * kStride);
+            }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 bf16x8_t vf;
@@ -270,6 +274,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
         }
         __syncthreads();
     }
+    if (bad) report(a.c);
 }
 
 // ---------------------------------------------------------------------------- many rows: tiles on the matrix cores --
@@ -317,6 +322,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
     const int rows = rq.n * a.group, before = rq.len - rq.n;
     const int keys = keys_of(rq, a.group, row0, T::kRows), count = shares(keys, a.chunk, a.most);
     if (split >= count) return;
+    bad = false;   // from here on: a page
     const Range range = share_of(keys, a.chunk, count, split);
     const int k1 = range.end;
 
@@ -344,11 +350,16 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
     const int slots = 1 << a.c.page_shift;
     u32x4_t kv[T::kLoads], vv[T::kLoads];
     float step;
+    int entry[T::kLoads], entry_s;   // of the page table, for the tile that is loaded next
+    auto entries = [&](int kt) {
+#pragma unroll
+        for (int n = 0; n < T::kLoads; ++n) entry[n] = page_entry(a.c, r, min(kt + n * T::kPass + 16 * group_in, k1 - 1) >> a.c.page_shift);
+        if constexpr (kEight) entry_s = page_entry(a.c, r, min(kt + (int)threadIdx.x % kTileKeys, k1 - 1) >> a.c.page_shift);
+    };
     auto load = [&](int kt) {
 #pragma unroll
         for (int n = 0; n < T::kLoads; ++n) {
-            const int first = __builtin_amdgcn_readfirstlane(min(kt + n * T::kPass + 16 * group_in, k1 - 1));
-            const size_t base = ((size_t)page_of(a.c, r, first >> a.c.page_shift) * H + h) << a.c.page_shift;
+            const size_t base = ((size_t)page_of(a.c, entry[n], bad) * H + h) << a.c.page_shift;
             const size_t at = (base + (min(kt + n * T::kPass + row_in, k1 - 1) & (slots - 1))) * (T::kPieces * 16) + piece * 16;
             kv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.k) + at);
             vv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.v) + at);
@@ -356,7 +367,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
         if constexpr (kEight) {
             if (threadIdx.x < 2 * kTileKeys) {   // threads 0 .. 63 a step of K each, 64 .. 127 of V
                 const int key = min(kt + (int)threadIdx.x % kTileKeys, k1 - 1);
-                const size_t at = (((size_t)page_of(a.c, r, key >> a.c.page_shift) * H + h) << a.c.page_shift) + (key & (slots - 1));
+                const size_t at = (((size_t)page_of(a.c, entry_s, bad) * H + h) << a.c.page_shift) + (key & (slots - 1));
                 step = (threadIdx.x < kTileKeys ? a.c.k_scale : a.c.v_scale)[at];
             }
         }
@@ -386,13 +397,18 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
 
     int kt = range.begin, buffer = 0;
     if (kt < k1) {
+        entries(kt);
         load(kt);
+        entries(kt + kTileKeys);   // (the last key's beyond the end)
         store(0);
     }
     for (; kt < k1; kt += kTileKeys, buffer ^= 1) {
         __syncthreads();
         const bool more = kt + kTileKeys < k1;
-        if (more) load(kt + kTileKeys);
+        if (more) {
+            load(kt + kTileKeys);
+            entries(kt + 2 * kTileKeys);
+        }
         const uint8_t* const kb = lds + buffer * T::kBuffer;
         const uint8_t* const vb = kb + kTileKeys * T::kRowBytes;
         const float* const steps = reinterpret_cast<const float*>(vb + kTileKeys * T::kRowBytes);
@@ -480,6 +496,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
         }
         if (more) store(buffer ^ 1);
     }
+    if (bad) report(a.c);
 
 #pragma unroll
     for (int t = 0; t < kMT; ++t) {
@@ -507,15 +524,13 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
     }
 }
 
-// Adds up the shares of the keys: a wave per output row.
+// Adds up the shares of the keys: a block has four heads of one token, a wave each.
+constexpr int kJoinHeads = 4;
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a) {
-    const int lane = threadIdx.x % kWave;
-    const long long at = (long long)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (at >= (long long)a.c.tokens * a.q_heads) return;   // whole waves
-    const int t = (int)(at / a.q_heads), head = (int)(at % a.q_heads);
+__global__ __launch_bounds__(kJoinHeads* kWave) void attend_join_kernel(const AttentionArgs a) {
+    const int lane = threadIdx.x % kWave, t = blockIdx.x, head = blockIdx.y * kJoinHeads + threadIdx.x / kWave;
     const int r = request_of(a.c, t);
-    if (r < 0) return;
+    if (r < 0 || head >= a.q_heads) return;   // whole waves
     bool bad;
     const Request rq = request(a.c, r, bad);
     if (t >= rq.start + rq.n) return;   // not a row of this request: q_start is bad
@@ -523,6 +538,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a)
     const int height = tiled ? a.tile_rows : kStreamRows, row0 = ((t - rq.start) * a.group + head % a.group) / height * height;
     const int count = shares(keys_of(rq, a.group, row0, height), tiled ? a.tile_chunk : a.chunk, tiled ? a.tile_most : a.most);
     if (count == 1) return;
+    const size_t at = (size_t)t * a.q_heads + head;
     const float2 mine = lane < count ? a.part_ml[at * a.splits + lane] : make_float2(-INFINITY, 0.f);
     float top = mine.x;
 #pragma unroll
@@ -533,11 +549,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttentionArgs a)
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
     const float w = sum > 0.f ? f / sum : sum == 0.f ? 0.f : sum;
     constexpr int kPer = D / kWave;
+    const float* part = a.part_o + at * a.splits * D + lane * kPer;
     float acc[kPer] = {};
     for (int s = 0; s < count; ++s) {
         const float ws = __shfl(w, s, kWave);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ws, a.part_o[(at * a.splits + s) * D + lane * kPer + e], acc[e]);
+        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ws, part[(size_t)s * D + e], acc[e]);
     }
     if constexpr (kPer == 2) reinterpret_cast<uint32_t*>(a.out + at * D)[lane] = f32x2_to_bf16x2_rne(acc[0], acc[1]);
     else a.out[at * D + lane] = (uint16_t)f32x2_to_bf16x2_rne(acc[0], acc[0]);
@@ -644,9 +661,8 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
         hipLaunchKernelGGL(stream, dim3((unsigned)((long long)b.requests * c.heads * p.most)), dim3(kStreamWaves * kWave), 0, st, a);
     }
     if (p.splits > 1) {
-        const long long rows = (long long)b.tokens * q_heads;
         auto* const join = wide ? attend_join_kernel<128> : attend_join_kernel<64>;
-        hipLaunchKernelGGL(join, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(join, dim3((unsigned)b.tokens, (unsigned)((q_heads + kJoinHeads - 1) / kJoinHeads)), dim3(kJoinHeads * kWave), 0, st, a);
     }
     return hipGetLastError();
 }
