@@ -33,8 +33,7 @@ struct AttentionArgs {
     int chunk, most;    // keys of a tile of rows are divided into shares of `chunk`, at most `most`
     int min_rows, max_rows;   // requests with fewer or more rows are left to the other kernel (stream: max_rows, tiles: min_rows)
     int tiles;          // of rows, at most
-    // the join's: where requests go, and how the tiles' keys are divided
-    int stream_rows, tile_rows, tile_chunk, tile_most;
+    int tile_rows;      // of a tile
 };
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(const u32x4_t& v) { return __builtin_bit_cast(bf16x8_t, v); }
@@ -524,21 +523,15 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
     }
 }
 
-// Adds up the shares of the keys: a block has four heads of one token, a wave each.
-constexpr int kJoinHeads = 4;
+// Adds up the shares of the keys that one of the two kernels above has left: a wave per output row.  The stream's requests have few rows, which
+// blocks of a request walk through; the tiles' have many, a block each four heads of a token.
+constexpr int kJoinWaves = 4;
 template <int D>
-__global__ __launch_bounds__(kJoinHeads* kWave) void attend_join_kernel(const AttentionArgs a) {
-    const int lane = threadIdx.x % kWave, t = blockIdx.x, head = blockIdx.y * kJoinHeads + threadIdx.x / kWave;
-    const int r = request_of(a.c, t);
-    if (r < 0 || head >= a.q_heads) return;   // whole waves
-    bool bad;
-    const Request rq = request(a.c, r, bad);
-    if (t >= rq.start + rq.n) return;   // not a row of this request: q_start is bad
-    const bool tiled = rq.n * a.group > a.stream_rows;
-    const int height = tiled ? a.tile_rows : kStreamRows, row0 = ((t - rq.start) * a.group + head % a.group) / height * height;
-    const int count = shares(keys_of(rq, a.group, row0, height), tiled ? a.tile_chunk : a.chunk, tiled ? a.tile_most : a.most);
+__device__ __forceinline__ void join_row(const AttentionArgs& a, const Request& rq, int head, int token, int height) {
+    const int lane = threadIdx.x % kWave, row0 = (token * a.group + head % a.group) / height * height;
+    const int count = shares(keys_of(rq, a.group, row0, height), a.chunk, a.most);
     if (count == 1) return;
-    const size_t at = (size_t)t * a.q_heads + head;
+    const size_t at = (size_t)(rq.start + token) * a.q_heads + head;
     const float2 mine = lane < count ? a.part_ml[at * a.splits + lane] : make_float2(-INFINITY, 0.f);
     float top = mine.x;
 #pragma unroll
@@ -558,6 +551,22 @@ __global__ __launch_bounds__(kJoinHeads* kWave) void attend_join_kernel(const At
     }
     if constexpr (kPer == 2) reinterpret_cast<uint32_t*>(a.out + at * D)[lane] = f32x2_to_bf16x2_rne(acc[0], acc[1]);
     else a.out[at * D + lane] = (uint16_t)f32x2_to_bf16x2_rne(acc[0], acc[0]);
+}
+
+template <int D, bool kTiles>
+__global__ __launch_bounds__(kJoinWaves* kWave) void attend_join_kernel(const AttentionArgs a) {
+    const int head = blockIdx.y * kJoinWaves + threadIdx.x / kWave;
+    const int r = kTiles ? request_of(a.c, blockIdx.x) : blockIdx.x;
+    if (r < 0 || head >= a.q_heads) return;   // whole waves
+    bool bad;
+    const Request rq = request(a.c, r, bad);
+    const int rows = rq.n * a.group;
+    if constexpr (kTiles) {
+        const int token = (int)blockIdx.x - rq.start;
+        if (token < rq.n && rows >= a.min_rows) join_row<D>(a, rq, head, token, a.tile_rows);   // (token >= n: q_start is bad)
+    } else if (rows <= a.max_rows) {
+        for (int token = 0; token < rq.n; ++token) join_row<D>(a, rq, head, token, kStreamRows);
+    }
 }
 
 // How a step is divided among blocks: which kernels run (both where requests of few rows and of many may come together) and how
@@ -640,11 +649,9 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
     a.max_rows = p.stream_rows;
     a.min_rows = p.stream_rows + 1;
     a.tiles = p.row_tiles;
-    a.stream_rows = p.stream_rows;
     a.tile_rows = Tile<128, false, kMT>::kRows;
-    a.tile_chunk = p.tile_chunk;
-    a.tile_most = p.tile_most;
     const bool eight = c.type == QAIL_KV_S8, wide = c.head_dim == 128;
+    const unsigned head_blocks = (unsigned)((q_heads + kJoinWaves - 1) / kJoinWaves);
     if (p.tiles) {   // the longer kernel first
         a.chunk = p.tile_chunk;
         a.most = p.tile_most;
@@ -652,17 +659,21 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
         const hipError_t e = wide ? (eight ? launch_tiles<128, true>(a, blocks, st) : launch_tiles<128, false>(a, blocks, st))
                                   : (eight ? launch_tiles<64, true>(a, blocks, st) : launch_tiles<64, false>(a, blocks, st));
         if (e != hipSuccess) return e;
+        if (p.tile_most > 1) {
+            auto* const join = wide ? attend_join_kernel<128, true> : attend_join_kernel<64, true>;
+            hipLaunchKernelGGL(join, dim3((unsigned)b.tokens, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+        }
     }
-    a.chunk = p.chunk;
-    a.most = p.most;
     if (p.stream) {
+        a.chunk = p.chunk;
+        a.most = p.most;
         auto* const stream = wide ? (eight ? attend_stream_kernel<128, true> : attend_stream_kernel<128, false>)
                                   : (eight ? attend_stream_kernel<64, true> : attend_stream_kernel<64, false>);
         hipLaunchKernelGGL(stream, dim3((unsigned)((long long)b.requests * c.heads * p.most)), dim3(kStreamWaves * kWave), 0, st, a);
-    }
-    if (p.splits > 1) {
-        auto* const join = wide ? attend_join_kernel<128> : attend_join_kernel<64>;
-        hipLaunchKernelGGL(join, dim3((unsigned)b.tokens, (unsigned)((q_heads + kJoinHeads - 1) / kJoinHeads)), dim3(kJoinHeads * kWave), 0, st, a);
+        if (p.most > 1) {
+            auto* const join = wide ? attend_join_kernel<128, false> : attend_join_kernel<64, false>;
+            hipLaunchKernelGGL(join, dim3((unsigned)b.requests, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+        }
     }
     return hipGetLastError();
 }
