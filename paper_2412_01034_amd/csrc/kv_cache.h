@@ -49,11 +49,48 @@ __device__ __forceinline__ int request_of(const CacheArgs& a, int t) {
     return before - 1;
 }
 
+// Keys that rows row0 .. row0 + count - 1 of a request see (its last row's), `group` rows a token.
+__host__ __device__ __forceinline__ int keys_of(const Request& q, int group, int row0, int count) {
+    const int rows = q.n * group, last = row0 + count < rows ? row0 + count - 1 : rows - 1;
+    const int keys = q.len - q.n + last / group + 1;
+    return keys > 0 ? keys : 0;
+}
+
 // Tiles of `height` rows that a request's new tokens make, `group` rows each; none for fewer than min_rows.
 __host__ __device__ __forceinline__ int tiles_of(const Request& q, int group, int min_rows, int height) {
     const int rows = q.n * group;
     return rows < min_rows ? 0 : (rows + height - 1) / height;
 }
+
+// Reports requests whose q_start is bad: they have no rows, so no block comes across them.
+__device__ __forceinline__ void report_rows(const CacheArgs& a) {
+    for (int r = threadIdx.x; r < a.requests; r += blockDim.x) {
+        bool bad;
+        const Request q = request(a, r, bad);
+        if (bad && q.n == 0) report(a);
+    }
+}
+
+// Few rows: the work of a request for one head of the cache, in steps of kStepKeys keys for a tile of kStreamRows rows.  (Every tile of a
+// request counts as many steps as its last.)
+constexpr int kStreamRows = 16, kStepKeys = 128;
+struct Steps {
+    int tiles, steps;   // steps of each tile: at least one, which writes zeros where there is no key
+};
+__host__ __device__ __forceinline__ Steps steps_of(const Request& q, int group, int max_rows) {
+    const int rows = q.n * group;
+    if (rows == 0 || rows > max_rows) return Steps{0, 0};
+    const int keys = keys_of(q, group, 0, rows), steps = (keys + kStepKeys - 1) / kStepKeys;
+    return Steps{(rows + kStreamRows - 1) / kStreamRows, steps > 1 ? steps : 1};
+}
+// The steps of all requests, heads and tiles in a row are cut into equal shares, one a block.
+__host__ __device__ __forceinline__ long long steps_of_a_share(long long total, int blocks, int least) {
+    const long long s = (total + blocks - 1) / blocks;
+    return s > least ? s : least;
+}
+// Where block b leaves its part of a tile whose steps begin at `begin`, if that is not all of it: a block can have two such tiles, one
+// that has begun before it and one that goes on after it.
+__host__ __device__ __forceinline__ long long place_of(long long begin, long long b, long long share) { return 2 * b + (begin >= b * share ? 1 : 0); }
 
 // The request and the first row of tile `tile` of all of them, counted in the order of the requests; false past the last one.
 __device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_rows, int height, int tile, int& r, int& row0) {
@@ -83,13 +120,6 @@ __device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_r
 __host__ __device__ __forceinline__ bool has_slot(const Request& q, int t, int positions, int& at) {
     at = q.len - q.n + (t - q.start);   // below len: inside the page table
     return t >= q.start && t < q.start + q.n && at >= 0 && (positions == 0 || at < positions);
-}
-
-// Keys that rows row0 .. row0 + count - 1 of a request see (its last row's), `group` rows a token.
-__host__ __device__ __forceinline__ int keys_of(const Request& q, int group, int row0, int count) {
-    const int rows = q.n * group, last = row0 + count < rows ? row0 + count - 1 : rows - 1;
-    const int keys = q.len - q.n + last / group + 1;
-    return keys > 0 ? keys : 0;
 }
 
 // Shares that `keys` are divided into: `chunk` each, at most `most` of them, of which the last takes what is left.

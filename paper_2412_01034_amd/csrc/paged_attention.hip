@@ -24,16 +24,15 @@ struct AttentionArgs {
     CacheArgs c;
     const uint16_t* q;
     uint16_t* out;
-    float* part_o;      // [tokens][q_heads][splits][D]: outputs of a share of the keys, not yet divided by their sum
-    float2* part_ml;    // [tokens][q_heads][splits]: their maximum and sum
+    float* part_o;      // partial results, D values each, not yet divided by their sum,
+    float2* part_ml;    // and their maximum and sum: [places][16] of the stream, [tokens][q_heads][most] of the tiles
     long long q_stride;
     float scale;        // times log2(e)
     int q_heads, group;
-    int splits;         // places for partial results of a row
-    int chunk, most;    // keys of a tile of rows are divided into shares of `chunk`, at most `most`
-    int min_rows, max_rows;   // requests with fewer or more rows are left to the other kernel (stream: max_rows, tiles: min_rows)
-    int tiles;          // of rows, at most
-    int tile_rows;      // of a tile
+    // stream: requests of at most max_rows rows; all steps shared by `blocks` blocks, `least` of them each, or a block for each request and head
+    int max_rows, shared, blocks, least;
+    // tiles: requests of at least min_rows rows in at most `tiles` tiles of tile_rows; their keys in shares of `chunk`, at most `most`
+    int min_rows, tiles, tile_rows, chunk, most;
 };
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(const u32x4_t& v) { return __builtin_bit_cast(bf16x8_t, v); }
@@ -57,7 +56,10 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
 // once.  A wave takes 32 keys at a time, on its own: K goes from memory into the registers that the first product reads,
 // V through the wave's part of LDS, which is read transposed.  The four waves of a block take tiles in turn and add up at the end.
 // Rows past the last key repeat it (its slot holds a token, which slots behind it need not) and get a score of minus infinity.
-constexpr int kStreamWaves = 4, kStreamKeys = 32, kStreamRows = 16;
+constexpr int kStreamWaves = 4, kStreamKeys = 32;   // a step (kStepKeys) is a tile of keys for each wave
+static_assert(kStreamWaves * kStreamKeys == kStepKeys, "a step is a tile of keys for each wave");
+
+constexpr int stream_blocks(int head_dim) { return head_dim == 64 ? 3 : 2; }   // that a compute unit holds: by registers
 
 template <int D, bool kEight>
 struct Stream {
@@ -77,28 +79,17 @@ struct Stream {
     }
 };
 
+// Keys k0 .. k1 - 1 of request r and head h for its rows from row0.  place < 0: these are all keys, the outputs are written; else they are left
+// in that place, with their maximum and sum, for the join.
 template <int D, bool kEight>
-__global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(const AttentionArgs a) {
+__device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds, float2 (*ml)[kStreamRows], const Request& rq, int r, int h, int row0, int k0, int k1,
+                                            long long place, bool& bad) {
     using S = Stream<D, kEight>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
-    __shared__ float2 ml[kStreamWaves][16];
-    const int H = a.c.heads, R = a.c.requests;
-    const int h = blockIdx.x % H, r = blockIdx.x / H % R, split = blockIdx.x / H / R;
+    const int H = a.c.heads, rows = rq.n * a.group, before = rq.len - rq.n;   // keys in front of the new ones; may be negative
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
-    bool bad;
-    const Request rq = request(a.c, r, bad);
-    const int rows = rq.n * a.group;
-    if (bad && h == 0 && split == 0 && threadIdx.x == 0) report(a.c);
-    if (rows > a.max_rows) return;
-    bad = false;   // from here on: a page
     uint8_t* const lds_v = lds + wave * kStreamKeys * S::kRowBytes;
     float* const lds_o = reinterpret_cast<float*>(lds);
-
-    for (int row0 = 0; row0 < rows; row0 += kStreamRows) {
-        const int before = rq.len - rq.n;                            // keys in front of the new ones; may be negative
-        const int keys = keys_of(rq, a.group, row0, kStreamRows), count = shares(keys, a.chunk, a.most);
-        if (split >= count) continue;   // uniform
-        const int k0 = share_of(keys, a.chunk, count, split).begin, k1 = share_of(keys, a.chunk, count, split).end;
+    {
         const int row = row0 + col, token = row / a.group, head = h * a.group + row % a.group;
         const int pos = row < rows ? before + token : -1;
 
@@ -149,7 +140,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
                 vs[i] = a.c.v_scale[at];
             }
         };
-        constexpr int kStride = kStreamWaves * kStreamKeys;
+        constexpr int kStride = kStepKeys;
         int kt = k0 + wave * kStreamKeys;
         if (kt < k1) {
             entries(kt);
@@ -256,7 +247,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
                 for (int e = 0; e < 8; ++e) acc[e] = fmaf(f, lds_o[(w * 16 + i) * S::kPadO + d + e], acc[e]);
             }
             const size_t at = (size_t)(rq.start + (row0 + i) / a.group) * a.q_heads + h * a.group + (row0 + i) % a.group;
-            if (count == 1) {
+            if (place < 0) {
                 const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
                 u32x4_t w;
                 w.x = f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv);
@@ -265,15 +256,154 @@ __global__ __launch_bounds__(kStreamWaves* kWave, 2) void attend_stream_kernel(c
                 w.w = f32x2_to_bf16x2_rne(acc[6] * inv, acc[7] * inv);
                 *reinterpret_cast<u32x4_t*>(a.out + at * D + d) = w;
             } else {
-                float4* out = reinterpret_cast<float4*>(a.part_o + (at * a.splits + split) * D + d);
+                const long long to = place * kStreamRows + i;
+                float4* out = reinterpret_cast<float4*>(a.part_o + to * D + d);
                 out[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
                 out[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                if (d == 0) a.part_ml[at * a.splits + split] = make_float2(top, sum);
+                if (d == 0) a.part_ml[to] = make_float2(top, sum);
             }
         }
         __syncthreads();
     }
-    if (bad) report(a.c);
+}
+
+// The steps of 64 requests and those before them in the same 64: what lane i holds is request first + i's.
+struct Scan {
+    long long mine, sum;
+};
+__device__ __forceinline__ Scan scan_steps(const AttentionArgs& a, int first) {
+    const int r = first + (int)threadIdx.x % kWave;
+    bool bad;
+    const Steps s = r < a.c.requests ? steps_of(request(a.c, r, bad), a.group, a.max_rows) : Steps{0, 0};
+    Scan v;
+    v.mine = v.sum = (long long)s.tiles * s.steps * a.c.heads;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const long long left = __shfl_up(v.sum, o, kWave);
+        if ((int)threadIdx.x % kWave >= o) v.sum += left;
+    }
+    return v;
+}
+__device__ __forceinline__ long long value_of_lane(long long v, int lane) {
+    return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
+}
+
+template <int D, bool kEight>
+__global__ __launch_bounds__(kStreamWaves* kWave, stream_blocks(D)) void attend_stream_kernel(const AttentionArgs a) {
+    using S = Stream<D, kEight>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[S::kLds];
+    __shared__ float2 ml[kStreamWaves][kStreamRows];
+    const int H = a.c.heads;
+    bool bad;
+    if (!a.shared) {   // a block for each request and head
+        const int r = blockIdx.x / H, h = blockIdx.x % H;
+        const Request rq = request(a.c, r, bad);
+        if (bad && h == 0 && threadIdx.x == 0) report(a.c);
+        bad = false;   // from here on: a page
+        const Steps s = steps_of(rq, a.group, a.max_rows);
+        for (int t = 0; t < s.tiles; ++t)
+            attend_rows<D, kEight>(a, lds, ml, rq, r, h, t * kStreamRows, 0, keys_of(rq, a.group, t * kStreamRows, kStreamRows), -1, bad);
+        if (bad) report(a.c);
+        return;
+    }
+    const Scan near = scan_steps(a, 0);
+    long long total = value_of_lane(near.sum, kWave - 1);
+    for (int r0 = kWave; r0 < a.c.requests; r0 += kWave) total += value_of_lane(scan_steps(a, r0).sum, kWave - 1);
+    const long long share = steps_of_a_share(total, gridDim.x, a.least), end = min((blockIdx.x + 1ll) * share, total);
+    bool page_bad = false;
+    for (long long p = blockIdx.x * share; p < end;) {
+        int r = 0;
+        long long first = 0;   // step of the request's beginning
+        for (int r0 = 0; r0 < a.c.requests; r0 += kWave) {   // p < total: one is found
+            const Scan v = r0 == 0 ? near : scan_steps(a, r0);
+            const unsigned long long past = __ballot(first + v.sum > p);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                r = r0 + at;
+                first += value_of_lane(v.sum, at) - value_of_lane(v.mine, at);
+                break;
+            }
+            first += value_of_lane(v.sum, kWave - 1);
+        }
+        const Request rq = request(a.c, r, bad);
+        const Steps s = steps_of(rq, a.group, a.max_rows);
+        if (bad && p == first && threadIdx.x == 0) report(a.c);
+        const int unit = (int)((p - first) / s.steps), step = (int)((p - first) % s.steps), h = unit / s.tiles, row0 = unit % s.tiles * kStreamRows;
+        const int steps = (int)min((long long)(s.steps - step), end - p);
+        const int keys = keys_of(rq, a.group, row0, kStreamRows);
+        attend_rows<D, kEight>(a, lds, ml, rq, r, h, row0, min(step * kStepKeys, keys), min((step + steps) * kStepKeys, keys),
+                               steps == s.steps ? -1 : place_of(p - step, blockIdx.x, share), page_bad);
+        p += steps;
+    }
+    if (page_bad) report(a.c);
+    if (blockIdx.x == 0) report_rows(a.c);
+}
+
+// Adds up what the stream's blocks have left: a wave per output row, which walks through the request's tokens.
+constexpr int kJoinWaves = 4;
+
+// The sum of `count` partial results, the i-th in place(i), as bf16 to `out`.
+template <int D, typename F>
+__device__ __forceinline__ void join_row(const AttentionArgs& a, long long count, uint16_t* out, F place) {
+    const int lane = threadIdx.x % kWave;
+    float top = -INFINITY;
+    for (long long i = lane; i < count; i += kWave) top = fmaxf(top, a.part_ml[place(i)].x);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    // D / 4 lanes take a partial result, the wave several at a time and four times as many on their way
+    constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (long long i0 = 0; i0 < count; i0 += 4 * kAtOnce) {
+        f32x4_t v[4];
+        float2 ml[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {   // past the end the last is read again and not counted
+            const long long at = place(min(i0 + u * kAtOnce + lane / kLanes, count - 1));
+            v[u] = reinterpret_cast<const f32x4_t*>(a.part_o + at * D)[lane % kLanes];
+            ml[u] = a.part_ml[at];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u * kAtOnce + lane / kLanes >= count || ml[u].x == -INFINITY) continue;   // (no key: a sum of 0)
+            const float w = __builtin_amdgcn_exp2f((ml[u].x - top) * a.scale);
+            sum = fmaf(w, ml[u].y, sum);
+            acc += v[u] * w;
+        }
+    }
+#pragma unroll
+    for (int o = kLanes; o < kWave; o <<= 1) {
+        sum += __shfl_xor(sum, o, kWave);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;
+    if (lane < kLanes) reinterpret_cast<uint2*>(out)[lane] = uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
+}
+
+template <int D>
+__global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const AttentionArgs a) {
+    const int r = blockIdx.x, head = blockIdx.y * kJoinWaves + threadIdx.x / kWave;
+    if (head >= a.q_heads) return;   // whole waves
+    long long total = 0, first = 0;
+    for (int r0 = 0; r0 < a.c.requests; r0 += kWave) {
+        const Scan v = scan_steps(a, r0);
+        if (r >= r0 && r < r0 + kWave) first = total + value_of_lane(v.sum, r - r0) - value_of_lane(v.mine, r - r0);
+        total += value_of_lane(v.sum, kWave - 1);
+    }
+    const long long share = steps_of_a_share(total, a.blocks, a.least);
+    bool bad;
+    const Request rq = request(a.c, r, bad);
+    const Steps s = steps_of(rq, a.group, a.max_rows);
+    if (s.tiles == 0) return;
+    for (int token = 0; token < rq.n; ++token) {
+        const int row = token * a.group + head % a.group;
+        const long long begin = first + ((long long)(head / a.group) * s.tiles + row / kStreamRows) * s.steps;
+        const long long b0 = begin / share, count = (begin + s.steps - 1) / share - b0 + 1;
+        if (count == 1) continue;
+        join_row<D>(a, count, a.out + ((size_t)(rq.start + token) * a.q_heads + head) * D,
+                    [&](long long i) { return place_of(begin, b0 + i, share) * kStreamRows + row % kStreamRows; });
+    }
 }
 
 // ---------------------------------------------------------------------------- many rows: tiles on the matrix cores --
@@ -314,6 +444,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
     const int h = blockIdx.x % H, split = blockIdx.x / H % a.most, tile = a.tiles - 1 - blockIdx.x / H / a.most;   // the longest first
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, col = lane % 32, half = lane / 32;
     int r, row0;
+    if (blockIdx.x == 0) report_rows(a.c);
     if (!tile_of(a.c, a.group, a.min_rows, T::kRows, tile, r, row0)) return;
     bool bad;
     const Request rq = request(a.c, r, bad);
@@ -512,124 +643,115 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
                     *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
                         uint2{f32x2_to_bf16x2_rne(o[t][d][e] * inv, o[t][d][e + 1] * inv), f32x2_to_bf16x2_rne(o[t][d][e + 2] * inv, o[t][d][e + 3] * inv)};
         } else {
-            float* out = a.part_o + (at * a.splits + split) * D;
+            float* out = a.part_o + (at * a.most + split) * D;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
                     *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[t][d][e], o[t][d][e + 1], o[t][d][e + 2], o[t][d][e + 3]);
-            if (half == 0) a.part_ml[at * a.splits + split] = make_float2(m[t], sum);
+            if (half == 0) a.part_ml[at * a.most + split] = make_float2(m[t], sum);
         }
     }
 }
 
-// Adds up the shares of the keys that one of the two kernels above has left: a wave per output row.  The stream's requests have few rows, which
-// blocks of a request walk through; the tiles' have many, a block each four heads of a token.
-constexpr int kJoinWaves = 4;
+// Adds up the shares of the keys of a tile of rows: a block has four heads of a token, a wave each.
 template <int D>
-__device__ __forceinline__ void join_row(const AttentionArgs& a, const Request& rq, int head, int token, int height) {
-    const int lane = threadIdx.x % kWave, row0 = (token * a.group + head % a.group) / height * height;
-    const int count = shares(keys_of(rq, a.group, row0, height), a.chunk, a.most);
-    if (count == 1) return;
-    const size_t at = (size_t)(rq.start + token) * a.q_heads + head;
-    const float2 mine = lane < count ? a.part_ml[at * a.splits + lane] : make_float2(-INFINITY, 0.f);
-    float top = mine.x;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-    const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - top) * a.scale);
-    float sum = f * mine.y;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-    const float w = sum > 0.f ? f / sum : sum == 0.f ? 0.f : sum;
-    constexpr int kPer = D / kWave;
-    const float* part = a.part_o + at * a.splits * D + lane * kPer;
-    float acc[kPer] = {};
-    for (int s = 0; s < count; ++s) {
-        const float ws = __shfl(w, s, kWave);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(ws, part[(size_t)s * D + e], acc[e]);
-    }
-    if constexpr (kPer == 2) reinterpret_cast<uint32_t*>(a.out + at * D)[lane] = f32x2_to_bf16x2_rne(acc[0], acc[1]);
-    else a.out[at * D + lane] = (uint16_t)f32x2_to_bf16x2_rne(acc[0], acc[0]);
-}
-
-template <int D, bool kTiles>
-__global__ __launch_bounds__(kJoinWaves* kWave) void attend_join_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const AttentionArgs a) {
     const int head = blockIdx.y * kJoinWaves + threadIdx.x / kWave;
-    const int r = kTiles ? request_of(a.c, blockIdx.x) : blockIdx.x;
+    const int r = request_of(a.c, blockIdx.x);
     if (r < 0 || head >= a.q_heads) return;   // whole waves
     bool bad;
     const Request rq = request(a.c, r, bad);
-    const int rows = rq.n * a.group;
-    if constexpr (kTiles) {
-        const int token = (int)blockIdx.x - rq.start;
-        if (token < rq.n && rows >= a.min_rows) join_row<D>(a, rq, head, token, a.tile_rows);   // (token >= n: q_start is bad)
-    } else if (rows <= a.max_rows) {
-        for (int token = 0; token < rq.n; ++token) join_row<D>(a, rq, head, token, kStreamRows);
-    }
+    const int token = (int)blockIdx.x - rq.start;
+    if (token >= rq.n || rq.n * a.group < a.min_rows) return;   // (token >= n: q_start is bad)
+    const int row0 = (token * a.group + head % a.group) / a.tile_rows * a.tile_rows;
+    const int count = shares(keys_of(rq, a.group, row0, a.tile_rows), a.chunk, a.most);
+    if (count == 1) return;
+    const size_t at = (size_t)blockIdx.x * a.q_heads + head;
+    join_row<D>(a, count, a.out + at * D, [&](long long i) { return (long long)at * a.most + i; });
 }
 
-// How a step is divided among blocks: which kernels run (both where requests of few rows and of many may come together) and how
-// the keys are shared.
+// How a step is divided among blocks, by what the host knows: which kernels run (both where requests of few rows and of many may come
+// together) and how they share the keys.
 struct Plan {
     bool stream, tiles;
-    int row_tiles;
-    int splits, most, tile_most;
-    int chunk, tile_chunk;
-    int stream_rows;   // requests of up to so many rows are the stream's
+    int stream_rows;            // requests of up to so many rows are the stream's
+    int shared, blocks, least;  // the stream's
+    int row_tiles, chunk, most; // the tiles'
 };
 constexpr int kMT = 1;
-int share_size(long long keys, long long count, int unit) { return (int)std::max<long long>((keys + count - 1) / count + unit - 1, unit) / unit * unit; }
 
 Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
     Plan p{};
     const int group = q_heads / c.heads, tile_rows = Tile<128, false, kMT>::kRows;
     const long long keys = std::max<long long>(1, std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size));   // at most 2^30
-    const long long most_rows = (long long)std::min(b.max_new, b.tokens) * group;
+    const long long most_rows = (long long)std::min(b.max_new, b.tokens) * group, cus = device_cu_count();
     p.stream = most_rows <= kStreamRows;
     p.tiles = !p.stream;
     if (p.tiles && b.requests > 1 && (long long)b.requests * b.max_new != b.tokens && group <= kStreamRows) p.stream = true;
     p.stream_rows = p.tiles ? (p.stream ? kStreamRows : 0) : INT32_MAX;
-    const long long cus = device_cu_count(), units = (long long)b.requests * c.heads;
-    long long s = 1, ts = 1;
-    if (p.stream) s = std::max(1ll, std::min({(3 * cus + units - 1) / units, 64ll, (keys + 255) / 256}));
+    if (p.stream) {
+        // Shared steps cost a join, about 4 us together with what the kernel does for it; a block for each request and head costs the time of the
+        // longest one, 1.6 us per step.  us, one / shared, uniform lengths: 32 units, 512 keys 8.9 / 10.9, 1024 keys 14.5 / 12, 16384 keys 224 / 49;
+        // 256 units, 2048 keys 31 / 33, 4096 keys 66 / 55; 512 units, 1024 keys 26 / 31, 8192 keys 192 / 203, but of 500 to 8000
+        // keys 153 / 128.
+        const long long units = (long long)b.requests * c.heads;
+        p.shared = keys > std::min(2048ll, 512 + 6 * units);
+        p.blocks = p.shared ? (int)cus * stream_blocks(c.head_dim) : (int)units;
+        p.least = 2;   // of 1, 2, 3 and 4 the best or next to it from 1024 to 16384 keys
+    }
     if (p.tiles) {
         p.row_tiles = (int)((long long)b.tokens * group / tile_rows) + b.requests;
         const long long work = std::max(1ll, (long long)b.tokens * group / tile_rows) * c.heads;
-        ts = std::max(1ll, std::min({(2 * cus + work - 1) / work, 64ll, (keys + 511) / 512}));
+        const long long n = std::max(1ll, std::min({(2 * cus + work - 1) / work, 64ll, (keys + 511) / 512}));
+        p.most = (int)n;
+        p.chunk = (int)((keys + n - 1) / n + kTileKeys - 1) / kTileKeys * kTileKeys;
     }
-    p.most = (int)s;
-    p.tile_most = (int)ts;
-    p.splits = std::max(p.most, p.tile_most);
-    p.chunk = share_size(keys, s, 128);
-    p.tile_chunk = share_size(keys, ts, kTileKeys);
     return p;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // More than 64 KB of LDS needs an opt-in; the call is idempotent, so two host threads that both find the flag clear may both make it.
-template <int D, bool kEight>
-hipError_t launch_tiles(const AttentionArgs& a, unsigned blocks, hipStream_t st) {
-    using T = Tile<D, kEight, kMT>;
+template <void (*kKernel)(AttentionArgs), int kLds>
+hipError_t launch_kernel(const AttentionArgs& a, long long blocks, int threads, hipStream_t st) {
     static std::atomic<bool> done{false};
-    if (T::kLds > 65536 && !done.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_tile_kernel<D, kEight, kMT>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
+    if (kLds > 60 * 1024 && !done.load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
         if (e != hipSuccess) return e;
         done.store(true, std::memory_order_release);
     }
-    hipLaunchKernelGGL((attend_tile_kernel<D, kEight, kMT>), dim3(blocks), dim3(kTileWaves * kWave), T::kLds, st, a);
+    hipLaunchKernelGGL(kKernel, dim3((unsigned)blocks), dim3(threads), kLds, st, a);
     return hipGetLastError();
+}
+
+template <int D, bool kEight>
+hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_requests& b, const AttentionArgs& a, hipStream_t st) {
+    const unsigned head_blocks = (unsigned)((a.q_heads + kJoinWaves - 1) / kJoinWaves);
+    if (p.tiles) {   // the longer kernel first
+        using T = Tile<D, kEight, kMT>;
+        const hipError_t e = launch_kernel<attend_tile_kernel<D, kEight, kMT>, T::kLds>(a, (long long)p.row_tiles * c.heads * p.most, kTileWaves * kWave, st);
+        if (e != hipSuccess) return e;
+        if (p.most > 1) hipLaunchKernelGGL(join_tiles_kernel<D>, dim3((unsigned)b.tokens, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+    }
+    if (p.stream) {   // (its partial results may lie where the tiles' were)
+        hipLaunchKernelGGL((attend_stream_kernel<D, kEight>), dim3((unsigned)p.blocks), dim3(kStreamWaves * kWave), 0, st, a);
+        if (p.shared) hipLaunchKernelGGL(join_stream_kernel<D>, dim3((unsigned)b.requests, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+// Partial results that a call may leave.
+size_t places(const Plan& p, const qail_requests& b, int q_heads) {
+    const size_t stream = p.stream && p.shared ? (size_t)2 * p.blocks * kStreamRows : 0, tiles = p.tiles && p.most > 1 ? (size_t)b.tokens * q_heads * p.most : 0;
+    return std::max(stream, tiles);
 }
 
 }  // namespace
 
 size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
-    const Plan p = plan_for(c, b, q_heads);
-    if (p.splits == 1) return 0;
-    const size_t rows = (size_t)b.tokens * q_heads * p.splits;
-    return align256(rows * c.head_dim * sizeof(float)) + align256(rows * sizeof(float2));
+    const size_t n = places(plan_for(c, b, q_heads), b, q_heads);
+    return align256(n * c.head_dim * sizeof(float)) + align256(n * sizeof(float2));
 }
 
 hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
@@ -640,42 +762,23 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
     a.q = q;
     a.out = out;
     a.part_o = static_cast<float*>(ws);
-    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256((size_t)b.tokens * q_heads * p.splits * c.head_dim * sizeof(float)));
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(places(p, b, q_heads) * c.head_dim * sizeof(float)));
     a.q_stride = q_stride;
     a.scale = scale * 1.44269504088896340736f;
     a.q_heads = q_heads;
     a.group = q_heads / c.heads;
-    a.splits = p.splits;
     a.max_rows = p.stream_rows;
-    a.min_rows = p.stream_rows + 1;
+    a.shared = p.shared;
+    a.blocks = p.blocks;
+    a.least = p.least;
+    a.min_rows = p.stream ? kStreamRows + 1 : 1;
     a.tiles = p.row_tiles;
     a.tile_rows = Tile<128, false, kMT>::kRows;
-    const bool eight = c.type == QAIL_KV_S8, wide = c.head_dim == 128;
-    const unsigned head_blocks = (unsigned)((q_heads + kJoinWaves - 1) / kJoinWaves);
-    if (p.tiles) {   // the longer kernel first
-        a.chunk = p.tile_chunk;
-        a.most = p.tile_most;
-        const unsigned blocks = (unsigned)((long long)p.row_tiles * c.heads * p.tile_most);
-        const hipError_t e = wide ? (eight ? launch_tiles<128, true>(a, blocks, st) : launch_tiles<128, false>(a, blocks, st))
-                                  : (eight ? launch_tiles<64, true>(a, blocks, st) : launch_tiles<64, false>(a, blocks, st));
-        if (e != hipSuccess) return e;
-        if (p.tile_most > 1) {
-            auto* const join = wide ? attend_join_kernel<128, true> : attend_join_kernel<64, true>;
-            hipLaunchKernelGGL(join, dim3((unsigned)b.tokens, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
-        }
-    }
-    if (p.stream) {
-        a.chunk = p.chunk;
-        a.most = p.most;
-        auto* const stream = wide ? (eight ? attend_stream_kernel<128, true> : attend_stream_kernel<128, false>)
-                                  : (eight ? attend_stream_kernel<64, true> : attend_stream_kernel<64, false>);
-        hipLaunchKernelGGL(stream, dim3((unsigned)((long long)b.requests * c.heads * p.most)), dim3(kStreamWaves * kWave), 0, st, a);
-        if (p.most > 1) {
-            auto* const join = wide ? attend_join_kernel<128, false> : attend_join_kernel<64, false>;
-            hipLaunchKernelGGL(join, dim3((unsigned)b.requests, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
-        }
-    }
-    return hipGetLastError();
+    a.chunk = p.chunk;
+    a.most = p.most;
+    const bool eight = c.type == QAIL_KV_S8;
+    if (c.head_dim == 128) return eight ? launch_step<128, true>(p, c, b, a, st) : launch_step<128, false>(p, c, b, a, st);
+    return eight ? launch_step<64, true>(p, c, b, a, st) : launch_step<64, false>(p, c, b, a, st);
 }
 
 }  // namespace qail

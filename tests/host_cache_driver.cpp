@@ -73,6 +73,37 @@ void walk(const Arrays& s, bool good) {
             for (int r = 0; r < a.requests; ++r) tiles += tiles_of(request(a, r, bad), group, 1, height);
             CHECK(!good || tiles <= (long long)s.tokens * group / height + a.requests, "%lld tiles of %d", tiles, height);
         }
+    for (int group : {1, 16, 24})   // the stream's steps: every one has one block, every part of a tile a place of its own
+        for (int max_rows : {16, INT_MAX})
+            for (int heads : {1, 3})
+                for (int least : {1, 3}) {
+                    const int blocks = 17;
+                    std::vector<Steps> of;
+                    long long total = 0;
+                    bool bad;
+                    for (int r = 0; r < a.requests; ++r) {
+                        const Request q = request(a, r, bad);
+                        of.push_back(steps_of(q, group, max_rows));
+                        CHECK((of[r].tiles == 0) == (q.n == 0 || q.n * group > max_rows), "request %d", r);
+                        CHECK(of[r].tiles * kStreamRows >= (of[r].tiles ? q.n * group : 0), "request %d", r);
+                        CHECK(of[r].tiles == 0 || (long long)of[r].steps * kStepKeys >= keys_of(q, group, 0, q.n * group), "request %d", r);
+                        total += (long long)of[r].tiles * of[r].steps * heads;
+                    }
+                    if (total > 100000) continue;
+                    const long long share = steps_of_a_share(total, blocks, least);
+                    CHECK(share * blocks >= total, "%lld steps, share %lld", total, share);
+                    std::vector<int> used(2 * blocks, 0);
+                    long long begin = 0;
+                    for (int r = 0; r < a.requests; ++r)
+                        for (int u = 0; u < of[r].tiles * heads; ++u, begin += of[r].steps) {
+                            const long long b0 = begin / share, b1 = (begin + of[r].steps - 1) / share;
+                            CHECK(b1 < blocks, "block %lld", b1);
+                            for (long long b = b0; b0 != b1 && b <= b1; ++b) {
+                                const long long at = place_of(begin, b, share);
+                                CHECK(at >= 0 && at < 2 * blocks && !used[at]++, "place %lld of block %lld", at, b);
+                            }
+                        }
+                }
     for (int r = 0; r < a.requests; ++r) {
         bool bad;
         const Request q = request(a, r, bad);
@@ -105,7 +136,7 @@ void walk(const Arrays& s, bool good) {
 int main() {
     std::mt19937 rng(7);
     auto pick = [&](int lo, int hi) { return (int)std::uniform_int_distribution<long long>(lo, hi)(rng); };
-    for (int round = 0; round < 3000; ++round) {
+    for (int round = 0; round < 1500; ++round) {
         Arrays s;
         const int R = pick(1, 6);
         s.page_shift = pick(4, 10);
