@@ -7,7 +7,6 @@
 //
 // Rows of one request and one head of the cache: row i is token i / group, head i % group, so grouped heads share every key that is loaded.
 #include <algorithm>
-#include <atomic>
 
 #include "kv_cache.h"
 
@@ -408,19 +407,22 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
 
 // ---------------------------------------------------------------------------- many rows: tiles on the matrix cores --
 //
-// A block takes kTileRows rows against 64 keys at a time, which its four waves stage in LDS together (bytes as bf16 codes; their steps beside
-// them) while they work on the tile before.  Bound by the matrix cores in principle: 4 D operations per score, against about five vector
-// instructions per score and the bytes of both operands from LDS.
-constexpr int kTileWaves = 4, kTileKeys = 64;
+// A block takes 128 rows, a wave 32 of them, against 64 keys at a time.  Both operands of the keys go through LDS, twice 64 keys: from memory
+// straight into it (bytes through registers, as bf16 codes, their steps beside them), while the waves work on the 64 keys before.
+// Bound by the vector unit next to the matrix cores: of 64 keys a wave has 32 products of 32 cycles each, and for every score a
+// multiply-add, an exponential and three halves of an instruction for the maximum, the sum (two rounded p at a time) and
+// the rounding.  So nothing else is left in the loop: places in LDS are registers and immediates (the loop has a copy for either half), places in memory
+// scalars, but for the last 64 keys.
+constexpr int kTileWaves = 4, kTileKeys = 64, kTileRows = kTileWaves * 32;
 
-template <int D, bool kEight, int kMT>
+template <int D, bool kEight>
 struct Tile {
-    static constexpr int kRows = kTileWaves * 32 * kMT;
     static constexpr int kRowBytes = 2 * D;                        // of LDS
     static constexpr int kPieces = kEight ? D / 16 : D / 8;        // 16-byte pieces of a row in memory
     static constexpr int kPass = kTileWaves * kWave / kPieces;     // rows that the block loads at once
     static constexpr int kLoads = kTileKeys / kPass;
-    static constexpr int kBuffer = 2 * kTileKeys * kRowBytes + (kEight ? 2 * kTileKeys * 4 : 0);   // K, V, their steps
+    static constexpr int kV = kTileKeys * kRowBytes, kSteps = 2 * kV;                 // K, V, their steps
+    static constexpr int kBuffer = 2 * kV + (kEight ? 2 * kTileKeys * 4 : 0);
     static constexpr int kLds = 2 * kBuffer;
 
     // Pieces of a row are exchanged so that what is read together lies in different banks: K by 16 rows and one piece, V by
@@ -436,63 +438,87 @@ __device__ __forceinline__ float max_of_halves(float x) {
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
-template <int D, bool kEight, int kMT>
-__global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_tile_kernel(const AttentionArgs a) {
-    using T = Tile<D, kEight, kMT>;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+constexpr int kVector = 0x002, kProducts = 0x008, kReads = 0x100;   // kinds of instructions, for the scheduler
+typedef __attribute__((address_space(3))) uint8_t lds_t;
+typedef __attribute__((address_space(1))) uint8_t global_t;
+
+// 16 bytes of each lane from memory into LDS, lane i's to to + 16 i.
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, lds_t* to) {
+#ifdef __HIP_DEVICE_COMPILE__   // (the host pass does not know the size)
+    __builtin_amdgcn_global_load_lds((const global_t*)from, to, 16, 0, 0);
+#endif
+}
+
+template <int D, bool kEight>
+__global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const AttentionArgs a) {
+    using T = Tile<D, kEight>;
+    __shared__ __attribute__((aligned(16))) uint8_t half0[T::kBuffer], half1[T::kBuffer];
+    lds_t* const lds0 = (lds_t*)half0;
+    lds_t* const lds1 = (lds_t*)half1;
     const int H = a.c.heads;
     const int h = blockIdx.x % H, split = blockIdx.x / H % a.most, tile = a.tiles - 1 - blockIdx.x / H / a.most;   // the longest first
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, col = lane % 32, half = lane / 32;
     int r, row0;
     if (blockIdx.x == 0) report_rows(a.c);
-    if (!tile_of(a.c, a.group, a.min_rows, T::kRows, tile, r, row0)) return;
+    if (!tile_of(a.c, a.group, a.min_rows, kTileRows, tile, r, row0)) return;
     bool bad;
     const Request rq = request(a.c, r, bad);
     if (bad && h == 0 && split == 0 && row0 == 0 && threadIdx.x == 0) report(a.c);
     const int rows = rq.n * a.group, before = rq.len - rq.n;
-    const int keys = keys_of(rq, a.group, row0, T::kRows), count = shares(keys, a.chunk, a.most);
+    const int keys = keys_of(rq, a.group, row0, kTileRows), count = shares(keys, a.chunk, a.most);
     if (split >= count) return;
     bad = false;   // from here on: a page
     const Range range = share_of(keys, a.chunk, count, split);
     const int k1 = range.end;
 
-    bf16x8_t q[kMT][D / 16];
-    int lim[kMT];
-    float m[kMT], l[kMT];
-    f32x16_t o[kMT][D / 32];
+    bf16x8_t q[D / 16];
+    f32x16_t o[D / 32];
+    const int row = row0 + wave * 32 + col, token = row / a.group;
+    const int lim = row < rows ? min(before + token, k1 - 1) : k1 - 1;   // the last key that the row sees; rows past the end are not stored
+    const int lim_first = __builtin_amdgcn_readfirstlane(lim), lim_last = __builtin_amdgcn_readlane(lim, 31);   // they ascend
+    {
+        const uint16_t* p = a.q + (rq.start + (row < rows ? token : 0)) * a.q_stride + (h * a.group + row % a.group) * D + 8 * half;
 #pragma unroll
-    for (int t = 0; t < kMT; ++t) {
-        const int row = row0 + (wave * kMT + t) * 32 + col, token = row / a.group, head = h * a.group + row % a.group;
-        lim[t] = row < rows ? min(before + token, k1 - 1) : k1 - 1;   // the last key that the row sees; rows past the end are not stored
-        const uint16_t* p = a.q + (rq.start + (row < rows ? token : 0)) * a.q_stride + head * D + 8 * half;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) q[t][s] = as_bf16x8(row < rows ? *reinterpret_cast<const u32x4_t*>(p + 16 * s) : u32x4_t{0u, 0u, 0u, 0u});
-        m[t] = -INFINITY;
-        l[t] = 0.f;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[t][d][e] = 0.f;
+        for (int s = 0; s < D / 16; ++s) q[s] = as_bf16x8(row < rows ? *reinterpret_cast<const u32x4_t*>(p + 16 * s) : u32x4_t{0u, 0u, 0u, 0u});
     }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
 
-    // Staging: the block's threads cover kPass rows at a time; 16 rows never lie in two pages.
-    const int piece = threadIdx.x % T::kPieces, row_in = threadIdx.x / T::kPieces, group_in = wave * (kWave / T::kPieces) / 16;
+    // From memory: the block's threads cover kPass rows at a time; 16 rows never lie in two pages, so that a wave's rows begin at a scalar place.
+    const int piece = threadIdx.x % T::kPieces, row_in = threadIdx.x / T::kPieces, group_in = wave * (kWave / T::kPieces) / 16 * 16;
     const int slots = 1 << a.c.page_shift;
-    u32x4_t kv[T::kLoads], vv[T::kLoads];
+    constexpr int kMemoryRow = T::kPieces * 16;
+    const int from_k = (kEight ? piece : T::swizzle_k(row_in, piece)) * 16, from_v = (kEight ? piece : T::swizzle_v(row_in, piece)) * 16;
+    u32x4_t kv[kEight ? T::kLoads : 1], vv[kEight ? T::kLoads : 1];
     float step;
-    int entry[T::kLoads], entry_s;   // of the page table, for the tile that is loaded next
+    int entry[T::kLoads], entry_s;   // of the page table, for the keys that are loaded next
     auto entries = [&](int kt) {
 #pragma unroll
-        for (int n = 0; n < T::kLoads; ++n) entry[n] = page_entry(a.c, r, min(kt + n * T::kPass + 16 * group_in, k1 - 1) >> a.c.page_shift);
+        for (int n = 0; n < T::kLoads; ++n) entry[n] = page_entry(a.c, r, min(kt + n * T::kPass + group_in, k1 - 1) >> a.c.page_shift);
         if constexpr (kEight) entry_s = page_entry(a.c, r, min(kt + (int)threadIdx.x % kTileKeys, k1 - 1) >> a.c.page_shift);
     };
-    auto load = [&](int kt) {
+    auto load = [&](int kt, lds_t* to) {
+        const bool whole = kt + kTileKeys <= k1;
 #pragma unroll
         for (int n = 0; n < T::kLoads; ++n) {
-            const size_t base = ((size_t)page_of(a.c, entry[n], bad) * H + h) << a.c.page_shift;
-            const size_t at = (base + (min(kt + n * T::kPass + row_in, k1 - 1) & (slots - 1))) * (T::kPieces * 16) + piece * 16;
-            kv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.k) + at);
-            vv[n] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.c.v) + at);
+            const size_t page = (size_t)(unsigned)__builtin_amdgcn_readfirstlane(page_of(a.c, entry[n], bad)) * H + h;
+            const int first = (kt + n * T::kPass + group_in) & (slots - 1);
+            // rows past the last key repeat it (its slot holds a token, which slots behind it need not) and are masked
+            const int slot = whole ? row_in % 16 : (min(kt + n * T::kPass + row_in, k1 - 1) & (slots - 1)) - first;
+            const size_t base = ((page << a.c.page_shift) + first) * kMemoryRow;
+            const uint8_t* const kp = static_cast<const uint8_t*>(a.c.k) + base + slot * kMemoryRow + from_k;
+            const uint8_t* const vp = static_cast<const uint8_t*>(a.c.v) + base + slot * kMemoryRow + from_v;
+            if constexpr (kEight) {
+                kv[n] = *reinterpret_cast<const u32x4_t*>(kp);
+                vv[n] = *reinterpret_cast<const u32x4_t*>(vp);
+            } else {
+                lds_t* const at = to + (n * T::kPass + wave * (kWave / T::kPieces)) * T::kRowBytes;   // of the wave; lane i's 16 bytes go to i * 16
+                load_to_lds(kp, at);
+                load_to_lds(vp, at + T::kV);
+            }
         }
         if constexpr (kEight) {
             if (threadIdx.x < 2 * kTileKeys) {   // threads 0 .. 63 a step of K each, 64 .. 127 of V
@@ -502,155 +528,176 @@ __global__ __launch_bounds__(kTileWaves* kWave, kMT == 1 ? 2 : 1) void attend_ti
             }
         }
     };
-    auto store = [&](int buffer) {
-        uint8_t* const kb = lds + buffer * T::kBuffer;
-        uint8_t* const vb = kb + kTileKeys * T::kRowBytes;
+    auto store = [&](lds_t* to) {   // what has been loaded is in LDS when the block's barrier is passed
+        if constexpr (kEight) {
 #pragma unroll
-        for (int n = 0; n < T::kLoads; ++n) {
-            const int row = n * T::kPass + row_in;
-            if constexpr (kEight) {
+            for (int n = 0; n < T::kLoads; ++n) {
+                const int at = n * T::kPass + row_in;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const bf16x8_t kc = i ? codes_to_bf16(kv[n].z, kv[n].w) : codes_to_bf16(kv[n].x, kv[n].y);
                     const bf16x8_t vc = i ? codes_to_bf16(vv[n].z, vv[n].w) : codes_to_bf16(vv[n].x, vv[n].y);
-                    *reinterpret_cast<bf16x8_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, 2 * piece + i) * 16) = kc;
-                    *reinterpret_cast<bf16x8_t*>(vb + row * T::kRowBytes + T::swizzle_v(row, 2 * piece + i) * 16) = vc;
+                    *(__attribute__((address_space(3))) bf16x8_t*)(to + at * T::kRowBytes + T::swizzle_k(at, 2 * piece + i) * 16) = kc;
+                    *(__attribute__((address_space(3))) bf16x8_t*)(to + T::kV + at * T::kRowBytes + T::swizzle_v(at, 2 * piece + i) * 16) = vc;
                 }
-            } else {
-                *reinterpret_cast<u32x4_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, piece) * 16) = kv[n];
-                *reinterpret_cast<u32x4_t*>(vb + row * T::kRowBytes + T::swizzle_v(row, piece) * 16) = vv[n];
             }
+            if (threadIdx.x < 2 * kTileKeys) ((__attribute__((address_space(3))) float*)(to + T::kSteps))[threadIdx.x] = step;
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
         }
-        if constexpr (kEight)
-            if (threadIdx.x < 2 * kTileKeys) reinterpret_cast<float*>(vb + kTileKeys * T::kRowBytes)[threadIdx.x] = step;
     };
 
-    int kt = range.begin, buffer = 0;
-    if (kt < k1) {
-        entries(kt);
-        load(kt);
-        entries(kt + kTileKeys);   // (the last key's beyond the end)
-        store(0);
+    // From LDS: K's row 32 u + col, piece 2 s + half; V's row 16 st + 8 j + 4 half + lane % 16 / 4, pieces 4 d + 2 (lane / 16 % 2) and the next.
+    int at_k[D / 16], at_v[D / 32];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) at_k[s] = col * T::kRowBytes + T::swizzle_k(col, 2 * s + half) * 16;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+        const int first = 4 * half + lane % 16 / 4;
+        at_v[d] = T::kV + first * T::kRowBytes + T::swizzle_v(first, 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2) * 16 + lane % 2 * 8;
     }
-    for (; kt < k1; kt += kTileKeys, buffer ^= 1) {
+    auto compute = [&](int kt, const lds_t* from) {
+        if (kt > lim_last) return;   // no row of the wave sees a key
+        f32x16_t sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                const bf16x8_t kf = *(const __attribute__((address_space(3))) bf16x8_t*)(from + at_k[s] + 32 * u * T::kRowBytes);
+                sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[s], sc[u], 0, 0, 0);
+            }
+        }
+        // six reads ahead of the products
+        __builtin_amdgcn_sched_group_barrier(kReads, 6, 0);
+#pragma unroll
+        for (int i = 0; i < D / 8 - 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, 6, 0);
+        // element e of half u is key kt + 32 u + 8 (e / 4) + 4 half + e % 4
+        const __attribute__((address_space(3))) f32x4_t* const steps = (const __attribute__((address_space(3))) f32x4_t*)(from + T::kSteps) + half;
+        if constexpr (kEight) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4_t k4 = steps[8 * u + e / 2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[u][e + i] *= k4[i];
+                }
+        }
+        if (kt + kTileKeys - 1 > lim_first) {
+            const int left = lim - kt - 4 * half;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (32 * u + 8 * (e / 4) + e % 4 > left) sc[u][e] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[u][e]);
+        top = max_of_halves(top);
+        // the maximum is followed only where it has grown by more than 2^8: p stays far from overflow, and a tile rarely rescales
+        if (__any((top - m) * a.scale > 8.f)) {
+            const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] *= alpha;
+        }
+        const float off = m == -INFINITY ? 0.f : m * a.scale;
+        bf16x8_t pf[4];
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = 8 * (st % 2) + 2 * e;
+                float x = __builtin_amdgcn_exp2f(fmaf(sc[st / 2][at], a.scale, -off)), y = __builtin_amdgcn_exp2f(fmaf(sc[st / 2][at + 1], a.scale, -off));
+                if constexpr (kEight) {
+                    l += x + y;
+                    const f32x4_t v4 = steps[kTileKeys / 4 + 8 * (st / 2) + at / 4 * 2];
+                    x *= v4[at % 4];
+                    y *= v4[at % 4 + 1];
+                }
+                w[e] = f32x2_to_bf16x2_rne(x, y);
+                if constexpr (!kEight) {
+                    const uint32_t ones = 0x3F803F80u;
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[e]), __builtin_bit_cast(bf16x2_t, ones), l, false);
+                }
+            }
+            pf[st] = as_bf16x8(u32x4_t{w[0], w[1], w[2], w[3]});
+        }
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                const lds_t* const at = from + at_v[d] + 16 * st * T::kRowBytes;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(at + 8 * T::kRowBytes));
+                const s16x8_t both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[st], o[d], 0, 0, 0);
+            }
+        // the exponentials of the next 16 keys between the products of these
+        constexpr int kAhead = D / 32, kBetween = (kEight ? 40 : 28) / kAhead;
+        __builtin_amdgcn_sched_group_barrier(kReads, 2 * kAhead, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, kAhead * kBetween, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+            if (i < 3 * kAhead) {
+                __builtin_amdgcn_sched_group_barrier(kReads, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kVector, kBetween, 0);
+            }
+        }
+    };
+    auto turn = [&](int kt, lds_t* mine, lds_t* next) {
         __syncthreads();
         const bool more = kt + kTileKeys < k1;
         if (more) {
-            load(kt + kTileKeys);
+            load(kt + kTileKeys, next);
             entries(kt + 2 * kTileKeys);
         }
-        const uint8_t* const kb = lds + buffer * T::kBuffer;
-        const uint8_t* const vb = kb + kTileKeys * T::kRowBytes;
-        const float* const steps = reinterpret_cast<const float*>(vb + kTileKeys * T::kRowBytes);
-        if (kt <= __builtin_amdgcn_readlane(lim[kMT - 1], 31)) {   // some row of the wave sees a key of the tile
-            f32x16_t sc[kMT][2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                for (int t = 0; t < kMT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sc[t][u][e] = 0.f;
-#pragma unroll
-                for (int s = 0; s < D / 16; ++s) {
-                    const int row = 32 * u + col;
-                    const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(kb + row * T::kRowBytes + T::swizzle_k(row, 2 * s + half) * 16);
-#pragma unroll
-                    for (int t = 0; t < kMT; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[t][s], sc[t][u], 0, 0, 0);
-                }
-            }
-            bf16x8_t pf[kMT][4];
-#pragma unroll
-            for (int t = 0; t < kMT; ++t) {
-                // element e of half u is key kt + 32 u + 8 (e / 4) + 4 half + e % 4
-                if constexpr (kEight) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) sc[t][u][e] *= steps[32 * u + 8 * (e / 4) + 4 * half + e % 4];
-                }
-                if (kt + kTileKeys - 1 > __builtin_amdgcn_readfirstlane(lim[t])) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (kt + 32 * u + 8 * (e / 4) + 4 * half + e % 4 > lim[t]) sc[t][u][e] = -INFINITY;
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][u][e]);
-                top = max_of_halves(top);
-                // the maximum is followed only where it has grown by more than 2^8: p stays far from overflow, and a tile rarely rescales
-                if (__any((top - m[t]) * a.scale > 8.f)) {
-                    const float m_new = fmaxf(m[t], top), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[t] - m_new) * a.scale);
-                    m[t] = m_new;
-                    l[t] *= alpha;
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d) o[t][d] *= alpha;
-                }
-                const float off = m[t] == -INFINITY ? 0.f : m[t] * a.scale;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        sc[t][u][e] = __builtin_amdgcn_exp2f(fmaf(sc[t][u][e], a.scale, -off));
-                        l[t] += sc[t][u][e];
-                        if constexpr (kEight) sc[t][u][e] *= steps[kTileKeys + 32 * u + 8 * (e / 4) + 4 * half + e % 4];
-                    }
-#pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = f32x2_to_bf16x2_rne(sc[t][st / 2][8 * (st % 2) + 2 * e], sc[t][st / 2][8 * (st % 2) + 2 * e + 1]);
-                    pf[t][st] = as_bf16x8(u32x4_t{w[0], w[1], w[2], w[3]});
-                }
-            }
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) {
-                    s16x4_t part[2];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int row = 16 * st + 8 * j + 4 * half + lane % 16 / 4;
-                        const int piece_v = 4 * d + 2 * (lane / 16 % 2) + lane % 4 / 2;
-                        part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(
-                            vb + row * T::kRowBytes + T::swizzle_v(row, piece_v) * 16 + lane % 2 * 8));
-                    }
-                    const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, both);
-#pragma unroll
-                    for (int t = 0; t < kMT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][st], o[t][d], 0, 0, 0);
-                }
+        compute(kt, mine);
+        if (more) store(next);
+    };
+    if (range.begin < k1) {
+        entries(range.begin);
+        load(range.begin, lds0);
+        entries(range.begin + kTileKeys);   // (the last key's beyond the end)
+        store(lds0);
+        for (int kt = range.begin; kt < k1; kt += 2 * kTileKeys) {
+            turn(kt, lds0, lds1);
+            if (kt + kTileKeys < k1) turn(kt + kTileKeys, lds1, lds0);
         }
-        if (more) store(buffer ^ 1);
     }
     if (bad) report(a.c);
 
+    const float sum = l + __shfl_xor(l, 32, kWave);
+    if (row >= rows) return;
+    const size_t at = (size_t)(rq.start + token) * a.q_heads + h * a.group + row % a.group;
+    if (count == 1) {
+        const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
 #pragma unroll
-    for (int t = 0; t < kMT; ++t) {
-        const float sum = l[t] + __shfl_xor(l[t], 32, kWave);
-        const int row = row0 + (wave * kMT + t) * 32 + col;
-        if (row >= rows) continue;
-        const size_t at = (size_t)(rq.start + row / a.group) * a.q_heads + h * a.group + row % a.group;
-        if (count == 1) {
-            const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
+        for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
+                    uint2{f32x2_to_bf16x2_rne(o[d][e] * inv, o[d][e + 1] * inv), f32x2_to_bf16x2_rne(o[d][e + 2] * inv, o[d][e + 3] * inv)};
+    } else {
+        float* out = a.part_o + (at * a.most + split) * D;
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
-                        uint2{f32x2_to_bf16x2_rne(o[t][d][e] * inv, o[t][d][e + 1] * inv), f32x2_to_bf16x2_rne(o[t][d][e + 2] * inv, o[t][d][e + 3] * inv)};
-        } else {
-            float* out = a.part_o + (at * a.most + split) * D;
+        for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[t][d][e], o[t][d][e + 1], o[t][d][e + 2], o[t][d][e + 3]);
-            if (half == 0) a.part_ml[at * a.most + split] = make_float2(m[t], sum);
-        }
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
+        if (half == 0) a.part_ml[at * a.most + split] = make_float2(m, sum);
     }
 }
 
@@ -679,11 +726,10 @@ struct Plan {
     int shared, blocks, least;  // the stream's
     int row_tiles, chunk, most; // the tiles'
 };
-constexpr int kMT = 1;
 
 Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
     Plan p{};
-    const int group = q_heads / c.heads, tile_rows = Tile<128, false, kMT>::kRows;
+    const int group = q_heads / c.heads, tile_rows = kTileRows;
     const long long keys = std::max<long long>(1, std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size));   // at most 2^30
     const long long most_rows = (long long)std::min(b.max_new, b.tokens) * group, cus = device_cu_count();
     p.stream = most_rows <= kStreamRows;
@@ -712,26 +758,11 @@ Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// More than 64 KB of LDS needs an opt-in; the call is idempotent, so two host threads that both find the flag clear may both make it.
-template <void (*kKernel)(AttentionArgs), int kLds>
-hipError_t launch_kernel(const AttentionArgs& a, long long blocks, int threads, hipStream_t st) {
-    static std::atomic<bool> done{false};
-    if (kLds > 60 * 1024 && !done.load(std::memory_order_acquire)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-        if (e != hipSuccess) return e;
-        done.store(true, std::memory_order_release);
-    }
-    hipLaunchKernelGGL(kKernel, dim3((unsigned)blocks), dim3(threads), kLds, st, a);
-    return hipGetLastError();
-}
-
 template <int D, bool kEight>
 hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_requests& b, const AttentionArgs& a, hipStream_t st) {
     const unsigned head_blocks = (unsigned)((a.q_heads + kJoinWaves - 1) / kJoinWaves);
     if (p.tiles) {   // the longer kernel first
-        using T = Tile<D, kEight, kMT>;
-        const hipError_t e = launch_kernel<attend_tile_kernel<D, kEight, kMT>, T::kLds>(a, (long long)p.row_tiles * c.heads * p.most, kTileWaves * kWave, st);
-        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((attend_tile_kernel<D, kEight>), dim3((unsigned)((long long)p.row_tiles * c.heads * p.most)), dim3(kTileWaves * kWave), 0, st, a);
         if (p.most > 1) hipLaunchKernelGGL(join_tiles_kernel<D>, dim3((unsigned)b.tokens, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
     }
     if (p.stream) {   // (its partial results may lie where the tiles' were)
@@ -773,7 +804,7 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
     a.least = p.least;
     a.min_rows = p.stream ? kStreamRows + 1 : 1;
     a.tiles = p.row_tiles;
-    a.tile_rows = Tile<128, false, kMT>::kRows;
+    a.tile_rows = kTileRows;
     a.chunk = p.chunk;
     a.most = p.most;
     const bool eight = c.type == QAIL_KV_S8;
