@@ -93,11 +93,12 @@ __host__ __device__ __forceinline__ long long steps_of_a_share(long long total, 
 __host__ __device__ __forceinline__ long long place_of(long long begin, long long b, long long share) { return 2 * b + (begin >= b * share ? 1 : 0); }
 
 // The request and the first row of tile `tile` of all of them, counted in the order of the requests; false past the last one.
-__device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_rows, int height, int tile, int& r, int& row0) {
+__device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_rows, int height, int tile, int& r, int& row0, Request& q, bool& bad) {
     const int lane = threadIdx.x % kWave;
     for (int r0 = 0; r0 < a.requests; r0 += kWave) {
-        bool bad;
-        const int mine = r0 + lane < a.requests ? tiles_of(request(a, r0 + lane, bad), group, min_rows, height) : 0;
+        bool bad_here = false;
+        const Request here = r0 + lane < a.requests ? request(a, r0 + lane, bad_here) : Request{0, 0, 0};
+        const int mine = tiles_of(here, group, min_rows, height);
         int sum = mine;   // of this lane's request and those before it
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) {
@@ -109,6 +110,8 @@ __device__ __forceinline__ bool tile_of(const CacheArgs& a, int group, int min_r
             const int at = __builtin_ctzll(past);
             r = r0 + at;
             row0 = (tile - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at))) * height;
+            q = Request{__builtin_amdgcn_readlane(here.start, at), __builtin_amdgcn_readlane(here.n, at), __builtin_amdgcn_readlane(here.len, at)};
+            bad = (__ballot(bad_here) >> at) & 1;
             return true;
         }
         tile -= __builtin_amdgcn_readlane(sum, kWave - 1);

@@ -30,8 +30,8 @@ struct AttentionArgs {
     int q_heads, group;
     // stream: requests of at most max_rows rows; all steps shared by `blocks` blocks, `least` of them each, or a block for each request and head
     int max_rows, shared, blocks, least;
-    // tiles: requests of at least min_rows rows in at most `tiles` tiles of tile_rows; their keys in shares of `chunk`, at most `most`
-    int min_rows, tiles, tile_rows, chunk, most;
+    // tiles: requests of at least min_rows rows, in at most `tiles` tiles; the keys of a tile in shares of `chunk`, at most `most`
+    int min_rows, tiles, chunk, most;
 };
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(const u32x4_t& v) { return __builtin_bit_cast(bf16x8_t, v); }
@@ -456,13 +456,13 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
     lds_t* const lds0 = (lds_t*)half0;
     lds_t* const lds1 = (lds_t*)half1;
     const int H = a.c.heads;
-    const int h = blockIdx.x % H, split = blockIdx.x / H % a.most, tile = a.tiles - 1 - blockIdx.x / H / a.most;   // the longest first
+    const int h = blockIdx.x % H, split = blockIdx.x / H % a.most, tile = a.tiles - 1 - blockIdx.x / H / a.most;   // a request's longest first
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, col = lane % 32, half = lane / 32;
     int r, row0;
     if (blockIdx.x == 0) report_rows(a.c);
-    if (!tile_of(a.c, a.group, a.min_rows, kTileRows, tile, r, row0)) return;
     bool bad;
-    const Request rq = request(a.c, r, bad);
+    Request rq;
+    if (!tile_of(a.c, a.group, a.min_rows, kTileRows, tile, r, row0, rq, bad)) return;
     if (bad && h == 0 && split == 0 && row0 == 0 && threadIdx.x == 0) report(a.c);
     const int rows = rq.n * a.group, before = rq.len - rq.n;
     const int keys = keys_of(rq, a.group, row0, kTileRows), count = shares(keys, a.chunk, a.most);
@@ -701,21 +701,42 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
     }
 }
 
-// Adds up the shares of the keys of a tile of rows: a block has four heads of a token, a wave each.
+// Adds up the shares of the keys of a tile of rows: D / 4 lanes a row, a block the heads of a token.
 template <int D>
 __global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const AttentionArgs a) {
-    const int head = blockIdx.y * kJoinWaves + threadIdx.x / kWave;
-    const int r = request_of(a.c, blockIdx.x);
-    if (r < 0 || head >= a.q_heads) return;   // whole waves
+    constexpr int kLanes = D / 4;
+    const int r = request_of(a.c, blockIdx.x), head = blockIdx.y * (kJoinWaves * kWave / kLanes) + threadIdx.x / kLanes;
+    if (r < 0 || head >= a.q_heads) return;
     bool bad;
     const Request rq = request(a.c, r, bad);
     const int token = (int)blockIdx.x - rq.start;
     if (token >= rq.n || rq.n * a.group < a.min_rows) return;   // (token >= n: q_start is bad)
-    const int row0 = (token * a.group + head % a.group) / a.tile_rows * a.tile_rows;
-    const int count = shares(keys_of(rq, a.group, row0, a.tile_rows), a.chunk, a.most);
+    const int row0 = (token * a.group + head % a.group) / kTileRows * kTileRows;
+    const int count = shares(keys_of(rq, a.group, row0, kTileRows), a.chunk, a.most);
     if (count == 1) return;
     const size_t at = (size_t)blockIdx.x * a.q_heads + head;
-    join_row<D>(a, count, a.out + at * D, [&](long long i) { return (long long)at * a.most + i; });
+    const float2* ml = a.part_ml + at * a.most;
+    const f32x4_t* part = reinterpret_cast<const f32x4_t*>(a.part_o + at * a.most * D) + threadIdx.x % kLanes;
+    float top = -INFINITY;
+    for (int i = 0; i < count; ++i) top = fmaxf(top, ml[i].x);
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int i0 = 0; i0 < count; i0 += 4) {
+        f32x4_t v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = part[min(i0 + u, count - 1) * kLanes];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float2 x = ml[min(i0 + u, count - 1)];
+            if (i0 + u >= count || x.x == -INFINITY) continue;   // (no key: a sum of 0)
+            const float w = __builtin_amdgcn_exp2f((x.x - top) * a.scale);
+            sum = fmaf(w, x.y, sum);
+            acc += v[u] * w;
+        }
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;
+    reinterpret_cast<uint2*>(a.out + at * D)[threadIdx.x % kLanes] =
+        uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }
 
 // How a step is divided among blocks, by what the host knows: which kernels run (both where requests of few rows and of many may come
@@ -763,7 +784,7 @@ hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_request
     const unsigned head_blocks = (unsigned)((a.q_heads + kJoinWaves - 1) / kJoinWaves);
     if (p.tiles) {   // the longer kernel first
         hipLaunchKernelGGL((attend_tile_kernel<D, kEight>), dim3((unsigned)((long long)p.row_tiles * c.heads * p.most)), dim3(kTileWaves * kWave), 0, st, a);
-        if (p.most > 1) hipLaunchKernelGGL(join_tiles_kernel<D>, dim3((unsigned)b.tokens, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+        if (p.most > 1) hipLaunchKernelGGL(join_tiles_kernel<D>, dim3((unsigned)b.tokens, (unsigned)((a.q_heads * (D / 4) + kJoinWaves * kWave - 1) / (kJoinWaves * kWave))), dim3(kJoinWaves * kWave), 0, st, a);
     }
     if (p.stream) {   // (its partial results may lie where the tiles' were)
         hipLaunchKernelGGL((attend_stream_kernel<D, kEight>), dim3((unsigned)p.blocks), dim3(kStreamWaves * kWave), 0, st, a);
@@ -804,7 +825,6 @@ hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b
     a.least = p.least;
     a.min_rows = p.stream ? kStreamRows + 1 : 1;
     a.tiles = p.row_tiles;
-    a.tile_rows = kTileRows;
     a.chunk = p.chunk;
     a.most = p.most;
     const bool eight = c.type == QAIL_KV_S8;
