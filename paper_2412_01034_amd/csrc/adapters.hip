@@ -11,8 +11,10 @@ namespace qail {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
 constexpr int kMaxItems = 8;    // linears that share the two launches
-constexpr int kMaxSplits = 8;   // shares of K
+constexpr int kMaxSplits = 4;   // shares of K
 constexpr int kDownWaves = 8, kUpWaves = 4;
 
 struct AdapterItem {
@@ -42,46 +44,55 @@ __device__ __forceinline__ void each_adapter(const AdapterArgs& a, const Adapter
     }
 }
 
+// A block takes 16 rows of x, all of the rank (kTiles tiles of 16) and a share of K, of which each wave has a piece of its own: whole lines of memory, so
+// that none is read by two compute units.
+template <int kTiles>
 __global__ __launch_bounds__(kDownWaves* kWave) void adapters_down_kernel(const AdapterArgs a) {
-    __shared__ f32x4_t red[kDownWaves][kWave];
-    const int item = blockIdx.z, slot = blockIdx.y;
-    const AdapterItem& it = a.it[item];
-    const int tiles_j = (it.r + 15) / 16;
-    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
-    const int j0 = tile % 4 * 16, m0 = tile / 4 * 16;   // four tiles of j for every item: a rank of 64
-    if (j0 / 16 >= tiles_j) return;
+    __shared__ f32x4_t red[kDownWaves][kTiles][kWave];
+    const AdapterItem& it = a.it[blockIdx.z];
+    const int split = blockIdx.x % a.splits, m0 = blockIdx.x / a.splits * 16;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane % 16, g = lane / 16;
     const int K = it.K, r = it.r, M = a.M;
-    const uint16_t* xr = it.x + (size_t)min(m0 + col, M - 1) * K + 8 * g;
-    each_adapter(a, it, m0, slot, [&](int of, bool mine) {
-        const uint16_t* ar = it.A + ((size_t)of * r + min(j0 + col, r - 1)) * K + 8 * g;
+    const int pieces = a.splits * kDownWaves, piece = (((K + 31) / 32 + pieces - 1) / pieces + 1) / 2 * 64;   // of K; a multiple of a line
+    const int k0 = (split * kDownWaves + wave) * piece, k1 = min(k0 + piece, K);
+    const uint16_t* xr = it.x + (size_t)min(m0 + col, M - 1) * K;
+    each_adapter(a, it, m0, blockIdx.y, [&](int of, bool mine) {
+        const uint16_t* ar[kTiles];
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) ar[j] = it.A + ((size_t)of * r + min(16 * j + col, r - 1)) * K;   // rows past the rank are not stored
         constexpr int kAhead = 4;
-        const int round = 32 * kDownWaves * a.splits;
-        f32x4_t part[kAhead];
+        f32x4_t part[kTiles][2];   // two chains
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) part[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int kb = (wave * a.splits + split) * 32; kb < K; kb += kAhead * round) {
-            uint4 xv[kAhead], av[kAhead];
+        for (int j = 0; j < kTiles; ++j) part[j][0] = part[j][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int kb = k0; kb < k1; kb += 32 * kAhead) {
+            u32x4_t xv[kAhead], av[kAhead][kTiles];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {   // past the end of K element 0 is read again and counts as 0
-                const bool in = kb + u * round + 8 * g < K;
-                xv[u] = *reinterpret_cast<const uint4*>(xr + (in ? kb + u * round : -8 * g));
-                av[u] = *reinterpret_cast<const uint4*>(ar + (in ? kb + u * round : -8 * g));
+            for (int u = 0; u < kAhead; ++u) {   // past the end element 0 is read again and counts as 0
+                const int k = kb + 32 * u + 8 * g, at = k < k1 ? k : 0;
+                xv[u] = *reinterpret_cast<const u32x4_t*>(xr + at);
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) av[u][j] = *reinterpret_cast<const u32x4_t*>(ar[j] + at);
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (kb + u * round + 8 * g >= K) xv[u] = av[u] = uint4{0u, 0u, 0u, 0u};
-                part[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, av[u]), __builtin_bit_cast(bf16x8_t, xv[u]), part[u], 0, 0, 0);
+                const bool in = kb + 32 * u + 8 * g < k1;
+                const bf16x8_t x = __builtin_bit_cast(bf16x8_t, in ? xv[u] : u32x4_t{0u, 0u, 0u, 0u});
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+                    part[j][u % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, in ? av[u][j] : u32x4_t{0u, 0u, 0u, 0u}), x,
+                                                                             part[j][u % 2], 0, 0, 0);
             }
         }
         __syncthreads();   // the sums of the adapter before have been read
-        red[wave][lane] = (part[0] + part[1]) + (part[2] + part[3]);
-        __syncthreads();
-        if (wave == 0 && mine) {   // (mine: the row exists)
-            f32x4_t sum = red[0][lane];
 #pragma unroll
-            for (int w = 1; w < kDownWaves; ++w) sum += red[w][lane];
-            if (j0 + 4 * g < r) *reinterpret_cast<f32x4_t*>(it.t + ((size_t)split * M + m0 + col) * r + j0 + 4 * g) = sum;   // r % 8 == 0
+        for (int j = 0; j < kTiles; ++j) red[wave][j][lane] = part[j][0] + part[j][1];
+        __syncthreads();
+        if (wave < kTiles && mine) {   // (mine: the row exists)
+            f32x4_t sum = red[0][wave][lane];
+#pragma unroll
+            for (int w = 1; w < kDownWaves; ++w) sum += red[w][wave][lane];
+            const int j = 16 * wave + 4 * g;
+            if (j < r) *reinterpret_cast<f32x4_t*>(it.t + ((size_t)split * M + m0 + col) * r + j) = sum;   // r % 8 == 0
         }
     });
 }
@@ -92,57 +103,68 @@ template <bool kWide>   // N % 8 == 0: rows of y are 16-byte aligned
 __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& it, int m0, int n0, int slot) {
     const int lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
     const int N = it.N, r = it.r, M = a.M, m = m0 + col;
+    const int n = n0 + 16 * g;
+    uint16_t* const y = it.y + (size_t)min(m, M - 1) * N + n;
     each_adapter(a, it, m0, slot, [&](int of, bool mine) {
+        const float scaling = it.scaling[of];
+        u32x4_t old[2];
+        if (kWide && mine) {   // on its way while the products are formed
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                if (n + 8 * half < N) old[half] = reinterpret_cast<u32x4_t*>(y)[half];
+        }
         f32x4_t acc[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         for (int j0 = 0; j0 < r; j0 += 32) {
             const bool in = j0 + 8 * g < r;
-            uint4 bv[4];
+            u32x4_t bv[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int n = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
-                bv[t] = in ? *reinterpret_cast<const uint4*>(it.B + ((size_t)of * N + n) * r + j0 + 8 * g) : uint4{0u, 0u, 0u, 0u};
+                const int row = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
+                bv[t] = in ? *reinterpret_cast<const u32x4_t*>(it.B + ((size_t)of * N + row) * r + j0 + 8 * g) : u32x4_t{0u, 0u, 0u, 0u};
             }
-            float s[8] = {};
-            if (in && mine)
-                for (int k = 0; k < a.splits; ++k) {
-                    const float4* p = reinterpret_cast<const float4*>(it.t + ((size_t)k * M + m) * r + j0 + 8 * g);
-                    const float4 lo = p[0], hi = p[1];
-                    s[0] += lo.x; s[1] += lo.y; s[2] += lo.z; s[3] += lo.w;
-                    s[4] += hi.x; s[5] += hi.y; s[6] += hi.z; s[7] += hi.w;
-                }
+            f32x4_t tl[kMaxSplits][2];
+#pragma unroll
+            for (int k = 0; k < kMaxSplits; ++k) {
+                const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4_t* p = reinterpret_cast<const f32x4_t*>(it.t + ((size_t)k * M + m) * r + j0 + 8 * g);
+                const bool have = in && mine && k < a.splits;
+                tl[k][0] = have ? p[0] : zero;
+                tl[k][1] = have ? p[1] : zero;
+            }
+            float s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = (tl[0][e / 4][e % 4] + tl[1][e / 4][e % 4]) + (tl[2][e / 4][e % 4] + tl[3][e / 4][e % 4]);
+            static_assert(kMaxSplits == 4, "four parts are added up");
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 hi[e] = f32x2_to_bf16x2_rne(s[2 * e], s[2 * e + 1]);
                 lo[e] = f32x2_to_bf16x2_rne(s[2 * e] - __builtin_bit_cast(float, hi[e] << 16), s[2 * e + 1] - __builtin_bit_cast(float, hi[e] & 0xFFFF0000u));
             }
-            const bf16x8_t th = __builtin_bit_cast(bf16x8_t, uint4{hi[0], hi[1], hi[2], hi[3]}), tl = __builtin_bit_cast(bf16x8_t, uint4{lo[0], lo[1], lo[2], lo[3]});
+            const bf16x8_t th = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]}), tr = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const bf16x8_t b = __builtin_bit_cast(bf16x8_t, bv[t]);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tl, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tr, acc[t], 0, 0, 0);
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, th, acc[t], 0, 0, 0);
             }
         }
-        const int n = n0 + 16 * g;
         if (!mine || n >= N) return;
-        const float scaling = it.scaling[of];
-        uint16_t* y = it.y + (size_t)m * N + n;
         if (kWide) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 if (n + 8 * half >= N) break;
-                uint4 v = reinterpret_cast<uint4*>(y)[half];
-                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                u32x4_t w = old[half];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const f32x4_t& d = acc[2 * half + e / 2];
-                    w[e] = f32x2_to_bf16x2_rne(fmaf(scaling, d[e % 2 * 2], __builtin_bit_cast(float, w[e] << 16)),
-                                               fmaf(scaling, d[e % 2 * 2 + 1], __builtin_bit_cast(float, w[e] & 0xFFFF0000u)));
+                    const uint32_t was = w[e];
+                    w[e] = f32x2_to_bf16x2_rne(fmaf(scaling, d[e % 2 * 2], __builtin_bit_cast(float, was << 16)),
+                                               fmaf(scaling, d[e % 2 * 2 + 1], __builtin_bit_cast(float, was & 0xFFFF0000u)));
                 }
-                reinterpret_cast<uint4*>(y)[half] = uint4{w[0], w[1], w[2], w[3]};
+                reinterpret_cast<u32x4_t*>(y)[half] = w;
             }
         } else {
 #pragma unroll
@@ -163,8 +185,7 @@ __global__ __launch_bounds__(kUpWaves* kWave) void adapters_up_kernel(const Adap
 
 // Shares of K: more where the tiles alone leave the chip empty.
 int k_splits(int M, int count) {
-    const long long blocks = 2ll * ((M + 15) / 16) * count;   // of a rank of 32
-    const long long s = device_cu_count() / blocks;
+    const long long blocks = (long long)((M + 15) / 16) * count, s = device_cu_count() / blocks;
     return s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : (int)s;
 }
 
@@ -187,7 +208,7 @@ hipError_t in_groups(const qail_w4a16_item* items, const qail_adapters* ad, cons
     for (int i0 = 0; i0 < count; i0 += kMaxItems) {
         const int c = count - i0 < kMaxItems ? count - i0 : kMaxItems;
         AdapterArgs a{};
-        int widest = 0, most = 1;
+        int widest = 0, most = 1, rank = 0;
         a.rows = rows;
         a.M = M;
         a.splits = k_splits(M, c);
@@ -198,11 +219,12 @@ hipError_t in_groups(const qail_w4a16_item* items, const qail_adapters* ad, cons
             t += (size_t)a.splits * M * l.r;
             widest = s.d.N > widest ? s.d.N : widest;
             most = l.n > most ? l.n : most;
+            rank = l.r > rank ? l.r : rank;
         }
         const int in_tile = M < 16 ? M : 16;   // distinct adapters of a tile, at most
         a.slots = most < in_tile ? most : in_tile;
         if (M > 64) a.slots = 1;
-        launch(a, c, widest);
+        launch(a, c, widest, (rank + 15) / 16);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -212,13 +234,14 @@ hipError_t in_groups(const qail_w4a16_item* items, const qail_adapters* ad, cons
 }  // namespace
 
 hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st) {
-    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int) {
-        hipLaunchKernelGGL(adapters_down_kernel, dim3((M + 15) / 16 * 4 * a.splits, a.slots, c), dim3(kDownWaves * kWave), 0, st, a);
+    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int, int tiles) {
+        auto* const kernel = tiles == 1 ? adapters_down_kernel<1> : tiles == 2 ? adapters_down_kernel<2> : tiles == 3 ? adapters_down_kernel<3> : adapters_down_kernel<4>;
+        hipLaunchKernelGGL(kernel, dim3((M + 15) / 16 * a.splits, a.slots, c), dim3(kDownWaves * kWave), 0, st, a);
     });
 }
 
 hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st) {
-    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int widest) {
+    return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int widest, int) {
         hipLaunchKernelGGL(adapters_up_kernel, dim3((M + 15) / 16 * ((widest + 64 * kUpWaves - 1) / (64 * kUpWaves)), a.slots, c), dim3(kUpWaves * kWave), 0, st, a);
     });
 }

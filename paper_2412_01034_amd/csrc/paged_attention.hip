@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kStreamWaves* kWave, stream_blocks(D)) void attend_
     if (blockIdx.x == 0) report_rows(a.c);
 }
 
-// Adds up what the stream's blocks have left: a wave per output row, which walks through the request's tokens.
+// Adds up what the stream's blocks have left: a wave per output row.
 constexpr int kJoinWaves = 4;
 
 // The sum of `count` partial results, the i-th in place(i), as bf16 to `out`.
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
     const Request rq = request(a.c, r, bad);
     const Steps s = steps_of(rq, a.group, a.max_rows);
     if (s.tiles == 0) return;
-    for (int token = 0; token < rq.n; ++token) {
+    for (int token = blockIdx.z; token < rq.n; token += gridDim.z) {
         const int row = token * a.group + head % a.group;
         const long long begin = first + ((long long)(head / a.group) * s.tiles + row / kStreamRows) * s.steps;
         const long long b0 = begin / share, count = (begin + s.steps - 1) / share - b0 + 1;
@@ -745,6 +745,7 @@ struct Plan {
     bool stream, tiles;
     int stream_rows;            // requests of up to so many rows are the stream's
     int shared, blocks, least;  // the stream's
+    unsigned join_tokens;
     int row_tiles, chunk, most; // the tiles'
 };
 
@@ -765,6 +766,7 @@ Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
         const long long units = (long long)b.requests * c.heads;
         p.shared = keys > std::min(2048ll, 512 + 6 * units);
         p.blocks = p.shared ? (int)cus * stream_blocks(c.head_dim) : (int)units;
+        p.join_tokens = (unsigned)std::max(1, std::min({b.max_new, b.tokens, kStreamRows}));
         p.least = 2;   // of 1, 2, 3 and 4 the best or next to it from 1024 to 16384 keys
     }
     if (p.tiles) {
@@ -788,7 +790,7 @@ hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_request
     }
     if (p.stream) {   // (its partial results may lie where the tiles' were)
         hipLaunchKernelGGL((attend_stream_kernel<D, kEight>), dim3((unsigned)p.blocks), dim3(kStreamWaves * kWave), 0, st, a);
-        if (p.shared) hipLaunchKernelGGL(join_stream_kernel<D>, dim3((unsigned)b.requests, head_blocks), dim3(kJoinWaves * kWave), 0, st, a);
+        if (p.shared) hipLaunchKernelGGL(join_stream_kernel<D>, dim3((unsigned)b.requests, head_blocks, p.join_tokens), dim3(kJoinWaves * kWave), 0, st, a);
     }
     return hipGetLastError();
 }

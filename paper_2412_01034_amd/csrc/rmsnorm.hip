@@ -214,32 +214,30 @@ __global__ __launch_bounds__(kGroup) void rmsnorm_back_kernel(const NormBackArgs
     }
 }
 
-// dweight[k] = sum over blocks of partial[block][k]: 16 threads a column of four, in a fixed order.
-__global__ __launch_bounds__(256) void rmsnorm_weight_kernel(const float* __restrict__ partial, int blocks, int K, float* __restrict__ dw) {
-    __shared__ float4 red[16][16];
+// dweight[k] = sum over blocks of partial[block][k]: kSlices threads a column of four, eight loads of each on their way, in a fixed order.
+constexpr int kSlices = 64;
+__global__ __launch_bounds__(16 * kSlices) void rmsnorm_weight_kernel(const float* __restrict__ partial, int blocks, int K, float* __restrict__ dw) {
+    __shared__ f32x4_t red[kSlices][16];
     const int c = threadIdx.x % 16, s = threadIdx.x / 16, n4 = K / 4;
     const int col = blockIdx.x * 16 + c;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col < n4)
-        for (int b = s; b < blocks; b += 16) {
-            const float4 p = reinterpret_cast<const float4*>(partial)[(size_t)b * n4 + col];
-            sum.x += p.x;
-            sum.y += p.y;
-            sum.z += p.z;
-            sum.w += p.w;
-        }
+    const f32x4_t* p = reinterpret_cast<const f32x4_t*>(partial) + min(col, n4 - 1);
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int b0 = s; b0 < blocks; b0 += 8 * kSlices) {
+        f32x4_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = p[(size_t)min(b0 + u * kSlices, blocks - 1) * n4];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (b0 + u * kSlices < blocks) sum += v[u];
+    }
     red[s][c] = sum;
     __syncthreads();
-    if (s != 0 || col >= n4) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) {
-        const float4 p = red[i][c];
-        sum.x += p.x;
-        sum.y += p.y;
-        sum.z += p.z;
-        sum.w += p.w;
+    for (int o = kSlices / 2; o >= 1; o >>= 1) {
+        if (s < o) red[s][c] = sum = sum + red[s + o][c];
+        __syncthreads();
     }
-    reinterpret_cast<float4*>(dw)[col] = sum;
+    if (s == 0 && col < n4) reinterpret_cast<f32x4_t*>(dw)[col] = sum;
 }
 
 int back_blocks(int M) {
@@ -289,7 +287,7 @@ hipError_t launch_rmsnorm_back(const uint16_t* h, const uint16_t* weight, float 
     else if (n8 <= 2048) QAIL_BACK(1024, 2);
     else QAIL_BACK(1024, 4);
 #undef QAIL_BACK
-    hipLaunchKernelGGL(rmsnorm_weight_kernel, dim3((K / 4 + 15) / 16), dim3(256), 0, st, ws, blocks, K, dweight);
+    hipLaunchKernelGGL(rmsnorm_weight_kernel, dim3((K / 4 + 15) / 16), dim3(16 * kSlices), 0, st, ws, blocks, K, dweight);
     return hipGetLastError();
 }
 
