@@ -15,7 +15,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kMaxItems = 8;    // linears that share the two launches
 constexpr int kMaxSplits = 4;   // shares of K
-constexpr int kDownWaves = 8, kUpWaves = 4;
+constexpr int kDownWaves = 8, kUpWaves = 4, kUpChunks = 4;
 
 struct AdapterItem {
     const uint16_t *x, *A, *B;
@@ -28,6 +28,7 @@ struct AdapterArgs {
     AdapterItem it[kMaxItems];
     const int32_t* rows;
     int M, slots, splits;
+    int chunks;   // of 64 columns that a wave of the second launch takes
 };
 
 // Calls f(a, mine) for the distinct adapters of the tile that are this slot's; `mine`: whether the lane's column (row m0 + lane % 16) uses it.
@@ -97,45 +98,30 @@ __global__ __launch_bounds__(kDownWaves* kWave) void adapters_down_kernel(const 
     });
 }
 
-// A wave adds to 16 rows of 64 columns.  Row i of tile t of the product is column 16 (i / 4) + 4 t + i % 4, so that a lane ends up with 16
+// A wave adds to 16 rows of `chunks` times 64 columns.  Row i of tile t of the product is column 16 (i / 4) + 4 t + i % 4, so that a lane ends up with 16
 // consecutive columns of one row.  t is split into two bf16 values (a relative 2^-17 is lost, where one alone would lose 2^-9).
 template <bool kWide>   // N % 8 == 0: rows of y are 16-byte aligned
-__device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& it, int m0, int n0, int slot) {
+__device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& it, int m0, int n_begin, int slot) {
     const int lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;
     const int N = it.N, r = it.r, M = a.M, m = m0 + col;
-    const int n = n0 + 16 * g;
-    uint16_t* const y = it.y + (size_t)min(m, M - 1) * N + n;
     each_adapter(a, it, m0, slot, [&](int of, bool mine) {
         const float scaling = it.scaling[of];
-        u32x4_t old[2];
-        if (kWide && mine) {   // on its way while the products are formed
+        bf16x8_t th[2], tl[2];   // of 32 j each
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-                if (n + 8 * half < N) old[half] = reinterpret_cast<u32x4_t*>(y)[half];
-        }
-        f32x4_t acc[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int j0 = 0; j0 < r; j0 += 32) {
-            const bool in = j0 + 8 * g < r;
-            u32x4_t bv[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int row = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
-                bv[t] = in ? *reinterpret_cast<const u32x4_t*>(it.B + ((size_t)of * N + row) * r + j0 + 8 * g) : u32x4_t{0u, 0u, 0u, 0u};
-            }
-            f32x4_t tl[kMaxSplits][2];
+        for (int jt = 0; jt < 2; ++jt) {
+            const bool in = mine && 32 * jt + 8 * g < r;
+            f32x4_t part[kMaxSplits][2];
 #pragma unroll
             for (int k = 0; k < kMaxSplits; ++k) {
                 const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-                const f32x4_t* p = reinterpret_cast<const f32x4_t*>(it.t + ((size_t)k * M + m) * r + j0 + 8 * g);
-                const bool have = in && mine && k < a.splits;
-                tl[k][0] = have ? p[0] : zero;
-                tl[k][1] = have ? p[1] : zero;
+                const f32x4_t* p = reinterpret_cast<const f32x4_t*>(it.t + ((size_t)k * M + m) * r + 32 * jt + 8 * g);
+                const bool have = in && k < a.splits;
+                part[k][0] = have ? p[0] : zero;
+                part[k][1] = have ? p[1] : zero;
             }
             float s[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] = (tl[0][e / 4][e % 4] + tl[1][e / 4][e % 4]) + (tl[2][e / 4][e % 4] + tl[3][e / 4][e % 4]);
+            for (int e = 0; e < 8; ++e) s[e] = (part[0][e / 4][e % 4] + part[1][e / 4][e % 4]) + (part[2][e / 4][e % 4] + part[3][e / 4][e % 4]);
             static_assert(kMaxSplits == 4, "four parts are added up");
             uint32_t hi[4], lo[4];
 #pragma unroll
@@ -143,33 +129,57 @@ __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& 
                 hi[e] = f32x2_to_bf16x2_rne(s[2 * e], s[2 * e + 1]);
                 lo[e] = f32x2_to_bf16x2_rne(s[2 * e] - __builtin_bit_cast(float, hi[e] << 16), s[2 * e + 1] - __builtin_bit_cast(float, hi[e] & 0xFFFF0000u));
             }
-            const bf16x8_t th = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]}), tr = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const bf16x8_t b = __builtin_bit_cast(bf16x8_t, bv[t]);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tr, acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, th, acc[t], 0, 0, 0);
-            }
+            th[jt] = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
+            tl[jt] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
         }
-        if (!mine || n >= N) return;
-        if (kWide) {
+        for (int n0 = n_begin, c = 0; c < a.chunks && n0 < N; ++c, n0 += 64) {
+            const int n = n0 + 16 * g;
+            uint16_t* const y = it.y + (size_t)min(m, M - 1) * N + n;
+            u32x4_t old[2];
+            if (kWide && mine) {   // on its way while the products are formed
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (n + 8 * half >= N) break;
-                u32x4_t w = old[half];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x4_t& d = acc[2 * half + e / 2];
-                    const uint32_t was = w[e];
-                    w[e] = f32x2_to_bf16x2_rne(fmaf(scaling, d[e % 2 * 2], __builtin_bit_cast(float, was << 16)),
-                                               fmaf(scaling, d[e % 2 * 2 + 1], __builtin_bit_cast(float, was & 0xFFFF0000u)));
-                }
-                reinterpret_cast<u32x4_t*>(y)[half] = w;
+                for (int half = 0; half < 2; ++half)
+                    if (n + 8 * half < N) old[half] = reinterpret_cast<u32x4_t*>(y)[half];
             }
-        } else {
+            f32x4_t acc[4];
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (n + e < N) y[e] = (uint16_t)f32x2_to_bf16x2_rne(fmaf(scaling, acc[e / 4][e % 4], bf16_bits_to_f32(y[e])), 0.f);
+            for (int t = 0; t < 4; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int jt = 0; jt < 2; ++jt) {
+                if (32 * jt >= r) break;
+                u32x4_t bv[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int row = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
+                    bv[t] = 32 * jt + 8 * g < r ? *reinterpret_cast<const u32x4_t*>(it.B + ((size_t)of * N + row) * r + 32 * jt + 8 * g) : u32x4_t{0u, 0u, 0u, 0u};
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const bf16x8_t b = __builtin_bit_cast(bf16x8_t, bv[t]);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tl[jt], acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, th[jt], acc[t], 0, 0, 0);
+                }
+            }
+            if (!mine || n >= N) continue;
+            if (kWide) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (n + 8 * half >= N) break;
+                    u32x4_t w = old[half];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x4_t& d = acc[2 * half + e / 2];
+                        const uint32_t was = w[e];
+                        w[e] = f32x2_to_bf16x2_rne(fmaf(scaling, d[e % 2 * 2], __builtin_bit_cast(float, was << 16)),
+                                                   fmaf(scaling, d[e % 2 * 2 + 1], __builtin_bit_cast(float, was & 0xFFFF0000u)));
+                    }
+                    reinterpret_cast<u32x4_t*>(y)[half] = w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (n + e < N) y[e] = (uint16_t)f32x2_to_bf16x2_rne(fmaf(scaling, acc[e / 4][e % 4], bf16_bits_to_f32(y[e])), 0.f);
+            }
         }
     });
 }
@@ -177,7 +187,7 @@ __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& 
 __global__ __launch_bounds__(kUpWaves* kWave) void adapters_up_kernel(const AdapterArgs a) {
     const AdapterItem& it = a.it[blockIdx.z];
     const int row_tiles = (a.M + 15) / 16;
-    const int m0 = blockIdx.x % row_tiles * 16, n0 = (blockIdx.x / row_tiles * kUpWaves + (int)threadIdx.x / kWave) * 64;
+    const int m0 = blockIdx.x % row_tiles * 16, n0 = (blockIdx.x / row_tiles * kUpWaves + (int)threadIdx.x / kWave) * 64 * a.chunks;
     if (n0 >= it.N) return;   // whole waves; no barrier below
     if (it.N % 8 == 0) add_up<true>(a, it, m0, n0, blockIdx.y);
     else add_up<false>(a, it, m0, n0, blockIdx.y);
@@ -185,7 +195,7 @@ __global__ __launch_bounds__(kUpWaves* kWave) void adapters_up_kernel(const Adap
 
 // Shares of K: more where the tiles alone leave the chip empty.
 int k_splits(int M, int count) {
-    const long long blocks = (long long)((M + 15) / 16) * count, s = device_cu_count() / blocks;
+    const long long blocks = (long long)((M + 15) / 16) * count, s = 2ll * device_cu_count() / blocks;
     return s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : (int)s;
 }
 
@@ -224,6 +234,7 @@ hipError_t in_groups(const qail_w4a16_item* items, const qail_adapters* ad, cons
         const int in_tile = M < 16 ? M : 16;   // distinct adapters of a tile, at most
         a.slots = most < in_tile ? most : in_tile;
         if (M > 64) a.slots = 1;
+        a.chunks = M > 64 ? kUpChunks : 1;
         launch(a, c, widest, (rank + 15) / 16);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -242,7 +253,7 @@ hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapter
 
 hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st) {
     return in_groups(items, ad, rows, count, M, t, [&](const AdapterArgs& a, int c, int widest, int) {
-        hipLaunchKernelGGL(adapters_up_kernel, dim3((M + 15) / 16 * ((widest + 64 * kUpWaves - 1) / (64 * kUpWaves)), a.slots, c), dim3(kUpWaves * kWave), 0, st, a);
+        hipLaunchKernelGGL(adapters_up_kernel, dim3((M + 15) / 16 * ((widest + 64 * kUpWaves * a.chunks - 1) / (64 * kUpWaves * a.chunks)), a.slots, c), dim3(kUpWaves * kWave), 0, st, a);
     });
 }
 
