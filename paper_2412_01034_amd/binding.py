@@ -166,7 +166,7 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-# The marshalling of three calls in C++ (csrc/marshal.cpp): a function returns the library's status, or None for a call that is not
+# The marshalling of the smallest calls in C++ (csrc/marshal.cpp): a function returns the library's status, or None for a call that is not
 # the plain case, which then goes the way below it.  Without the compiled module, or with one that was built for another Python,
 # torch or layout of the items, every call does.
 def _not_plain(*args):
@@ -174,16 +174,19 @@ def _not_plain(*args):
 
 
 _linear_native = _linear_batch_native = _conv_batch_native = _not_plain
+_rmsnorm_native = _rmsnorm_backward_native = _kv_append_native = _paged_attention_native = _adapters_batch_native = _not_plain
 
 
 def _marshal_for() -> tuple:
     """What a module has to be built for: its layouts are compiled in."""
     return (sys.hexversion >> 16, "%s %s" % (torch.__version__, torch.version.git_version), ctypes.sizeof(qail_wdesc),
-            ctypes.sizeof(qail_w4a16_item), ctypes.sizeof(qail_conv_item))
+            ctypes.sizeof(qail_w4a16_item), ctypes.sizeof(qail_conv_item), ctypes.sizeof(qail_kv_cache), ctypes.sizeof(qail_requests),
+            ctypes.sizeof(qail_adapters))
 
 
 def _use_native(L: ctypes.CDLL) -> None:
     global _linear_native, _linear_batch_native, _conv_batch_native
+    global _rmsnorm_native, _rmsnorm_backward_native, _kv_append_native, _paged_attention_native, _adapters_batch_native
     try:
         from . import _marshal
     except ImportError:
@@ -192,6 +195,10 @@ def _use_native(L: ctypes.CDLL) -> None:
         return
     _marshal.use(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.qail_w4a16_linear, L.qail_w4a16_linear_batch, L.qail_w4a4_conv_batch)))
     _linear_native, _linear_batch_native, _conv_batch_native = _marshal.w4a16_linear, _marshal.w4a16_linear_batch, _marshal.w4a4_conv_batch
+    _marshal.use_serving(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.qail_rmsnorm, L.qail_rmsnorm_backward, L.qail_kv_append, L.qail_paged_attention,
+                                                                           L.qail_w4a16_linear_adapters_batch)))
+    _rmsnorm_native, _rmsnorm_backward_native, _kv_append_native = _marshal.rmsnorm, _marshal.rmsnorm_backward, _marshal.kv_append
+    _paged_attention_native, _adapters_batch_native = _marshal.paged_attention, _marshal.adapters_batch
 
 
 def status_string(status: int) -> str:
@@ -658,6 +665,11 @@ def qail_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Op
                  residual_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, y_s8: Optional[torch.Tensor] = None,
                  y_scale: Optional[torch.Tensor] = None) -> None:
     """x, residual: bf16 [M, K]; residual_out (the rounded sum), y: bf16 [M, K]; y_s8: M * K bytes of codes; y_scale: fp32 [M]."""
+    status = _rmsnorm_native(x, weight, eps, residual, residual_out, y, y_s8, y_scale)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_rmsnorm")
+        return
     M, K = x.shape
     n = M * K
     if y_s8 is not None:
@@ -676,6 +688,11 @@ def qail_rmsnorm_backward_workspace(M: int, K: int) -> int:
 def qail_rmsnorm_backward(h: torch.Tensor, weight: torch.Tensor, eps: float, dy: torch.Tensor, dx: torch.Tensor, dweight: torch.Tensor,
                           workspace: torch.Tensor, dres: Optional[torch.Tensor] = None) -> None:
     """h, dy, dres, dx: bf16 [M, K]; dweight: fp32 [K]."""
+    status = _rmsnorm_backward_native(h, weight, eps, dy, dx, dweight, workspace, dres)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_rmsnorm_backward")
+        return
     M, K = h.shape
     n = M * K
     _check(lib().qail_rmsnorm_backward(_bf16(h, n, "h"), _bf16(weight, K, "weight"), eps, _bf16(dy, n, "dy"), _bf16(dres, n, "dres"), M, K,
@@ -730,11 +747,20 @@ def _heads(t: torch.Tensor, tokens: int, dim: int, what: str) -> Tuple[int, int,
     return t.data_ptr(), across if n > 1 else heads * d, heads
 
 
+def _are_step(cache, requests) -> bool:
+    return type(cache) is qail_kv_cache and type(requests) is qail_requests
+
+
 def qail_kv_append(cache: qail_kv_cache, requests: qail_requests, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                    q_out: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
                    errors: Optional[torch.Tensor] = None) -> None:
     """k, v: bf16 [tokens, heads, head_dim], q: bf16 [tokens, q_heads, head_dim], views of a wider tensor among them; q_out: contiguous;
     cos, sin: fp32 [positions, head_dim / 2]."""
+    status = _kv_append_native(cache, requests, k, v, q, q_out, cos, sin, errors) if _are_step(cache, requests) else None
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_kv_append")
+        return
     T, D = requests.tokens, cache.head_dim
     ka, ks, kh = _heads(k, T, D, "k")
     va, vs, vh = _heads(v, T, D, "v")
@@ -757,6 +783,11 @@ def qail_paged_attention_workspace(cache: qail_kv_cache, requests: qail_requests
 def qail_paged_attention(cache: qail_kv_cache, requests: qail_requests, q: torch.Tensor, out: torch.Tensor, scale: float,
                          workspace: Optional[torch.Tensor] = None, errors: Optional[torch.Tensor] = None) -> None:
     """q: bf16 [tokens, q_heads, head_dim], a view of a wider tensor among them; out: contiguous."""
+    status = _paged_attention_native(cache, requests, q, out, scale, workspace, errors) if _are_step(cache, requests) else None
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_paged_attention")
+        return
     T, D = requests.tokens, cache.head_dim
     qa, qs, qh = _heads(q, T, D, "q")
     ws, wsb = (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
@@ -785,6 +816,13 @@ def qail_w4a16_adapters_workspace(items, adapters, count: int, M: int) -> int:
 def qail_w4a16_linear_adapters_batch(items, adapters, row_adapter: torch.Tensor, count: int, M: int, workspace: torch.Tensor,
                                      stream: Optional[int] = None) -> None:
     """items: make_w4a16_items, adapters: make_adapters of the same list; row_adapter: int32 [M], -1 for a row without an adapter."""
+    status = None
+    if stream is None and getattr(items, "_type_", None) is qail_w4a16_item and getattr(adapters, "_type_", None) is qail_adapters:
+        status = _adapters_batch_native(items, adapters, row_adapter, count, M, workspace)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_w4a16_linear_adapters_batch")
+        return
     wsb = workspace.nbytes if workspace is not None else 0
     _check(lib().qail_w4a16_linear_adapters_batch(items, adapters, _int32(row_adapter, M, "row_adapter"), count, M, _ptr(workspace), wsb,
                                                   _stream() if stream is None else stream), "qail_w4a16_linear_adapters_batch")

@@ -514,3 +514,67 @@ def test_adapters_in_a_graph(B):
         B.qail_w4a16_linear_adapters_batch(handle, ad, rows, 2, M, ws)
         torch.cuda.synchronize()
         assert all(torch.equal(e["y"], y) for e, y in zip(items, got))
+
+
+# -------------------------------------------------------------------------------------- marshalling --
+
+def test_native_marshalling_takes_plain_calls_with_the_same_results(B, monkeypatch):
+    """Each of the five calls is taken by the compiled marshalling, on the current stream, and gives what the way through Python gives."""
+    s = P.Step([2, 1], [30, 20], 4, 2, 64, 16, False, 61, pad=8)
+    pools, keep = s.pools("cuda"), (s.table.cuda(), s.starts.cuda(), s.kv_len.cuda(), s.qkv.cuda())
+    c, b = B.make_kv_cache(*pools), B.make_requests(*keep[:3], tokens=3, max_new=2, max_len=30)
+    q, k, v = s.split(keep[3])
+    cos, sin = (a.cuda() for a in P.angles(40, 64))
+    x, w = P.normal((3, 256), 1).to(BF16).cuda(), P.normal((256,), 2).to(BF16).cuda()
+    h, y, dx, q_out, out = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty((3, 4, 64), dtype=BF16, device="cuda"), \
+        torch.empty((3, 4, 64), dtype=BF16, device="cuda")
+    dw = torch.empty(256, device="cuda")
+    codes, scale = torch.empty((3, 256), dtype=torch.int8, device="cuda"), torch.empty(3, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    items = adapter_case([(64, 128, 64)], 3, 2, 8, 70)
+    handle, ad, rows = B.make_w4a16_items(items, 3), B.make_adapters(items), torch.tensor([0, 1, -1], dtype=torch.int32, device="cuda")
+    errors = torch.zeros(1, dtype=torch.int32, device="cuda")
+    outputs = [h, y, dx, q_out, out, dw, codes, scale, pools[0], pools[1], items[0]["y"]]
+
+    def native():
+        return [B._rmsnorm_native(x, w, 1e-5, x, h, y, codes, scale), B._rmsnorm_backward_native(x, w, 1e-5, h, dx, dw, ws, y),
+                B._kv_append_native(c, b, k, v, q, q_out, cos, sin, errors), B._paged_attention_native(c, b, q_out, out, 0.125, None, errors),
+                B._paged_attention_native(c, B.make_requests(keep[0][:1], keep[1][:2], keep[2][:1], tokens=1, max_new=1, max_len=30), q[:1], out[:1], 0.125, ws, None),
+                B._paged_attention_native(c, b, q_out, out, 0.125, ws, None), B._adapters_batch_native(handle, ad, rows, 1, 3, ws)]
+
+    def python():
+        B.qail_rmsnorm(x, w, 1e-5, residual=x, residual_out=h, y=y, y_s8=codes, y_scale=scale)
+        B.qail_rmsnorm_backward(x, w, 1e-5, h, dx, dw, ws, dres=y)
+        B.qail_kv_append(c, b, k, v, q=q, q_out=q_out, cos=cos, sin=sin, errors=errors)
+        B.qail_paged_attention(c, b, q_out, out, 0.125, None, errors)
+        B.qail_w4a16_linear_adapters_batch(handle, ad, rows, 1, 3, ws)
+
+    assert native() == [B.QAIL_OK] * 7
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outputs]
+    for name in ("_rmsnorm_native", "_rmsnorm_backward_native", "_kv_append_native", "_paged_attention_native", "_adapters_batch_native"):
+        monkeypatch.setattr(B, name, B._not_plain)
+    for t in outputs[:8] + outputs[10:]:
+        t.zero_()
+    python()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outputs[:8] + outputs[10:], want[:8] + want[10:]))
+    assert torch.equal(pools[0].view(torch.int16), want[8].view(torch.int16)) and errors.item() == 0
+    monkeypatch.undo()
+    # on the stream that is current
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for t in outputs[:2]:
+            t.zero_()
+        assert B._rmsnorm_native(x, w, 1e-5, x, h, y, codes, scale) == B.QAIL_OK
+    side.synchronize()
+    assert torch.equal(h, want[0]) and torch.equal(y, want[1])
+    # errors come back as the library's
+    with pytest.raises(B.QailError):
+        B.qail_rmsnorm(x, w, -1.0, y=y)
+    assert B._rmsnorm_native(x.float(), w, 1e-5, None, None, y, None, None) is None
+    with pytest.raises(ValueError, match="bfloat16"):
+        B.qail_rmsnorm(x.float(), w, 1e-5, y=y)
+    with pytest.raises(ValueError, match="heads of a token must be contiguous"):
+        B.qail_paged_attention(c, b, q.transpose(1, 2).contiguous().transpose(1, 2), out, 0.125)

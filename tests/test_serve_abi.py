@@ -230,3 +230,26 @@ def test_adapters_refusals(B):
     assert call(items, ad, ws=None) == B.QAIL_ERR_WORKSPACE and call(items, ad, n=need - 1) == B.QAIL_ERR_WORKSPACE
     assert call(items, ad, count=0) == B.QAIL_OK
     assert L.qail_w4a16_adapters_workspace(items, ad, 1, 3, None) == B.QAIL_ERR_NULL
+
+
+# -------------------------------------------------------------------------------------- marshalling --
+
+def test_native_calls_leave_what_is_not_plain_to_python(B):
+    """None for what the compiled marshalling does not take (here: nothing is on a GPU), the library's own errors in Python's words."""
+    x, w = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros(64, dtype=torch.bfloat16)
+    assert B._rmsnorm_native(x, w, 1e-5, None, None, x, None, None) is None
+    assert B._rmsnorm_backward_native(x, w, 1e-5, x, x, w, x, None) is None
+    c, b = cache(B), requests(B)
+    t = torch.zeros((7, 2, 128), dtype=torch.bfloat16)
+    assert B._kv_append_native(c, b, t, t, None, None, None, None, None) is None
+    assert B._paged_attention_native(c, b, t, t, 0.1, None, None) is None
+    assert B._adapters_batch_native((B.qail_w4a16_item * 1)(), (B.qail_adapters * 1)(), torch.zeros(1, dtype=torch.int32), 1, 1, x) is None
+    for call in (B._rmsnorm_native, B._rmsnorm_backward_native, B._kv_append_native, B._paged_attention_native, B._adapters_batch_native):
+        assert call() is None and call(*[None] * 8) is None and call(*[5] * 7) is None
+    # structures of other kinds, also of the same size, are none of the cache's
+    item = B.qail_w4a16_item()
+    assert ctypes.sizeof(item) == ctypes.sizeof(c)
+    with pytest.raises((ctypes.ArgumentError, AttributeError)):
+        B.qail_paged_attention(item, b, t, t, 0.1)
+    with pytest.raises((ctypes.ArgumentError, ValueError)):
+        B.qail_w4a16_linear_adapters_batch((B.qail_adapters * 1)(), (B.qail_adapters * 1)(), torch.zeros(1, dtype=torch.int32), 1, 1, x)
