@@ -49,6 +49,93 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
     return __builtin_bit_cast(bf16x8_t, u32x4_t{w[0], w[1], w[2], w[3]});
 }
 
+// One row by one wave, which reads no key behind the row's last: keys k0 .. last of request r and head h.  The products on the matrix cores
+// multiply the values of keys that a row does not see by a p of zero, and zero times an infinity or NaN is NaN: where that may have
+// happened (a result that is not finite, of a row that has not seen all keys of its tile) the row is computed again, here.
+// A lane takes a key of 64 for the scores, then D / 64 values of every key.  o, m and l as in the kernels: not yet divided by l.
+template <int D, bool kEight>
+__device__ __forceinline__ void attend_row_alone(const AttentionArgs& a, int r, int h, const uint16_t* q, int k0, int last, float* o, float& m, float& l) {
+    constexpr int kRowBytes = kEight ? D : 2 * D, kPer = D / kWave;
+    const int lane = threadIdx.x % kWave, slots = 1 << a.c.page_shift;
+    bool bad = false;   // (has been reported)
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int kt = k0; kt <= last; kt += kWave) {
+        const int key = min(kt + lane, last);
+        const size_t slot = (((size_t)page_of(a.c, page_entry(a.c, r, key >> a.c.page_shift), bad) * a.c.heads + h) << a.c.page_shift) + (key & (slots - 1));
+        const uint8_t* const k = static_cast<const uint8_t*>(a.c.k) + slot * kRowBytes;
+        float s = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 8) {
+            bf16x8_t kd;
+            if constexpr (kEight) {
+                const uint2 c = *reinterpret_cast<const uint2*>(k + d);
+                kd = codes_to_bf16(c.x, c.y);
+            } else {
+                kd = as_bf16x8(*reinterpret_cast<const u32x4_t*>(k + 2 * d));
+            }
+            const bf16x8_t qd = as_bf16x8(*reinterpret_cast<const u32x4_t*>(q + d));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fmaf((float)kd[e], (float)qd[e], s);
+        }
+        if constexpr (kEight) s *= a.c.k_scale[slot];
+        if (kt + lane > last) s = -INFINITY;
+        float top = s;
+#pragma unroll
+        for (int i = 32; i >= 1; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, kWave));
+        const float m_new = fmaxf(m, top), off = m_new == -INFINITY ? 0.f : m_new * a.scale;
+        const float alpha = __builtin_amdgcn_exp2f(m * a.scale - off);   // 0 where there was no key yet
+        float p = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -off)), sum = p;
+#pragma unroll
+        for (int i = 32; i >= 1; i >>= 1) sum += __shfl_xor(sum, i, kWave);
+        l = fmaf(l, alpha, sum);
+        m = m_new;
+        if constexpr (kEight) p *= a.c.v_scale[slot];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] *= alpha;
+        const int held = min(kWave, last + 1 - kt);
+#pragma unroll 1
+        for (int i0 = 0; i0 < held; i0 += 8) {
+            float x[8][kPer];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {   // past the end the last is read again and not counted
+                const uint8_t* const v = static_cast<const uint8_t*>(a.c.v) + (size_t)__shfl((long long)slot, min(i0 + u, held - 1), kWave) * kRowBytes;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    if constexpr (kEight) x[u][e] = (float)reinterpret_cast<const int8_t*>(v)[lane * kPer + e];
+                    else x[u][e] = bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(v)[lane * kPer + e]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float pi = __shfl(p, min(i0 + u, held - 1), kWave);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (i0 + u < held) o[e] = fmaf(pi, x[u][e], o[e]);
+            }
+        }
+    }
+}
+
+// 1 / l; no key: a factor of 0, the row is zeros.
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; }
+
+// That row's result to `out`, or to place `at` of the partial ones where there is one.
+template <int D>
+__device__ __forceinline__ void store_row_alone(const AttentionArgs& a, const float* o, float m, float l, uint16_t* out, long long at) {
+    constexpr int kPer = D / kWave;
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        if (at < 0) out[lane * kPer + e] = (uint16_t)f32x2_to_bf16x2_rne(o[e] * inverse(l), 0.f);
+        else a.part_o[at * D + lane * kPer + e] = o[e];
+    }
+    if (at >= 0 && lane == 0) a.part_ml[at] = make_float2(m, l);
+}
+
 // ---------------------------------------------------------------------------- few rows: a stream of keys --
 //
 // Up to 16 rows (a decode step: the heads that share a head of the cache) against all keys: bound by the cache's bytes, each read
@@ -232,12 +319,12 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
         for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4_t*>(lds_o + (wave * 16 + col) * S::kPadO + 16 * d + 4 * g) = o[d];
         __syncthreads();
         constexpr int kLanesO = D / 8;   // of an output row, eight values each
-        for (int i = threadIdx.x / kLanesO; i < min(kStreamRows, rows - row0); i += kStreamWaves * kWave / kLanesO) {
-            const int d = threadIdx.x % kLanesO * 8;
-            float top = ml[0][i].x;
+        static_assert(kStreamWaves * kWave / kLanesO >= kStreamRows, "the block's threads cover all rows");
+        const int i = threadIdx.x / kLanesO, d = threadIdx.x % kLanesO * 8, n = min(kStreamRows, rows - row0);
+        float top = -INFINITY, sum = 0.f, acc[8] = {}, odd = 0.f;
+        if (i < n) {
 #pragma unroll
-            for (int w = 1; w < kStreamWaves; ++w) top = fmaxf(top, ml[w][i].x);
-            float sum = 0.f, acc[8] = {};
+            for (int w = 0; w < kStreamWaves; ++w) top = fmaxf(top, ml[w][i].x);
 #pragma unroll
             for (int w = 0; w < kStreamWaves; ++w) {
                 const float f = ml[w][i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[w][i].x - top) * a.scale);
@@ -245,15 +332,26 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] = fmaf(f, lds_o[(w * 16 + i) * S::kPadO + d + e], acc[e]);
             }
-            const size_t at = (size_t)(rq.start + (row0 + i) / a.group) * a.q_heads + h * a.group + (row0 + i) % a.group;
+        }
+        // where a row's result goes, and whether that is a partial one
+        auto out_of = [&](int row) { return (size_t)(rq.start + (row0 + row) / a.group) * a.q_heads + h * a.group + (row0 + row) % a.group; };
+        unsigned long long left = 0;
+        if (__builtin_expect(before + row0 / a.group < k1 - 1, 0)) {   // there are keys that a row does not see; its own scores are no NaN
+            if (i < n && before + (row0 + i) / a.group < k1 - 1 && sum == sum)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) odd = fmaf(acc[e], 0.f, odd);
+            left = __ballot(odd != 0.f);   // NaN
+        }
+        const bool again = (left >> (lane / kLanesO * kLanesO)) & ((1ull << kLanesO) - 1);
+        if (i < n && !again) {
             if (place < 0) {
-                const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
+                const float inv = inverse(sum);
                 u32x4_t w;
                 w.x = f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv);
                 w.y = f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv);
                 w.z = f32x2_to_bf16x2_rne(acc[4] * inv, acc[5] * inv);
                 w.w = f32x2_to_bf16x2_rne(acc[6] * inv, acc[7] * inv);
-                *reinterpret_cast<u32x4_t*>(a.out + at * D + d) = w;
+                *reinterpret_cast<u32x4_t*>(a.out + out_of(i) * D + d) = w;
             } else {
                 const long long to = place * kStreamRows + i;
                 float4* out = reinterpret_cast<float4*>(a.part_o + to * D + d);
@@ -261,6 +359,13 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
                 out[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
                 if (d == 0) a.part_ml[to] = make_float2(top, sum);
             }
+        }
+        while (__builtin_expect(left != 0, 0)) {   // the wave's rows that are computed again
+            const int which = __builtin_ctzll(left) / kLanesO, row = wave * (kWave / kLanesO) + which, token = (row0 + row) / a.group;
+            left &= ~(((1ull << kLanesO) - 1) << (which * kLanesO));
+            float again_o[D / kWave], again_m, again_l;
+            attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + token) * a.q_stride + (h * a.group + (row0 + row) % a.group) * D, k0, before + token, again_o, again_m, again_l);
+            store_row_alone<D>(a, again_o, again_m, again_l, a.out + out_of(row) * D, place < 0 ? -1 : place * kStreamRows + row);
         }
         __syncthreads();
     }
@@ -376,7 +481,7 @@ __device__ __forceinline__ void join_row(const AttentionArgs& a, long long count
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
     }
-    const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;
+    const float inv = inverse(sum);
     if (lane < kLanes) reinterpret_cast<uint2*>(out)[lane] = uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }
 
@@ -680,24 +785,40 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
     if (bad) report(a.c);
 
     const float sum = l + __shfl_xor(l, 32, kWave);
-    if (row >= rows) return;
     const size_t at = (size_t)(rq.start + token) * a.q_heads + h * a.group + row % a.group;
-    if (count == 1) {
-        const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // no key: zeros
+    float odd = 0.f;
+    if (row < rows && lim < k1 - 1 && sum == sum)   // there are keys that the row does not see; its own scores are no NaN
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
-                    uint2{f32x2_to_bf16x2_rne(o[d][e] * inv, o[d][e + 1] * inv), f32x2_to_bf16x2_rne(o[d][e + 2] * inv, o[d][e + 3] * inv)};
-    } else {
-        float* out = a.part_o + (at * a.most + split) * D;
+            for (int e = 0; e < 16; ++e) odd = fmaf(o[d][e], 0.f, odd);
+    odd += __shfl_xor(odd, 32, kWave);
+    unsigned left = (unsigned)__ballot(odd != 0.f);   // NaN
+    if (row < rows && !((left >> col) & 1)) {
+        if (count == 1) {
+            const float inv = inverse(sum);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
+            for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
-        if (half == 0) a.part_ml[at * a.most + split] = make_float2(m, sum);
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 2 * e + 4 * half) =
+                        uint2{f32x2_to_bf16x2_rne(o[d][e] * inv, o[d][e + 1] * inv), f32x2_to_bf16x2_rne(o[d][e + 2] * inv, o[d][e + 3] * inv)};
+        } else {
+            float* out = a.part_o + (at * a.most + split) * D;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<float4*>(out + 32 * d + 2 * e + 4 * half) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
+            if (half == 0) a.part_ml[at * a.most + split] = make_float2(m, sum);
+        }
+    }
+    for (; __builtin_expect(left != 0, 0); left &= left - 1) {   // rows that are computed again
+        const int again = row0 + wave * 32 + __builtin_ctz(left), new_token = again / a.group, head = h * a.group + again % a.group;
+        const size_t to = (size_t)(rq.start + new_token) * a.q_heads + head;
+        float again_o[D / kWave], again_m, again_l;
+        attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + new_token) * a.q_stride + head * D, range.begin, min(before + new_token, k1 - 1), again_o, again_m, again_l);
+        store_row_alone<D>(a, again_o, again_m, again_l, a.out + to * D, count == 1 ? -1 : (long long)(to * a.most + split));
     }
 }
 
@@ -734,7 +855,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const Att
             acc += v[u] * w;
         }
     }
-    const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;
+    const float inv = inverse(sum);
     reinterpret_cast<uint2*>(a.out + at * D)[threadIdx.x % kLanes] =
         uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }

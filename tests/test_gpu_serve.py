@@ -270,6 +270,39 @@ def test_paged_attention_scores_of_any_size(B, eight):
     within(attention(B, s, 1.0), want, tol)
 
 
+# the last keys of the first request, from one on, hold what is not finite: few rows, rows of many tokens, grouped heads, both kernels in one call,
+# keys that are divided among blocks
+UNSEEN = [([5], [90], 2, 1, 64, 16, 87), ([4, 3], [4, 40], 4, 4, 128, 16, 1), ([70], [70], 2, 1, 128, 16, 33), ([200, 2], [1300, 9], 4, 1, 64, 32, 1250), ([9], [2500], 1, 1, 128, 64, 2495)]
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page,first", UNSEEN)
+def test_what_a_token_does_not_see_stays_out(B, new, lens, heads, kv_heads, dim, page, first, eight, value):
+    """An infinity or NaN in a later token's value (one of its values, or its step) and NaN in its key: the rows in front of it are what they are without
+    it, the rows that see it are not finite in the values concerned."""
+    s = P.Step(new, lens, heads, kv_heads, dim, page, eight, 700 + first, pad=8)
+    scale = 1 / math.sqrt(dim)
+    want, tol = P.attend(s, scale)
+    rows = torch.arange(s.tokens)
+    sees = (rows < new[0]) & (lens[0] - new[0] + rows >= first)
+    at = slice(None) if eight else 3
+    for only_v in (True, False):
+        k, v = s.values[0]
+        for t in (v,) if only_v else (k, v):
+            if eight:
+                t[1][:, first] = value if t is v else math.nan
+            else:
+                t[:, first, 3] = value if t is v else math.nan
+        out = attention(B, s, scale)
+        within(out[~sees], want[~sees], tol[~sees], "before")
+        got = out[sees].float().cpu()
+        assert not torch.isfinite(got[..., at] if only_v else got).any()
+        if not eight and only_v:
+            others = torch.arange(dim) != 3
+            within(out[sees][..., others], want[sees][..., others], tol[sees][..., others], "beside")
+
+
 def test_paged_attention_beyond_32_bits(B):
     """Pages that lie more than 4 GB into the cache."""
     s = P.Step([1, 40], [200, 100], 2, 1, 128, 256, False, 9, pool=70000)    # 70000 pages of 64 KB
