@@ -139,7 +139,7 @@ size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b,
 hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
                                   uint16_t* out, uint32_t* errors, void* ws, hipStream_t st);
 // fp32 values of workspace for the down-projections of a list; `t` of the two launches has as many
-size_t adapters_workspace(const qail_adapters* ad, int count, int M);
+size_t adapters_workspace(const qail_w4a16_item* items, const qail_adapters* ad, int count, int M);
 hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
 hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
 

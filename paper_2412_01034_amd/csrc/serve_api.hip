@@ -162,7 +162,7 @@ int qail_w4a16_adapters_workspace(const qail_w4a16_item* items, const qail_adapt
     const int e = check_adapters(items, adapters, count, M, &base);
     if (e != QAIL_OK) return e;
     if (!bytes) return QAIL_ERR_NULL;
-    *bytes = round256(base) + round256(adapters_workspace(adapters, count, M) * sizeof(float));
+    *bytes = round256(base) + round256(adapters_workspace(items, adapters, count, M) * sizeof(float));
     return QAIL_OK;
 }
 
@@ -182,7 +182,7 @@ int qail_w4a16_linear_adapters_batch(const qail_w4a16_item* items, const qail_ad
                   aligned(ad.B) && aligned(ad.scaling);
     }
     if (!sixteen) return QAIL_ERR_ALIGN;
-    const size_t need = round256(base) + round256(adapters_workspace(adapters, count, M) * sizeof(float));
+    const size_t need = round256(base) + round256(adapters_workspace(items, adapters, count, M) * sizeof(float));
     if (!workspace || workspace_bytes < need) return QAIL_ERR_WORKSPACE;
     if (!aligned<256>(workspace)) return QAIL_ERR_ALIGN;
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -480,6 +480,9 @@ ADAPTERS = [
     ([(129, 256, 128)], 300, 2, 40),
     ([(64, 72, 8)], 5, 3, 8),                               # K of no full step
     ([(64 + 8 * i, 256, 128) for i in range(11)], 4, 3, 16),   # more linears than share a launch
+    ([(64, 72, 8), (256, 2816, 128), (520, 1024, 128)], 333, 5, 64),   # many rows: shares of K of different linears
+    ([(96, 512, 128)], 260, 200, 16),                                  # ... of an adapter each
+    ([(48, 9216, 128), (40, 256, 128)], 270, 3, 24),                   # ... the most shares and one
 ]
 
 
