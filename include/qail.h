@@ -421,7 +421,7 @@ int qail_qbc_loss(const float* logits_q, const float* logits_fp, int32_t B, int3
  *   h_out        bf16 [M][K], the rounded h, or NULL; may be x or residual itself
  *   y            bf16 [M][K] or NULL; may be x or residual itself, when h_out is not
  *   y_s8, y_scale  uint32 [M][K/4] and fp32 [M], both or neither
- * At least one of h_out (with a residual), y and y_s8 is required.  K % 8 == 0, M * K < 2^31. */
+ * At least one of h_out (with a residual), y and y_s8 is required.  K % 8 == 0, K <= 32768, M * K < 2^31, M < 2^26. */
 int qail_rmsnorm(const uint16_t* x, const uint16_t* residual, const uint16_t* weight, float eps, int32_t M, int32_t K,
                  uint16_t* h_out, uint16_t* y, uint32_t* y_s8, float* y_scale, void* stream);
 
@@ -461,6 +461,7 @@ int qail_kv_cache_sizes(const qail_kv_cache* c, size_t* data_bytes, size_t* scal
  * kv_len[r] - (q_start[r + 1] - q_start[r]) + i; a token at position p lies in slot p % page_size of page page_table[r][p / page_size].
  * page_table, q_start and kv_len are device memory (4-byte aligned), read when the kernels run, so that a captured graph can be
  * replayed with other contents: q_start ascends from 0 to `tokens`.
+ * tokens < 2^24, requests <= 2^20, max_pages * page_size <= 2^30; for attention requests * heads of the cache <= 2^22 and tokens * q_heads <= 2^30.
  * max_new and max_len are upper bounds on a request's new tokens and its kv_len that the launches are planned by; contents
  * beyond them cost speed, not results. */
 typedef struct {
@@ -498,7 +499,7 @@ int qail_kv_append(const qail_kv_cache* c, const qail_requests* b, const uint16_
  * included, does not reach its rows.
  *   q         bf16, token t and head a at t * q_stride + a * head_dim; q_stride % 8 == 0
  *   out       bf16 [tokens][q_heads][head_dim]
- *   scale     finite
+ *   scale     > 0, finite
  * The workspace (256-byte aligned; may be NULL where the query says 0) holds the partial results of keys that are divided among blocks. */
 int qail_paged_attention_workspace(const qail_kv_cache* c, const qail_requests* b, int32_t q_heads, size_t* bytes);
 int qail_paged_attention(const qail_kv_cache* c, const qail_requests* b, const uint16_t* q, int64_t q_stride, int32_t q_heads, float scale,

@@ -15,7 +15,7 @@ size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
 int check_norm(int32_t M, int32_t K, float eps) {
     if (M < 1 || K < 8 || K % 8 != 0 || !(eps > 0.f && eps <= 3.0e38f)) return QAIL_ERR_SHAPE;
-    if ((long long)M * K > 0x7FFFFFFFll || !rmsnorm_supports(K)) return QAIL_ERR_UNSUPPORTED;
+    if ((long long)M * K > 0x7FFFFFFFll || M >= (1 << 26) || !rmsnorm_supports(K)) return QAIL_ERR_UNSUPPORTED;   // 64 threads a row, below 2^32
     return QAIL_OK;
 }
 
@@ -34,8 +34,8 @@ int check_step(const qail_kv_cache* c, const qail_requests* b) {
     if (e != QAIL_OK) return e;
     if (!b) return QAIL_ERR_NULL;
     if (b->requests < 1 || b->max_pages < 1 || b->tokens < 0 || b->max_new < 0 || b->max_len < 0) return QAIL_ERR_SHAPE;
-    // positions and rows are 32-bit values in the kernels
-    if ((long long)b->max_pages * c->page_size > (1 << 30) || b->tokens > (1 << 26) || b->requests > (1 << 20)) return QAIL_ERR_UNSUPPORTED;
+    // positions and rows are 32-bit values in the kernels, and 256 threads a token stay below 2^32
+    if ((long long)b->max_pages * c->page_size > (1 << 30) || b->tokens >= (1 << 24) || b->requests > (1 << 20)) return QAIL_ERR_UNSUPPORTED;
     if (!c->k || !c->v || !b->page_table || !b->q_start || !b->kv_len) return QAIL_ERR_NULL;
     if (c->type == QAIL_KV_S8 && (!c->k_scale || !c->v_scale)) return QAIL_ERR_NULL;
     if (!aligned(c->k) || !aligned(c->v) || !aligned(c->k_scale) || !aligned(c->v_scale) || !aligned<4>(b->page_table) || !aligned<4>(b->q_start) ||
@@ -51,7 +51,7 @@ int check_rows(int64_t stride, int heads, int head_dim) {
 
 int check_heads(const qail_kv_cache* c, const qail_requests* b, int32_t q_heads) {
     if (q_heads < 1 || q_heads % c->heads != 0) return QAIL_ERR_SHAPE;
-    if (q_heads > 65535 || (long long)b->tokens * q_heads > (1 << 30) || (long long)b->requests * c->heads > (1 << 24)) return QAIL_ERR_UNSUPPORTED;
+    if (q_heads > 65535 || (long long)b->tokens * q_heads > (1 << 30) || (long long)b->requests * c->heads > (1 << 22)) return QAIL_ERR_UNSUPPORTED;
     return QAIL_OK;
 }
 

@@ -172,6 +172,16 @@ def test_paged_attention_refusals(B):
     assert B.qail_paged_attention_workspace(c, requests(B, tokens=0), 4) == 0
 
 
+def test_sizes_whose_launches_would_be_too_large_are_refused(B):
+    """A launch has less than 2^32 threads: rows of a norm have 64 at least, tokens and (request, head) pairs 256."""
+    assert norm(B, M=1 << 26, K=8) == B.QAIL_ERR_UNSUPPORTED
+    c, many = cache(B), requests(B, tokens=1 << 24)
+    assert append(B, c, many, q=None, out=None) == B.QAIL_ERR_UNSUPPORTED and attend(B, c, many) == B.QAIL_ERR_UNSUPPORTED
+    heads = (1 << 22) // (1 << 20) + 1
+    wide = dict(heads=heads, qs=heads * 128)
+    assert attend(B, cache(B, heads=heads), requests(B, requests=1 << 20), **wide) == B.QAIL_ERR_UNSUPPORTED
+
+
 def test_binding_refuses_what_is_no_device_tensor(B):
     bf = torch.zeros((4, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="device tensor"):
