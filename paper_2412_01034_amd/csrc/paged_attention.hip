@@ -518,8 +518,8 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
 // Bound by the vector unit next to the matrix cores: of 64 keys a wave has 32 products of 32 cycles each, and for every score a
 // multiply-add, an exponential and three halves of an instruction for the maximum, the sum (two rounded p at a time) and
 // the rounding.  So nothing else is left in the loop: places in LDS are registers and immediates (the loop has a copy for either half), places in memory
-// scalars, but for the last 64 keys.  Four prompts to 2500 tokens (111 GFLOP) take 160 us, 690 TFLOP/s, three chunks behind 7000 to 13000 keys 765: the
-// matrix cores are busy 34 % of the time and the vector unit 36 %, next to each other for little of it; a quarter of a wave's time is waiting.
+// scalars, but for the last 64 keys.  Four prompts to 2500 tokens (111 GFLOP) take 160 us, 690 TFLOP/s, three chunks behind 7000 to 13000 keys 760: the
+// matrix cores are busy 36 and 40 % of the time and the vector unit 41 and 39 %, next to each other for little of it; a quarter of a wave's time is waiting.
 // 32 keys at a time and three blocks a compute unit instead of two: prompts the same, chunks 171 -> 213.
 constexpr int kTileWaves = 4, kTileKeys = 64, kTileRows = kTileWaves * 32;
 
