@@ -470,7 +470,7 @@ __device__ __forceinline__ void join_row(const AttentionArgs& a, long long count
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (i0 + u * kAtOnce + lane / kLanes >= count || ml[u].x == -INFINITY) continue;   // (no key: a sum of 0)
+            if (i0 + u * kAtOnce + lane / kLanes >= count || ml[u].y == 0.f) continue;   // no key; scores that are all NaN leave a maximum of -inf too, and a sum of NaN
             const float w = __builtin_amdgcn_exp2f((ml[u].x - top) * a.scale);
             sum = fmaf(w, ml[u].y, sum);
             acc += v[u] * w;
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const Att
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const float2 x = ml[min(i0 + u, count - 1)];
-            if (i0 + u >= count || x.x == -INFINITY) continue;   // (no key: a sum of 0)
+            if (i0 + u >= count || x.y == 0.f) continue;   // no key; scores that are all NaN leave a maximum of -inf too, and a sum of NaN
             const float w = __builtin_amdgcn_exp2f((x.x - top) * a.scale);
             sum = fmaf(w, x.y, sum);
             acc += v[u] * w;
