@@ -438,7 +438,8 @@ int qail_rmsnorm_backward(const uint16_t* h, const uint16_t* weight, float eps, 
 /* How a cache holds keys and values. */
 typedef enum {
     QAIL_KV_BF16 = 0,
-    QAIL_KV_S8 = 1    /* signed codes -127..127 with one fp32 step per token and head: max|t| / 127, 1 for an all-zero row */
+    QAIL_KV_S8 = 1    /* signed codes -127..127 with one fp32 step per token and head: max|t| / 127, 1 for an all-zero row,
+                         NaN where a value is not finite */
 } qail_kv_type;
 
 /* The keys and values of one layer in pages that requests are given as they grow.  k and v (and their steps) are

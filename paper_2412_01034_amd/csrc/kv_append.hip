@@ -86,10 +86,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
     if constexpr (kEight) {
         float most = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fmaxf(fabsf(x[e]), fabsf(y[e])));
+        for (int e = 0; e < 8; ++e) most = max_magnitude(most, max_magnitude(fabsf(x[e]), fabsf(y[e])));
 #pragma unroll
-        for (int o = kLanes / 2; o >= 1; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
-        const float s = most > 0.f ? most / 127.0f : 1.0f;
+        for (int o = kLanes / 2; o >= 1; o >>= 1) most = max_magnitude(most, __shfl_xor(most, o, kWave));
+        const float s = step_of_codes(most);
         auto codes = [&](const float* f) {
             uint32_t w[2] = {0u, 0u};
 #pragma unroll

@@ -65,3 +65,40 @@ def test_nan_of_all_keys_of_a_share(B, new, lens, heads, kv_heads, dim, page, fi
         (k[1] if eight else k)[0, first:last] = math.nan
 
     nan_rows(B, s, poison, rows)
+
+
+# -------------------------------------------------------------------------------- a cache of bytes --
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_head_that_is_not_finite_has_a_step_of_nan(B, dim, value):
+    """One value of a key, one of a value, a whole head: their tokens are NaN when they are read; every other code and step is what it is without them."""
+    s = P.Step([3, 2], [20, 40], 2, 2, dim, 16, True, 11)
+    cos, sin = (t.cuda() for t in P.angles(40, dim))
+    clean, qkv = s.qkv.cuda(), s.qkv.cuda()
+    _, k, v = s.split(qkv)
+    k[0, 1, dim - 1] = value
+    v[4, 0, 2] = value
+    k[2, 0] = value
+    v[2, 1] = value
+    got = []
+    for t in (clean, qkv):
+        pools = s.pools("cuda")
+        keep = s.table.cuda(), s.starts.cuda(), s.kv_len.cuda()
+        q, nk, nv = s.split(t)
+        out = torch.empty((s.tokens, 2, dim), dtype=BF16, device="cuda")
+        errors = torch.zeros(1, dtype=torch.int32, device="cuda")
+        req = B.make_requests(*keep, tokens=s.tokens, max_new=3, max_len=40)
+        B.qail_kv_append(B.make_kv_cache(*pools), req, nk, nv, q=q, q_out=out, cos=cos, sin=sin, errors=errors)
+        torch.cuda.synchronize()
+        assert errors.item() == 0
+        got.append([p.cpu() for p in pools])
+    bad = torch.zeros((2,) + got[0][2].shape, dtype=torch.bool)    # of keys and of values: [page, head, slot]
+    at = [(int(s.table[r, p // 16]), p % 16) for r, p in P.positions(s)]
+    for which, token, head in ((0, 0, 1), (1, 4, 0), (0, 2, 0), (1, 2, 1)):
+        bad[which, at[token][0], head, at[token][1]] = True
+    for which in range(2):
+        codes, step = got[1][which], got[1][2 + which]
+        assert bool(torch.isnan(step[bad[which]]).all())
+        assert torch.equal(codes[~bad[which]], got[0][which][~bad[which]])
+        assert torch.equal(step[~bad[which]].view(torch.int32), got[0][2 + which][~bad[which]].view(torch.int32))
