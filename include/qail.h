@@ -413,7 +413,7 @@ int qail_qbc_loss(const float* logits_q, const float* logits_fp, int32_t B, int3
  *     y[m][k] = bf16(h[m][k] * r[m] * weight[k])
  * and, for 8-bit linears, codes with one step per row:
  *     u = h * weight                                 fp32, one rounding
- *     s = max_k |u[m][k]| / 127                      fp32, correctly rounded; 1 for an all-zero row
+ *     s = max_k |u[m][k]| / 127                      fp32, correctly rounded; 1 for an all-zero row, NaN where a u is not finite
  *     q[m][k] = clamp(rint(u / s), -127, 127);       y_scale[m] = s * r[m]
  * so q * y_scale stands for y; r is in the scale alone and decides no code.  Codes are packed as by qail_quantize_act_s8:
  * a row is the a_s8 of a qail_w8a8_gemm with H = W = 1, whose int32 sums are scaled by y_scale[m] and the weight's scale.

@@ -27,14 +27,14 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
                  f32x2_to_bf16x2_rne(f[6], f[7])};
 }
 
-// Sum of a and maximum (or sum) of b over the kGroup threads that share a row; every thread gets them.
+// Sum of a and maximum (of magnitudes) or sum of b over the kGroup threads that share a row; every thread gets them.
 template <int kGroup, bool kMax>
 __device__ __forceinline__ void row_reduce(float& a, float& b, float2* red) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         a += __shfl_xor(a, o, kWave);
         const float c = __shfl_xor(b, o, kWave);
-        b = kMax ? fmaxf(b, c) : b + c;
+        b = kMax ? max_magnitude(b, c) : b + c;
     }
     if constexpr (kGroup > kWave) {
         constexpr int waves = kGroup / kWave;
@@ -44,7 +44,7 @@ __device__ __forceinline__ void row_reduce(float& a, float& b, float2* red) {
 #pragma unroll
         for (int w = 1; w < waves; ++w) {
             t.x += red[w].x;
-            t.y = kMax ? fmaxf(t.y, red[w].y) : t.y + red[w].y;
+            t.y = kMax ? max_magnitude(t.y, red[w].y) : t.y + red[w].y;
         }
         a = t.x;
         b = t.y;
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kGroup < 256 ? 256 : kGroup) void rmsnorm_kernel(co
         for (int e = 0; e < 8; ++e) {
             if (a.residual) h[u][e] += r[e];
             ss = fmaf(h[u][e], h[u][e], ss);
-            if constexpr (kEight) most = fmaxf(most, fabsf(h[u][e] * w[e]));
+            if constexpr (kEight) most = max_magnitude(most, fabsf(h[u][e] * w[e]));
         }
         const int i = t + u * kGroup;
         if (a.h_out && i < n8) reinterpret_cast<uint4*>(a.h_out)[base + i] = pack8(h[u]);
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kGroup < 256 ? 256 : kGroup) void rmsnorm_kernel(co
     row_reduce<kGroup, true>(ss, most, red);
     const float r = 1.0f / sqrtf(fmaf(ss, a.inv_k, a.eps));
     if constexpr (kEight) {
-        const float s = most > 0.f ? most / 127.0f : 1.0f;
+        const float s = step_of_codes(most);
         if (t == 0) a.y_scale[m] = s * r;
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {

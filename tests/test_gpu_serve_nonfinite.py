@@ -102,3 +102,28 @@ def test_a_head_that_is_not_finite_has_a_step_of_nan(B, dim, value):
         assert bool(torch.isnan(step[bad[which]]).all())
         assert torch.equal(codes[~bad[which]], got[0][which][~bad[which]])
         assert torch.equal(step[~bad[which]].view(torch.int32), got[0][2 + which][~bad[which]].view(torch.int32))
+
+
+# ------------------------------------------------------------------------------------ codes of a norm --
+
+@pytest.mark.parametrize("where", ["x", "residual", "weight"])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("K", [64, 1000, 2048, 4096, 16384])
+def test_codes_of_a_norm_of_what_is_not_finite(B, K, value, where):
+    """The scale of a row with an infinity or NaN is NaN (the weight's is in every row); other rows keep their bits."""
+    M = 5
+    x, res, w = P.normal((M, K), 1).to(BF16).cuda(), P.normal((M, K), 2).to(BF16).cuda(), (1 + P.normal((K,), 3, 0.2)).to(BF16).cuda()
+    got = []
+    for poisoned in (False, True):
+        if poisoned:
+            if where == "weight":
+                w[K - 3] = value
+            else:
+                (x if where == "x" else res)[3, K - 3] = value
+        codes, scale = torch.empty((M, K), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+        B.qail_rmsnorm(x, w, 1e-5, residual=res, y_s8=codes, y_scale=scale)
+        got.append((codes.cpu(), scale.cpu()))
+    rows = torch.full((M,), where == "weight")
+    rows[3] = True
+    assert bool(torch.isnan(got[1][1][rows]).all())
+    assert torch.equal(got[1][0][~rows], got[0][0][~rows]) and torch.equal(got[1][1][~rows], got[0][1][~rows])
