@@ -6,9 +6,7 @@
 // chosen by the order in which rows of K enter the first product, which is free.
 //
 // Rows of one request and one head of the cache: row i is token i / group, head i % group, so grouped heads share every key that is loaded.
-#include <algorithm>
-
-#include "kv_cache.h"
+#include "attention_plan.h"
 
 namespace qail {
 
@@ -145,8 +143,6 @@ __device__ __forceinline__ void store_row_alone(const AttentionArgs& a, const fl
 // 500 to 8000 8-bit keys, 32 heads to 8: 589 MB in 128 us, 4.6 TB/s; one of 295 bf16 keys 7 us, which are trips to memory.
 constexpr int kStreamWaves = 4, kStreamKeys = 32;   // a step (kStepKeys) is a tile of keys for each wave
 static_assert(kStreamWaves * kStreamKeys == kStepKeys, "a step is a tile of keys for each wave");
-
-constexpr int stream_blocks(int head_dim) { return head_dim == 64 ? 3 : 2; }   // that a compute unit holds: by registers
 
 template <int D, bool kEight>
 struct Stream {
@@ -521,7 +517,8 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
 // scalars, but for the last 64 keys.  Four prompts to 2500 tokens (111 GFLOP) take 160 us, 690 TFLOP/s, three chunks behind 7000 to 13000 keys 760: the
 // matrix cores are busy 36 and 40 % of the time and the vector unit 41 and 39 %, next to each other for little of it; a quarter of a wave's time is waiting.
 // 32 keys at a time and three blocks a compute unit instead of two: prompts the same, chunks 171 -> 213.
-constexpr int kTileWaves = 4, kTileKeys = 64, kTileRows = kTileWaves * 32;
+constexpr int kTileWaves = 4;
+static_assert(kTileRows == kTileWaves * 32, "a wave takes 32 rows");
 
 template <int D, bool kEight>
 struct Tile {
@@ -865,50 +862,10 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const Att
         uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }
 
-// How a step is divided among blocks, by what the host knows: which kernels run (both where requests of few rows and of many may come
-// together) and how they share the keys.
-struct Plan {
-    bool stream, tiles;
-    int stream_rows;            // requests of up to so many rows are the stream's
-    int shared, blocks, least;  // the stream's
-    unsigned join_tokens;
-    int row_tiles, chunk, most; // the tiles'
-};
-
-Plan plan_for(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
-    Plan p{};
-    const int group = q_heads / c.heads, tile_rows = kTileRows;
-    const long long keys = std::max<long long>(1, std::min<long long>(b.max_len, (long long)b.max_pages * c.page_size));   // at most 2^30
-    const long long most_rows = (long long)std::min(b.max_new, b.tokens) * group, cus = device_cu_count();
-    p.stream = most_rows <= kStreamRows;
-    p.tiles = !p.stream;
-    if (p.tiles && b.requests > 1 && (long long)b.requests * b.max_new != b.tokens && group <= kStreamRows) p.stream = true;
-    p.stream_rows = p.tiles ? (p.stream ? kStreamRows : 0) : INT32_MAX;
-    if (p.stream) {
-        // Shared steps cost a join, about 4 us together with what the kernel does for it; a block for each request and head costs the time of the
-        // longest one, 1.6 us per step.  us, one / shared, uniform lengths: 32 units, 512 keys 8.9 / 10.9, 1024 keys 14.5 / 12, 16384 keys 224 / 49;
-        // 256 units, 2048 keys 31 / 33, 4096 keys 66 / 55; 512 units, 1024 keys 26 / 31, 8192 keys 192 / 203, but of 500 to 8000
-        // keys 153 / 128.
-        const long long units = (long long)b.requests * c.heads;
-        p.shared = keys > std::min(2048ll, 512 + 6 * units);
-        p.blocks = p.shared ? (int)cus * stream_blocks(c.head_dim) : (int)units;
-        p.join_tokens = (unsigned)std::max(1, std::min({b.max_new, b.tokens, kStreamRows}));
-        p.least = 2;   // of 1, 2, 3 and 4 the best or next to it from 1024 to 16384 keys
-    }
-    if (p.tiles) {
-        p.row_tiles = (int)((long long)b.tokens * group / tile_rows) + b.requests;
-        const long long work = std::max(1ll, (long long)b.tokens * group / tile_rows) * c.heads;
-        const long long n = std::max(1ll, std::min({(2 * cus + work - 1) / work, 64ll, (keys + 511) / 512}));
-        p.most = (int)n;
-        p.chunk = (int)((keys + n - 1) / n + kTileKeys - 1) / kTileKeys * kTileKeys;
-    }
-    return p;
-}
-
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <int D, bool kEight>
-hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_requests& b, const AttentionArgs& a, hipStream_t st) {
+hipError_t launch_step(const AttentionPlan& p, const qail_kv_cache& c, const qail_requests& b, const AttentionArgs& a, hipStream_t st) {
     const unsigned head_blocks = (unsigned)((a.q_heads + kJoinWaves - 1) / kJoinWaves);
     if (p.tiles) {   // the longer kernel first
         hipLaunchKernelGGL((attend_tile_kernel<D, kEight>), dim3((unsigned)((long long)p.row_tiles * c.heads * p.most)), dim3(kTileWaves * kWave), 0, st, a);
@@ -921,28 +878,22 @@ hipError_t launch_step(const Plan& p, const qail_kv_cache& c, const qail_request
     return hipGetLastError();
 }
 
-// Partial results that a call may leave.
-size_t places(const Plan& p, const qail_requests& b, int q_heads) {
-    const size_t stream = p.stream && p.shared ? (size_t)2 * p.blocks * kStreamRows : 0, tiles = p.tiles && p.most > 1 ? (size_t)b.tokens * q_heads * p.most : 0;
-    return std::max(stream, tiles);
-}
-
 }  // namespace
 
 size_t paged_attention_workspace(const qail_kv_cache& c, const qail_requests& b, int q_heads) {
-    const size_t n = places(plan_for(c, b, q_heads), b, q_heads);
+    const size_t n = attention_places(plan_attention(c, b, q_heads, device_cu_count()), b, q_heads);
     return align256(n * c.head_dim * sizeof(float)) + align256(n * sizeof(float2));
 }
 
 hipError_t launch_paged_attention(const qail_kv_cache& c, const qail_requests& b, const uint16_t* q, int64_t q_stride, int q_heads, float scale,
                                   uint16_t* out, uint32_t* errors, void* ws, hipStream_t st) {
-    const Plan p = plan_for(c, b, q_heads);
+    const AttentionPlan p = plan_attention(c, b, q_heads, device_cu_count());
     AttentionArgs a{};
     a.c = cache_args(c, b, errors);
     a.q = q;
     a.out = out;
     a.part_o = static_cast<float*>(ws);
-    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(places(p, b, q_heads) * c.head_dim * sizeof(float)));
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(attention_places(p, b, q_heads) * c.head_dim * sizeof(float)));
     a.q_stride = q_stride;
     a.scale = scale * 1.44269504088896340736f;
     a.q_heads = q_heads;
