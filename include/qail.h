@@ -475,9 +475,10 @@ typedef struct {
 } qail_requests;
 
 /* `errors` (device, one uint32, may be NULL; not cleared) of the two calls below is incremented at least once if the contents of the
- * three arrays are bad: a page outside 0 .. num_pages - 1 for a token in use, a kv_len beyond max_pages * page_size, a q_start that descends
- * or leaves 0 .. tokens, for qail_kv_append a negative position or one beyond `positions`.  Nothing outside the given
- * buffers is read or written then; the outputs of the requests concerned are unspecified. */
+ * three arrays are bad: a page outside 0 .. num_pages - 1 for a token that the call reads or writes, a kv_len that is negative or beyond
+ * max_pages * page_size (of a request that waits as well), a q_start that descends or leaves 0 .. tokens, for qail_kv_append a negative position
+ * or one beyond `positions`.  Nothing outside the given buffers is read or written then; the outputs of the requests concerned are unspecified.
+ * A step of zero tokens launches nothing and looks at nothing. */
 
 /* Rotates the new tokens' keys and queries and writes keys and values to their slots.  With half = head_dim / 2, position p, i < half,
  * each product and sum one fp32 operation (no fused multiply-add):

@@ -33,8 +33,9 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
                  f32x2_to_bf16x2_rne(f[6], f[7])};
 }
 
+// A block's heads of a token.
 template <int D, bool kEight>
-__global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
+__device__ __forceinline__ void append_token(const AppendArgs& a) {
     constexpr int kLanes = D / 16, kHalf = D / 2;
     const int t = blockIdx.x, H = a.c.heads;
     const int unit = blockIdx.y * (256 / kLanes) + threadIdx.x / kLanes;   // head: keys, values, then queries
@@ -105,6 +106,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
         *reinterpret_cast<uint4*>(out + i) = pack8(x);
         *reinterpret_cast<uint4*>(out + kHalf + i) = pack8(y);
     }
+}
+
+template <int D, bool kEight>
+__global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a) {
+    append_token<D, kEight>(a);
+    if (blockIdx.x == 0 && blockIdx.y == 0) report_rows(a.c);   // at the end: after an atomic the arrays' loads are no scalar ones (55 -> 65 us at 5512 tokens)
 }
 
 }  // namespace
