@@ -206,6 +206,10 @@ __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& 
             th[jt] = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
             tl[jt] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
         }
+        auto b_of = [&](int n0, int t, int jt) {
+            const int row = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
+            return 32 * jt + 8 * g < r ? *reinterpret_cast<const u32x4_t*>(it.B + ((size_t)of * N + row) * r + 32 * jt + 8 * g) : u32x4_t{0u, 0u, 0u, 0u};
+        };
         for (int n0 = n_begin, c = 0; c < a.chunks && n0 < N; ++c, n0 += 64) {
             const int n = n0 + 16 * g;
             uint16_t* const y = it.y + (size_t)min(m, M - 1) * N + n;
@@ -222,15 +226,27 @@ __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& 
             for (int jt = 0; jt < kParts; ++jt) {
                 u32x4_t bv[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int row = min(n0 + col / 4 * 16 + 4 * t + col % 4, N - 1);
-                    bv[t] = 32 * jt + 8 * g < r ? *reinterpret_cast<const u32x4_t*>(it.B + ((size_t)of * N + row) * r + 32 * jt + 8 * g) : u32x4_t{0u, 0u, 0u, 0u};
-                }
+                for (int t = 0; t < 4; ++t) bv[t] = b_of(n0, t, jt);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const bf16x8_t b = __builtin_bit_cast(bf16x8_t, bv[t]);
                     acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, tl[jt], acc[t], 0, 0, 0);
                     acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, th[jt], acc[t], 0, 0, 0);
+                }
+            }
+            float odd = 0.f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd = fmaf(acc[t][e], 0.f, odd);
+            if (__builtin_expect(__any(mine && odd != 0.f), 0)) {   // NaN: an infinity of t or B is right times t's upper part; its product with the lower one is NaN or of either sign
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    f32x4_t high = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int jt = 0; jt < kParts; ++jt) high = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b_of(n0, t, jt)), th[jt], high, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][e] = fabsf(acc[t][e]) < INFINITY ? acc[t][e] : high[e];
                 }
             }
             if (!mine || n >= N) continue;

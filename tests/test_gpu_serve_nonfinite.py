@@ -7,7 +7,7 @@ import torch
 
 from tests import serve_reference as P
 from tests.helpers import ensure_built
-from tests.test_gpu_serve import attention, within
+from tests.test_gpu_serve import adapter_case, adapter_part, attention, linears, run_adapters, within
 
 pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
@@ -127,3 +127,43 @@ def test_codes_of_a_norm_of_what_is_not_finite(B, K, value, where):
     rows[3] = True
     assert bool(torch.isnan(got[1][1][rows]).all())
     assert torch.equal(got[1][0][~rows], got[0][0][~rows]) and torch.equal(got[1][1][~rows], got[0][1][~rows])
+
+
+# ----------------------------------------------------------------------------------------- adapters --
+
+@pytest.mark.parametrize("shapes,M,n,r", [([(256, 512, 128)], 3, 3, 8), ([(520, 1024, 128), (33, 512, 64)], 20, 2, 16), ([(96, 512, 128)], 100, 4, 64),
+                                          ([(129, 256, 128), (64, 2048, 128)], 350, 3, 40)])
+def test_infinities_of_an_adapter_are_what_the_products_say(B, shapes, M, n, r):
+    """A down-projection beyond fp32, and infinities among B's values: y is infinite with the sign of their product; what they do not reach stays."""
+    items = adapter_case(shapes, M, n, r, 120, zero_weights=True)
+    rows = [i % (n + 1) - 1 for i in range(M)]
+    device_rows = torch.tensor(rows, dtype=torch.int32, device="cuda")
+    row = rows.index(1)
+    for kind in ("t", "B"):
+        for e in items:
+            if kind == "t":    # t[row][2] = 1e25 * 1e25 and what is finite beside it; every other t is finite
+                e["A"][:, :, 7] = 0
+                e["A"][1, 2, 7] = 1e25
+                e["x"][:, 7] = 0
+                e["x"][row, 7] = 1e25
+            else:
+                e["A"][1, 2, 7] = 0
+                e["x"][row, 7] = 0
+                e["B"][1, 1::3, 4] = math.inf
+                e["B"][1, 2::3, 4] = -math.inf
+        base = linears(B, items, M)
+        run_adapters(B, items, device_rows, M)
+        for e, linear in zip(items, base):
+            y = e["y"].double().cpu()
+            part, tol = adapter_part(dict(e, B=torch.where(torch.isfinite(e["B"]), e["B"], 0), x=torch.where(e["x"].float().abs() < 1e20, e["x"], 0)), rows)
+            want = linear.double().cpu() + part
+            if kind == "t":
+                want[row] = e["B"][1, :, 2].double().cpu() * math.inf
+            else:
+                t = e["x"].double().cpu() @ e["A"][1, 4].double().cpu()
+                for m in [i for i, a in enumerate(rows) if a == 1]:
+                    want[m, 1::3] = t[m] * math.inf
+                    want[m, 2::3] = -t[m] * math.inf
+            inf = torch.isinf(want)
+            assert not torch.isnan(want).any() and torch.equal(y[inf], want[inf]), kind
+            assert bool(((y - want).abs() <= 2 ** -8 * want.abs() + tol * (1 + 2 ** -7))[~inf].all()), kind
