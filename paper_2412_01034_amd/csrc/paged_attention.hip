@@ -48,8 +48,8 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t lo, uint32_t hi) {
 }
 
 // One row by one wave, which reads no key behind the row's last: keys k0 .. last of request r and head h.  The products on the matrix cores
-// multiply the values of keys that a row does not see by a p of zero, and zero times an infinity or NaN is NaN: where that may have
-// happened (a result that is not finite, of a row that has not seen all keys of its tile) the row is computed again, here.
+// multiply by a p of zero the values of keys that a row does not see, and the last key's in every place behind it; zero times an infinity or NaN is
+// NaN: where that may have happened (a result that is not finite, of a row whose sum is) the row is computed again, here.
 // A lane takes a key of 64 for the scores, then D / 64 values of every key.  o, m and l as in the kernels: not yet divided by l.
 template <int D, bool kEight>
 __device__ __forceinline__ void attend_row_alone(const AttentionArgs& a, int r, int h, const uint16_t* q, int k0, int last, float* o, float& m, float& l) {
@@ -332,13 +332,10 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
         }
         // where a row's result goes, and whether that is a partial one
         auto out_of = [&](int row) { return (size_t)(rq.start + (row0 + row) / a.group) * a.q_heads + h * a.group + (row0 + row) % a.group; };
-        unsigned long long left = 0;
-        if (__builtin_expect(before + row0 / a.group < k1 - 1, 0)) {   // there are keys that a row does not see; its own scores are no NaN
-            if (i < n && before + (row0 + i) / a.group < k1 - 1 && sum == sum)
+        if (i < n && sum == sum)   // its own scores are no NaN
 #pragma unroll
-                for (int e = 0; e < 8; ++e) odd = fmaf(acc[e], 0.f, odd);
-            left = __ballot(odd != 0.f);   // NaN
-        }
+            for (int e = 0; e < 8; ++e) odd = fmaf(acc[e], 0.f, odd);
+        unsigned long long left = __ballot(odd != 0.f);   // NaN
         const bool again = (left >> (lane / kLanesO * kLanesO)) & ((1ull << kLanesO) - 1);
         if (i < n && !again) {
             if (place < 0) {
@@ -789,7 +786,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
     const float sum = l + __shfl_xor(l, 32, kWave);
     const size_t at = (size_t)(rq.start + token) * a.q_heads + h * a.group + row % a.group;
     float odd = 0.f;
-    if (row < rows && lim < k1 - 1 && sum == sum)   // there are keys that the row does not see; its own scores are no NaN
+    if (row < rows && sum == sum)   // its own scores are no NaN
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll

@@ -67,6 +67,43 @@ def test_nan_of_all_keys_of_a_share(B, new, lens, heads, kv_heads, dim, page, fi
     nan_rows(B, s, poison, rows)
 
 
+# ---------------------------------------------------------------------------- values that are infinite --
+
+# lengths that end inside a tile of keys and at its end, few rows and many, undivided and divided
+LAST = [([1], [90], 4, 2, 128, 32), ([1], [96], 4, 2, 128, 32), ([5], [91], 2, 1, 64, 16), ([1, 1], [3001, 2999], 8, 8, 64, 64), ([70], [70], 2, 1, 128, 16),
+        ([64], [128], 2, 1, 128, 16), ([40], [2601], 8, 2, 128, 64), ([100, 3], [2100, 1501], 8, 8, 64, 256)]
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page", LAST)
+def test_an_infinite_value_is_infinite_for_those_who_see_it(B, new, lens, heads, kv_heads, dim, page, eight, value):
+    """In each request's last token's value: the rows of that token alone see it, however many slots of a tile lie behind it."""
+    s = P.Step(new, lens, heads, kv_heads, dim, page, eight, 2300 + lens[0], pad=8)
+    scale = 1 / math.sqrt(dim)
+    for r in range(len(new)):
+        v = s.values[r][1]
+        if eight:
+            v[0][:, -1] = torch.where(v[0][:, -1] == 0, 1, v[0][:, -1])    # zero times an infinity is NaN
+    want, tol = P.attend(s, scale)
+    sees = torch.zeros((s.tokens, heads, dim), dtype=torch.bool)
+    for r in range(len(new)):
+        row = int(s.starts[r + 1]) - 1
+        if eight:
+            v = s.values[r][1]
+            v[1][:, -1] = abs(value)
+            want[row] = (v[0][:, -1].double() * math.inf).repeat_interleave(heads // kv_heads, 0)
+            sees[row] = True
+        else:
+            s.values[r][1][:, -1, 7] = value
+            want[row, :, 7] = value
+            sees[row, :, 7] = True
+    out = attention(B, s, scale).double().cpu()
+    assert torch.equal(out[sees], want[sees])
+    if not sees.all():
+        within(out[~sees], want[~sees], tol[~sees])
+
+
 # -------------------------------------------------------------------------------- a cache of bytes --
 
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
