@@ -118,17 +118,17 @@ __device__ __forceinline__ void attend_row_alone(const AttentionArgs& a, int r, 
     }
 }
 
-// 1 / l; no key: a factor of 0, the row is zeros.
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; }
+// 1 / l for a row at position `pos`.  A row that sees no key is zeros; one whose keys all have a score of minus infinity has no largest: NaN.
+__device__ __forceinline__ float inverse(float l, int pos) { return l > 0.f ? 1.0f / l : l == 0.f && pos < 0 ? 0.f : __builtin_nanf(""); }
 
 // That row's result to `out`, or to place `at` of the partial ones where there is one.
 template <int D>
-__device__ __forceinline__ void store_row_alone(const AttentionArgs& a, const float* o, float m, float l, uint16_t* out, long long at) {
+__device__ __forceinline__ void store_row_alone(const AttentionArgs& a, const float* o, float m, float l, int pos, uint16_t* out, long long at) {
     constexpr int kPer = D / kWave;
     const int lane = threadIdx.x % kWave;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        if (at < 0) out[lane * kPer + e] = (uint16_t)f32x2_to_bf16x2_rne(o[e] * inverse(l), 0.f);
+        if (at < 0) out[lane * kPer + e] = (uint16_t)f32x2_to_bf16x2_rne(o[e] * inverse(l, pos), 0.f);
         else a.part_o[at * D + lane * kPer + e] = o[e];
     }
     if (at >= 0 && lane == 0) a.part_ml[at] = make_float2(m, l);
@@ -339,7 +339,7 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
         const bool again = (left >> (lane / kLanesO * kLanesO)) & ((1ull << kLanesO) - 1);
         if (i < n && !again) {
             if (place < 0) {
-                const float inv = inverse(sum);
+                const float inv = inverse(sum, before + (row0 + i) / a.group);
                 u32x4_t w;
                 w.x = f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv);
                 w.y = f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv);
@@ -359,7 +359,7 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
             left &= ~(((1ull << kLanesO) - 1) << (which * kLanesO));
             float again_o[D / kWave], again_m, again_l;
             attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + token) * a.q_stride + (h * a.group + (row0 + row) % a.group) * D, k0, before + token, again_o, again_m, again_l);
-            store_row_alone<D>(a, again_o, again_m, again_l, a.out + out_of(row) * D, place < 0 ? -1 : place * kStreamRows + row);
+            store_row_alone<D>(a, again_o, again_m, again_l, before + token, a.out + out_of(row) * D, place < 0 ? -1 : place * kStreamRows + row);
         }
         __syncthreads();
     }
@@ -440,9 +440,9 @@ __global__ __launch_bounds__(kStreamWaves* kWave, stream_blocks(D)) void attend_
 // Adds up what the stream's blocks have left: a wave per output row.
 constexpr int kJoinWaves = 4;
 
-// The sum of `count` partial results, the i-th in place(i), as bf16 to `out`.
+// The sum of `count` partial results of a row at position `pos`, the i-th in place(i), as bf16 to `out`.
 template <int D, typename F>
-__device__ __forceinline__ void join_row(const AttentionArgs& a, long long count, uint16_t* out, F place) {
+__device__ __forceinline__ void join_row(const AttentionArgs& a, long long count, int pos, uint16_t* out, F place) {
     const int lane = threadIdx.x % kWave;
     float top = -INFINITY;
     for (long long i = lane; i < count; i += kWave) top = fmaxf(top, a.part_ml[place(i)].x);
@@ -475,7 +475,7 @@ __device__ __forceinline__ void join_row(const AttentionArgs& a, long long count
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
     }
-    const float inv = inverse(sum);
+    const float inv = inverse(sum, pos);
     if (lane < kLanes) reinterpret_cast<uint2*>(out)[lane] = uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }
 
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
         const long long begin = first + ((long long)(head / a.group) * s.tiles + row / kStreamRows) * s.steps;
         const long long b0 = begin / share, count = (begin + s.steps - 1) / share - b0 + 1;
         if (count == 1) continue;
-        join_row<D>(a, count, a.out + ((size_t)(rq.start + token) * a.q_heads + head) * D,
+        join_row<D>(a, count, rq.len - rq.n + token, a.out + ((size_t)(rq.start + token) * a.q_heads + head) * D,
                     [&](long long i) { return place_of(begin, b0 + i, share) * kStreamRows + row % kStreamRows; });
     }
 }
@@ -795,7 +795,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
     unsigned left = (unsigned)__ballot(odd != 0.f);   // NaN
     if (row < rows && !((left >> col) & 1)) {
         if (count == 1) {
-            const float inv = inverse(sum);
+            const float inv = inverse(sum, before + token);
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -817,7 +817,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
         const size_t to = (size_t)(rq.start + new_token) * a.q_heads + head;
         float again_o[D / kWave], again_m, again_l;
         attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + new_token) * a.q_stride + head * D, range.begin, min(before + new_token, k1 - 1), again_o, again_m, again_l);
-        store_row_alone<D>(a, again_o, again_m, again_l, a.out + to * D, count == 1 ? -1 : (long long)(to * a.most + split));
+        store_row_alone<D>(a, again_o, again_m, again_l, before + new_token, a.out + to * D, count == 1 ? -1 : (long long)(to * a.most + split));
     }
 }
 
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_tiles_kernel(const Att
             acc += v[u] * w;
         }
     }
-    const float inv = inverse(sum);
+    const float inv = inverse(sum, rq.len - rq.n + token);
     reinterpret_cast<uint2*>(a.out + at * D)[threadIdx.x % kLanes] =
         uint2{f32x2_to_bf16x2_rne(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2_rne(acc[2] * inv, acc[3] * inv)};
 }

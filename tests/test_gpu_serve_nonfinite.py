@@ -104,6 +104,33 @@ def test_an_infinite_value_is_infinite_for_those_who_see_it(B, new, lens, heads,
         within(out[~sees], want[~sees], tol[~sees])
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page", LAST + [([1], [1], 1, 1, 64, 16), ([200], [150], 4, 4, 128, 64)])
+def test_scores_of_minus_infinity_alone_are_nan(B, new, lens, heads, kv_heads, dim, page, eight):
+    """A row whose keys all have a score of minus infinity has no largest one, unlike a row without keys, which is zeros."""
+    s = P.Step(new, lens, heads, kv_heads, dim, page, eight, 2400 + lens[0], pad=8)
+    scale = 1 / math.sqrt(dim)
+    want, tol = P.attend(s, scale)
+    q, _, _ = s.split(s.qkv)
+    q[:, 0] = q[:, 0].abs() + 1    # the first head's scores of keys below zero are below zero
+    k = s.values[0][0]
+    if eight:
+        k[0][0] = -1
+        k[1][0] = math.inf
+    else:
+        k[0] = -math.inf
+    rows = torch.zeros((s.tokens, heads), dtype=torch.bool)
+    rows[max(0, new[0] - lens[0]):new[0], 0] = True
+    others = torch.ones_like(rows)
+    others[:, 0] = False                                   # its queries are others
+    others[:new[0], :heads // kv_heads] = False            # these read the same keys
+    out = attention(B, s, scale).cpu()
+    assert bool(torch.isnan(out[rows]).all())
+    if others.any():
+        within(out[others], want[others], tol[others])
+    assert not out[:max(0, new[0] - lens[0]), 0].any()
+
+
 # -------------------------------------------------------------------------------- a cache of bytes --
 
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
