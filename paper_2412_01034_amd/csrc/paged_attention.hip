@@ -358,7 +358,7 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
             const int which = __builtin_ctzll(left) / kLanesO, row = wave * (kWave / kLanesO) + which, token = (row0 + row) / a.group;
             left &= ~(((1ull << kLanesO) - 1) << (which * kLanesO));
             float again_o[D / kWave], again_m, again_l;
-            attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + token) * a.q_stride + (h * a.group + (row0 + row) % a.group) * D, k0, before + token, again_o, again_m, again_l);
+            attend_row_alone<D, kEight>(a, r, h, a.q + (rq.start + token) * a.q_stride + (h * a.group + (row0 + row) % a.group) * D, k0, min(before + token, k1 - 1), again_o, again_m, again_l);
             store_row_alone<D>(a, again_o, again_m, again_l, before + token, a.out + out_of(row) * D, place < 0 ? -1 : place * kStreamRows + row);
         }
         __syncthreads();

@@ -104,6 +104,23 @@ def test_an_infinite_value_is_infinite_for_those_who_see_it(B, new, lens, heads,
         within(out[~sees], want[~sees], tol[~sees])
 
 
+@pytest.mark.parametrize("first", [0, 0.3, 0.6])
+@pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page", LAST)
+def test_an_infinite_value_of_a_key_in_front(B, new, lens, heads, kv_heads, dim, page, first):
+    """One value of one key of each request, at the beginning or further on: infinite in the rows that see it, which are right beside it."""
+    s = P.Step(new, lens, heads, kv_heads, dim, page, False, 2500 + lens[0], pad=8)
+    scale = 1 / math.sqrt(dim)
+    want, tol = P.attend(s, scale)
+    sees = torch.zeros((s.tokens, heads, dim), dtype=torch.bool)
+    for r, (n, length) in enumerate(zip(new, lens)):
+        key = int(first * length)
+        s.values[r][1][:, key, 5] = math.inf
+        sees[int(s.starts[r]) + max(0, key - (length - n)):int(s.starts[r + 1]), :, 5] = True
+    out = attention(B, s, scale).double().cpu()
+    assert bool((out[sees] == math.inf).all())
+    within(out[~sees], want[~sees], tol[~sees])
+
+
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("new,lens,heads,kv_heads,dim,page", LAST + [([1], [1], 1, 1, 64, 16), ([200], [150], 4, 4, 128, 64)])
 def test_scores_of_minus_infinity_alone_are_nan(B, new, lens, heads, kv_heads, dim, page, eight):
