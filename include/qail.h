@@ -495,8 +495,9 @@ int qail_kv_append(const qail_kv_cache* c, const qail_requests* b, const uint16_
 
 /* Causal attention of the new tokens over their requests' cache, which holds their own keys and values already:
  *     out[t][a] = sum_j p_j v[j],  p = softmax_j(scale * q[t][a] . k[j]),  j = 0 .. position of t, head a / (q_heads / heads) of the cache
- * (q_heads is a multiple of the cache's heads).  A chunk may be one token, a few, or a whole prompt.  Scores, maxima and sums are fp32; p is
- * rounded to bf16 for its product with v (one that is below 2^-126 of its row's largest may count as zero).  A token whose position is negative (more new tokens than kv_len) sees no key: its
+ * (q_heads is a multiple of the cache's heads).  A chunk may be one token, a few, or a whole prompt.  Scores, maxima and sums are fp32.  For its
+ * product with v, p is held to 2^-16 of it where a request has at most 16 rows (new tokens times q_heads / heads) and rounded to bf16 where it has
+ * more; one that is below 2^-126 of its row's largest may count as zero.  A token whose position is negative (more new tokens than kv_len) sees no key: its
  * rows are zero; one whose scores are all minus infinity is NaN.  The sum of p_j v[j] is formed before it is divided by the sum of p, and overflows
  * where it passes fp32's range.  Slots behind a request's last token may hold anything; what a token does not see, infinities and NaN of later tokens
  * included, does not reach its rows.

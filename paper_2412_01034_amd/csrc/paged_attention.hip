@@ -270,7 +270,9 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
                 for (int d = 0; d < D / 16; ++d) o[d] *= alpha;
                 m = m_new;
             }
-            uint32_t pw[4];
+            // p in two parts, each rounded to bf16: 2^-17 of it is lost instead of 2^-9, for 8 more products of 32 keys beside a stream of bytes (attend_one
+            // 7.0 -> 7.2 us, 64 requests of 8-bit keys 129 -> 133)
+            uint32_t ph[4], pl[4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.scale, -off));
@@ -278,8 +280,11 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
                 if constexpr (kEight) p[i] *= vs[i];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pw[i] = f32x2_to_bf16x2_rne(p[2 * i], p[2 * i + 1]);
-            const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[0], pw[1], pw[2], pw[3]});
+            for (int i = 0; i < 4; ++i) {
+                ph[i] = f32x2_to_bf16x2_rne(p[2 * i], p[2 * i + 1]);
+                pl[i] = f32x2_to_bf16x2_rne(p[2 * i] - __builtin_bit_cast(float, ph[i] << 16), p[2 * i + 1] - __builtin_bit_cast(float, ph[i] & 0xFFFF0000u));
+            }
+            const bf16x8_t upper = as_bf16x8(u32x4_t{ph[0], ph[1], ph[2], ph[3]}), lower = as_bf16x8(u32x4_t{pl[0], pl[1], pl[2], pl[3]});
             if (more) {
                 if constexpr (kEight) load_steps(kt + kStride);
                 entries(kt + 2 * kStride);
@@ -303,7 +308,8 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
                     const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
                     vf = __builtin_bit_cast(bf16x8_t, both);
                 }
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, upper, o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lower, o[d], 0, 0, 0);
             }
         }
         l += __shfl_xor(l, 16, kWave);
@@ -718,6 +724,8 @@ __global__ __launch_bounds__(kTileWaves* kWave, 2) void attend_tile_kernel(const
         bf16x8_t pf[4];
 #pragma unroll
         for (int st = 0; st < 4; ++st) {
+            // p is rounded to bf16 once: in two parts, as with few rows, the error against 64 bits would be 0.0016 of the result's norm instead of 0.0021 (prompts) and
+            // 0.0024 (chunks), and the kernel takes 161 -> 195 us and 168 -> 210.  Without steps the sum is fp32 of the rounded p, so that weights add up to one.
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
