@@ -90,7 +90,7 @@ __device__ __forceinline__ void append_token(const AppendArgs& a) {
         for (int e = 0; e < 8; ++e) most = max_magnitude(most, max_magnitude(fabsf(x[e]), fabsf(y[e])));
 #pragma unroll
         for (int o = kLanes / 2; o >= 1; o >>= 1) most = max_magnitude(most, __shfl_xor(most, o, kWave));
-        const float s = step_of_codes(most);
+        const float s = most > 0.f ? most / 127.0f : 1.0f;
         auto codes = [&](const float* f) {
             uint32_t w[2] = {0u, 0u};
 #pragma unroll
@@ -100,7 +100,7 @@ __device__ __forceinline__ void append_token(const AppendArgs& a) {
         uint8_t* out = static_cast<uint8_t*>(key ? a.c.k : a.c.v) + slot * D;
         *reinterpret_cast<uint2*>(out + i) = codes(x);
         *reinterpret_cast<uint2*>(out + kHalf + i) = codes(y);
-        if (i == 0) (key ? a.c.k_scale : a.c.v_scale)[slot] = s;
+        if (i == 0) (key ? a.c.k_scale : a.c.v_scale)[slot] = most < INFINITY ? s : __builtin_nanf("");   // no code could say that a value is not finite
     } else {
         uint16_t* out = static_cast<uint16_t*>(key ? a.c.k : a.c.v) + slot * D;
         *reinterpret_cast<uint4*>(out + i) = pack8(x);

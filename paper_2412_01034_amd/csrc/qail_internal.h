@@ -47,11 +47,6 @@ __device__ __forceinline__ float max_magnitude(float a, float b) {
     return __builtin_bit_cast(float, x > y ? x : y);
 }
 
-// The step of signed 8-bit codes of values whose largest magnitude is `most`; NaN where one is not finite: no code could say so.
-__device__ __forceinline__ float step_of_codes(float most) {
-    return !(most < INFINITY) ? __builtin_nanf("") : most > 0.f ? most / 127.0f : 1.0f;
-}
-
 // Launchers (host side).  Each validates nothing: the C entry points do.
 hipError_t launch_quantize_asym(const qail_wdesc& d, const float* w, uint32_t* qw, uint16_t* scales,
                                 uint32_t* zeros, uint32_t* range_errors, hipStream_t st);

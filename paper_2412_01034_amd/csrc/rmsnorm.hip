@@ -101,8 +101,8 @@ __global__ __launch_bounds__(kGroup < 256 ? 256 : kGroup) void rmsnorm_kernel(co
     row_reduce<kGroup, true>(ss, most, red);
     const float r = 1.0f / sqrtf(fmaf(ss, a.inv_k, a.eps));
     if constexpr (kEight) {
-        const float s = step_of_codes(most);
-        if (t == 0) a.y_scale[m] = s * r;
+        const float s = most > 0.f ? most / 127.0f : 1.0f;
+        if (t == 0) a.y_scale[m] = most < INFINITY ? s * r : __builtin_nanf("");   // no code could say that a u is not finite
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
             const int i = t + u * kGroup;

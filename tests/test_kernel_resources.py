@@ -47,3 +47,14 @@ def test_medium_batch_kernels_use_no_scratch():
     found = {k[".name"]: (k[".private_segment_fixed_size"], k[".vgpr_spill_count"]) for k in kernels(ensure_built().LIB_PATH) if "midm_kernel" in k[".name"]}
     assert len(found) == 11   # nibbles in groups of 128 and bytes with one to four blocks of 16 rows, groups of 64 with up to three
     assert set(found.values()) == {(0, 0)}, found
+
+
+def test_serving_kernels_use_no_scratch():
+    """A row of a norm, a tile's results and its operands lie in registers.  The exception is the norm's gradient beyond 8192 columns: 1024 threads with 128
+    registers each hold two or four pieces of the row, of the next one and of the weight's sums."""
+    names = ("rmsnorm", "kv_append", "attend_", "join_", "adapters_")
+    found = {k[".name"]: (k[".private_segment_fixed_size"], k[".vgpr_spill_count"]) for k in kernels(ensure_built().LIB_PATH) if any(n in k[".name"] for n in names)}
+    assert len(found) == 47, sorted(found)   # 14 and 6 + 1 of the norm, 4 of the writer, 4 + 4 and 2 + 2 of the attention, 4 + 4 + 2 of the adapters
+    wide = {n for n in found if "rmsnorm_back_kernelILi1024ELi2E" in n or "rmsnorm_back_kernelILi1024ELi4E" in n}
+    assert len(wide) == 2
+    assert {n: v for n, v in found.items() if n not in wide and v != (0, 0)} == {}
