@@ -47,6 +47,9 @@ inline AttentionPlan plan_attention(const qail_kv_cache& c, const qail_requests&
         // threads): tokens * q_heads / 128 + requests * heads is at most 2^23 + 2^22, and where keys are shared, `work` times `most` is below four blocks a unit.
         p.row_tiles = (int)((long long)b.tokens * group / kTileRows) + std::min(b.requests, b.tokens);
         const long long work = std::max(1ll, (long long)b.tokens * group / kTileRows) * c.heads;
+        // Shares until there are two blocks a unit, of 512 keys or more (us with 128 / 256 / 512 / 1024: one prompt of 1049, 4 heads to 1 22 / 19 / 20 / 23; 40 rows behind 2560
+        // keys, 8 to 2 21 / 19 / 21 / 28; 200 behind 12000, 8 to 1 54 / 54 / 38 / 37; two of 64 behind 4000 keys of 8 bits, 32 to 8 47 / 34 / 34 / 45), and 64 at most: the
+        // join reads them all (32 rows behind 40000 keys, 8 to 1, 48 with 64 and 61 with 256; behind 100000 67 and 123).
         const long long n = std::max(1ll, std::min({(2ll * cus + work - 1) / work, 64ll, (keys + 511) / 512}));
         p.most = (int)n;
         p.chunk = (int)((keys + n - 1) / n + kTileKeys - 1) / kTileKeys * kTileKeys;

@@ -241,6 +241,8 @@ __global__ __launch_bounds__(16 * kSlices) void rmsnorm_weight_kernel(const floa
     if (s == 0 && col < n4) reinterpret_cast<f32x4_t*>(dw)[col] = sum;
 }
 
+// Two blocks a unit: more have more rows on their way and leave more sums of the weight.  us with 1 / 2 / 4 / 8: 4096 x 4096 31 / 31 / 37 / 43, 289 x 4096 9.5 / 9.3 / 9.0 / 9.1,
+// 2000 x 8192 32 / 36 / 45 / 54, 6964 x 392 25 / 17 / 14 / 16, 6396 x 1024 27 / 19 / 17 / 21, 301 x 16384 22 / 23 / 23 / 23.
 int back_blocks(int M) {
     const int most = 2 * device_cu_count();
     return M < most ? M : most;
