@@ -20,19 +20,6 @@ struct AppendArgs {
     int q_heads, positions;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f[2 * e] = __builtin_bit_cast(float, w[e] << 16);
-        f[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float* f) {
-    return uint4{f32x2_to_bf16x2_rne(f[0], f[1]), f32x2_to_bf16x2_rne(f[2], f[3]), f32x2_to_bf16x2_rne(f[4], f[5]),
-                 f32x2_to_bf16x2_rne(f[6], f[7])};
-}
-
 // A block's heads of a token.
 template <int D, bool kEight>
 __device__ __forceinline__ void append_token(const AppendArgs& a) {

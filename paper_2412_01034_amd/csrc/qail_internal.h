@@ -41,6 +41,20 @@ __device__ __forceinline__ float f16_bits_to_f32(uint16_t b) {
     return (float)__builtin_bit_cast(_Float16, b);
 }
 
+// Eight bf16 values in 16 bytes.
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+        f[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+    return uint4{f32x2_to_bf16x2_rne(f[0], f[1]), f32x2_to_bf16x2_rne(f[2], f[3]), f32x2_to_bf16x2_rne(f[4], f[5]),
+                 f32x2_to_bf16x2_rne(f[6], f[7])};
+}
+
 // The larger of two magnitudes (no sign bits); NaN is larger than any number, so that a maximum keeps it (fmaxf does not).
 __device__ __forceinline__ float max_magnitude(float a, float b) {
     const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);

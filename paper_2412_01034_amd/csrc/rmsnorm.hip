@@ -14,19 +14,6 @@ namespace {
 
 constexpr int kNormMaxK = 32768;   // 1024 threads hold a row as four pieces of eight values each
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f[2 * e] = __builtin_bit_cast(float, w[e] << 16);
-        f[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float* f) {
-    return uint4{f32x2_to_bf16x2_rne(f[0], f[1]), f32x2_to_bf16x2_rne(f[2], f[3]), f32x2_to_bf16x2_rne(f[4], f[5]),
-                 f32x2_to_bf16x2_rne(f[6], f[7])};
-}
-
 // Sum of a and maximum (of magnitudes) or sum of b over the kGroup threads that share a row; every thread gets them.
 template <int kGroup, bool kMax>
 __device__ __forceinline__ void row_reduce(float& a, float& b, float2* red) {
