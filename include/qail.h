@@ -421,11 +421,12 @@ int qail_qbc_loss(const float* logits_q, const float* logits_fp, int32_t B, int3
  *   h_out        bf16 [M][K], the rounded h, or NULL; may be x or residual itself
  *   y            bf16 [M][K] or NULL; may be x or residual itself, when h_out is not
  *   y_s8, y_scale  uint32 [M][K/4] and fp32 [M], both or neither
- * At least one of h_out (with a residual), y and y_s8 is required.  K % 8 == 0, K <= 32768, M * K < 2^31, M < 2^26. */
+ * At least one of h_out (with a residual), y and y_s8 is required.  K % 8 == 0, K <= 32768, M * K < 2^31, 1 <= M < 2^26. */
 int qail_rmsnorm(const uint16_t* x, const uint16_t* residual, const uint16_t* weight, float eps, int32_t M, int32_t K,
                  uint16_t* h_out, uint16_t* y, uint32_t* y_s8, float* y_scale, void* stream);
 
-/* Its gradient.  h: bf16 [M][K], what was normalised (h_out of the forward call, or x where there is no residual);
+/* Its gradient, at the rounded h: bf16 [M][K], h_out of the forward call, or x where there is no residual (the forward call with a residual normalises the
+ * sum before its rounding to bf16; the two gradients differ by what that rounding changes);
  * dy: the gradient of y; dres: the gradient that reaches h_out on its other way, or NULL; both bf16 [M][K].  With n = h * r:
  *     dx = bf16(r * (dy * weight - n * mean_k(dy * weight * n)) + dres)     the gradient of x and of residual; [M][K]
  *     dweight[k] = sum_m dy * n                                             fp32 [K], a fixed order of summation
@@ -515,7 +516,8 @@ int qail_paged_attention(const qail_kv_cache* c, const qail_requests* b, const u
  * A: bf16 [n][r][K], B: bf16 [n][N][r], scaling: fp32 [n]; device memory, 16-byte aligned; 8 <= r <= 64, r % 8 == 0, n >= 1; an
  * adapter of a lower rank is filled up with zeros.  row_adapter: int32 [M], device, 4-byte aligned, the same for all linears.
  * The linear is rounded to bf16 as by qail_w4a16_linear_batch, the adapter's fp32 part is added and rounded again; a row without an adapter
- * keeps the linear's bits.  What one adapter holds reaches no row of another. */
+ * keeps the linear's bits.  What one adapter holds reaches no row of another.  M >= 1: a step of zero tokens, which the writer and the attention take,
+ * has nothing to multiply, here and in the norm as in every linear. */
 typedef struct {
     const uint16_t* A;
     const uint16_t* B;

@@ -5,6 +5,8 @@
 // nothing an adapter holds (an infinity included) reaches another's rows.  At decode sizes, where every row may have its own,
 // the distinct adapters of a tile are spread over blocks (`slots`), since one after the other they would be a chain of round
 // trips to memory.  The bytes are those of the adapters in use, r (K + N) bf16 each.
+// y is rounded to bf16 twice, by the linear's launch and here (0.0023 of its norm from 64 bits, 0.0017 with one rounding): a linear in fp32 between the two would be
+// written and read with twice the bytes, 170 MB more at 1000 rows of a 7B layer.
 #include <algorithm>
 
 #include "qail_internal.h"
