@@ -3,8 +3,8 @@
 // Bound by memory, or at a few tokens by the latency of finding a token's place: q_start -> request -> kv_len and page -> slot.
 // head_dim / 16 lanes share a head, each with eight values of either half, so that a lane has both values of its rotations and
 // a head's largest magnitude is three exchanges away.  Where the cache has bytes, codes are decided in fp32 without fused
-// multiply-adds: the same codes come out of any correct fp32 implementation of the formulas.  16 tokens of 32 heads of 128 take 3.1 us,
-// 5512 into a cache of bytes 55 us (228 MB, 4.1 TB/s).
+// multiply-adds: the same codes come out of any correct fp32 implementation of the formulas.  16 tokens of 32 heads of 128 take 3.0 us,
+// 5512 into a cache of bytes 56 us (228 MB, 4.1 TB/s), with the vector unit busy for 78 % of them.
 #include "kv_cache.h"
 
 namespace qail {

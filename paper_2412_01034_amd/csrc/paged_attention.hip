@@ -140,7 +140,7 @@ __device__ __forceinline__ void store_row_alone(const AttentionArgs& a, const fl
 // once.  A wave takes 32 keys at a time, on its own: K goes from memory into the registers that the first product reads,
 // V through the wave's part of LDS, which is read transposed.  The four waves of a block take tiles in turn and add up at the end.
 // Rows past the last key repeat it (its slot holds a token, which slots behind it need not) and get a score of minus infinity.  64 requests of
-// 500 to 8000 8-bit keys, 32 heads to 8: 589 MB in 128 us, 4.6 TB/s; one of 295 bf16 keys 7 us, which are trips to memory.
+// 500 to 8000 8-bit keys, 32 heads to 8: 589 MB in 133 us with the join, 4.4 TB/s; one of 295 bf16 keys 7.2 us, which are trips to memory.
 constexpr int kStreamWaves = 4, kStreamKeys = 32;   // a step (kStepKeys) is a tile of keys for each wave
 static_assert(kStreamWaves * kStreamKeys == kStepKeys, "a step is a tile of keys for each wave");
 
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_stream_kernel(const At
 // Bound by the vector unit next to the matrix cores: of 64 keys a wave has 32 products of 32 cycles each, and for every score a
 // multiply-add, an exponential and three halves of an instruction for the maximum, the sum (two rounded p at a time) and
 // the rounding.  So nothing else is left in the loop: places in LDS are registers and immediates (the loop has a copy for either half), places in memory
-// scalars, but for the last 64 keys.  Four prompts to 2500 tokens (111 GFLOP) take 160 us, 690 TFLOP/s, three chunks behind 7000 to 13000 keys 760: the
+// scalars, but for the last 64 keys.  Four prompts to 2500 tokens (111 GFLOP) take 158 us, 700 TFLOP/s, three chunks behind 7000 to 13000 keys 790: the
 // matrix cores are busy 36 and 40 % of the time and the vector unit 41 and 39 %, next to each other for little of it; a quarter of a wave's time is waiting.
 // 32 keys at a time and three blocks a compute unit instead of two: prompts the same, chunks 171 -> 213.
 constexpr int kTileWaves = 4;

@@ -4,8 +4,8 @@
 // kGroup threads from its first to its last use, so that everything is read once and written once; both reductions of a row (its
 // sum of squares, the largest |h * weight|) go through one exchange.  The codes do not depend on r = 1 / rms: q = rint(u / s) with
 // u = h * weight and s = max |u| / 127, and r goes into the scale that is written beside them.  Two machines or two orders of
-// summation then agree on every code.  With the residual 2048 x 4096 to codes take 13.6 us (59 MB, 4.3 TB/s), 7 rows 3.4; the gradient of
-// 4096 x 4096 26.9 us (134 MB, 5.0 TB/s) and 4.7 for the weight's sums, 289 rows 6.0 and 3.8.
+// summation then agree on every code.  With the residual 2048 x 4096 to codes take 13.8 us (59 MB, 4.3 TB/s), 7 rows 3.2; the gradient of
+// 4096 x 4096 26.8 us (134 MB, 5.0 TB/s) and 4.8 for the weight's sums, 289 rows 5.9 and 3.7.
 #include "qail_internal.h"
 
 namespace qail {
