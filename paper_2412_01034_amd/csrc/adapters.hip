@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kDownWaves* kWave) void adapters_down_rows_kernel(c
 }
 
 // A wave adds to 16 rows of `chunks` times 64 columns.  Row i of tile t of the product is column 16 (i / 4) + 4 t + i % 4, so that a lane ends up with 16
-// consecutive columns of one row.  t is split into two bf16 values (a relative 2^-17 is lost, where one alone would lose 2^-9).
+// consecutive columns of one row.  t is split into two bf16 values (a relative 2^-16 may be lost, where one alone may lose 2^-8).
 template <int kParts, bool kWide>   // of 32 of the rank; N % 8 == 0: rows of y are 16-byte aligned
 __device__ __forceinline__ void add_up(const AdapterArgs& a, const AdapterItem& it, int m0, int n_begin, int slot) {
     const int lane = threadIdx.x % kWave, col = lane % 16, g = lane / 16;

@@ -270,8 +270,8 @@ __device__ __forceinline__ void attend_rows(const AttentionArgs& a, uint8_t* lds
                 for (int d = 0; d < D / 16; ++d) o[d] *= alpha;
                 m = m_new;
             }
-            // p in two parts, each rounded to bf16: 2^-17 of it is lost instead of 2^-9, for 8 more products of 32 keys beside a stream of bytes (attend_one
-            // 7.0 -> 7.2 us, 64 requests of 8-bit keys 129 -> 133)
+            // p in two parts, each rounded to bf16: 2^-16 of it may be lost instead of 2^-8, for D / 16 more products of 32 keys (one request of 295 keys 7.0 -> 7.2 us,
+            // 64 of 8-bit keys 129 -> 133)
             uint32_t ph[4], pl[4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
