@@ -530,6 +530,94 @@ int qail_w4a16_adapters_workspace(const qail_w4a16_item* items, const qail_adapt
 int qail_w4a16_linear_adapters_batch(const qail_w4a16_item* items, const qail_adapters* adapters, const int32_t* row_adapter, int32_t count,
                                      int32_t M, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------- the policy's ends, in 16 bits --
+ * Sec. 5.4 and the appendix "Analysis" quantise the backbone's linears; the table of embeddings, the head, the projector and the vision
+ * side stay in 16 bits.  These calls are what a policy does before its first decoder layer and after its last one. */
+
+/* Rows of a table: h[t][k] = bf16(scale * table[ids[t]][k]), one rounding.
+ *   table  bf16 [V][K]; ids int32 [T]; h bf16 [T][K] (not the table); scale finite
+ * A row whose id is negative is left as it was: image patches, written by the projector, lie between the tokens.  For an id >= V the row
+ * is zero and *errors (device, one uint32, may be NULL; not cleared) is incremented at least once.
+ * K % 8 == 0, K <= 65536, V < 2^24, 0 <= T < 2^24 (0 launches nothing), V * K and T * K <= 2^36. */
+int qail_embed(const uint16_t* table, int32_t V, int32_t K, const int32_t* ids, int32_t T, float scale, uint16_t* h, uint32_t* errors,
+               void* stream);
+
+/* Its gradient: dtable[v][k] = scale * sum of dh[t][k] over the t with ids[t] == v, fp32 [V][K], in an order that depends on ids alone, so
+ * that the same call always gives the same bits; accumulate != 0 adds it to what dtable holds and leaves the rows without a token alone,
+ * 0 overwrites all of it.  Negative ids and ids >= V have no row; the latter are counted as above.  What dh holds in their rows is not used.
+ * Sizes as above, T = 0 among them (with accumulate == 0 the gradient is zero).  The workspace is 256-byte aligned. */
+int qail_embed_backward_workspace(int32_t V, int32_t K, int32_t T, size_t* bytes);
+int qail_embed_backward(const int32_t* ids, const uint16_t* dh, int32_t T, float scale, int32_t V, int32_t K, int32_t accumulate, float* dtable,
+                        uint32_t* errors, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum {
+    QAIL_ACT_NONE = 0,
+    QAIL_ACT_RELU = 1,       /* max(z, 0); slope 0 at 0 */
+    QAIL_ACT_GELU = 2,       /* z (1 + erf(z / sqrt(2))) / 2 */
+    QAIL_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+    QAIL_ACT_SILU = 4        /* z / (1 + exp(-z)) */
+} qail_activation;
+
+/* A linear whose weights stay in 16 bits: W bf16 [N][K], bias bf16 [N] or NULL; device memory, 16-byte aligned. */
+typedef struct {
+    int32_t N, K;             /* N >= 1; K a multiple of 8 */
+    int32_t activation;       /* qail_activation */
+    const uint16_t* weight;
+    const uint16_t* bias;
+} qail_w16a16;
+
+/*     z[m][n] = sum_k x[m][k] W[n][k] + bias[n]           fp32
+ *     y[m][n] = act(z[m][n]) + residual[m][n]              fp32, rounded once
+ *   x          bf16 [M][K]; residual bf16 [M][N] or NULL
+ *   y, y_f32   bf16 or fp32 [M][N], exactly one of them; y may be the residual itself
+ *   z_out      bf16 [M][N], the rounded z for the backward call, or NULL; not y or the residual
+ * M, N, K <= 2^22, M * N, M * K and N * K <= 2^33.  The workspace (256-byte aligned; may be NULL where the query says 0) holds partial sums
+ * of output tiles whose K is divided among blocks. */
+int qail_w16a16_workspace(const qail_w16a16* d, int32_t M, size_t* bytes);
+int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const uint16_t* residual, uint16_t* z_out, uint16_t* y, float* y_f32,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients, at the rounded z:
+ *     dz = dy * act'(z)                     fp32; rounded to bf16 for the products
+ *     dx[m][k] = sum_n dz[m][n] W[n][k]     fp32 sums, rounded once; bf16 [M][K] or NULL
+ *     dweight[n][k] = sum_m dz[m][n] x[m][k]   likewise; bf16 [N][K] or NULL
+ *     dbias[n] = sum_m dz[m][n]             of the unrounded dz, a fixed order of summation; fp32 [N] or NULL
+ * (that of the residual is dy).
+ *   x            needed for dweight only
+ *   z            z_out of the forward call, bf16 [M][N]; not looked at without an activation
+ *   dy, dy_f32   bf16 or fp32 [M][N], exactly one of them
+ * At least one of the three outputs is required, and each is written whole; none may be an input.  Sizes as above. */
+int qail_w16a16_backward_workspace(const qail_w16a16* d, int32_t M, size_t* bytes);
+int qail_w16a16_backward(const qail_w16a16* d, const uint16_t* x, const uint16_t* z, const uint16_t* dy, const float* dy_f32, int32_t M,
+                         uint16_t* dx, uint16_t* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum { QAIL_LOGITS_BF16 = 0, QAIL_LOGITS_F32 = 1 } qail_logits_type;
+
+/* How the rows of a step are drawn from: one value a row, device memory, 4-byte aligned; a NULL array leaves its choice off in all rows. */
+typedef struct {
+    const float* temperature;   /* > 0; 0: the largest logit.  Off: 1 */
+    const int32_t* top_k;       /* <= 0: off */
+    const float* top_p;         /* >= 1: off; <= 0 keeps the first token alone */
+    const float* min_p;         /* <= 0: off */
+} qail_sampling;
+
+/* A token for each row of logits [R][V], row r at r * stride (elements, >= V).  With the tokens of a row in the order of falling logits, equal
+ * ones in the order of their numbers, w[j] = exp((logit[j] - the row's largest) / temperature):
+ *     top_k keeps the first top_k tokens of that order; top_p, of what is kept, the shortest leading part whose sum of w is at least
+ *     top_p of the sum of all that is kept; min_p, of those, the ones with w >= min_p; the first token is always kept
+ *     token[r] = the lowest j that is kept with sum_{i <= j, i kept} w[i] > u[r] * sum_{i kept} w[i]
+ *     logprob[r] = log(w[token] / sum_{i kept} w[i]), fp32; 0 at temperature 0
+ * w and its sums are held in 64 bits, as multiples of 2^-44: a token below 2^-45 of its row's largest counts as impossible, and the order of
+ * the sums does not matter, so that the same call always gives the same tokens.
+ *   logits   of `type`, 16-byte aligned; minus infinity: never drawn
+ *   u        fp32 [R], in [0, 1): the random numbers; not looked at where temperature is 0
+ *   token    int32 [R]; logprob fp32 [R] or NULL
+ * A row that holds NaN or plus infinity or nothing above minus infinity, whose temperature is negative, infinite or NaN, whose top_p or min_p is NaN or whose u is outside
+ * [0, 1) gets token -1 and logprob NaN, and *errors (device, one uint32, may be NULL; not cleared) is incremented.
+ * 0 <= R <= 2^20, 1 <= V <= 2^18. */
+int qail_sample(const void* logits, int32_t type, int64_t stride, int32_t R, int32_t V, const qail_sampling* s, const float* u, int32_t* token,
+                float* logprob, uint32_t* errors, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,8 @@ EXPORTS = (
     "qail_fake_quant_w4", "qail_lsq_forward", "qail_lsq_backward_workspace", "qail_lsq_backward", "qail_qbc_loss",
     "qail_rmsnorm", "qail_rmsnorm_backward_workspace", "qail_rmsnorm_backward", "qail_kv_cache_sizes", "qail_kv_append",
     "qail_paged_attention_workspace", "qail_paged_attention", "qail_w4a16_adapters_workspace", "qail_w4a16_linear_adapters_batch",
+    "qail_embed", "qail_embed_backward_workspace", "qail_embed_backward", "qail_w16a16_workspace", "qail_w16a16_linear",
+    "qail_w16a16_backward_workspace", "qail_w16a16_backward", "qail_sample",
 )
 
 
@@ -95,6 +97,14 @@ class qail_requests(ctypes.Structure):
 
 class qail_adapters(ctypes.Structure):
     _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scaling", ctypes.c_void_p), ("n", ctypes.c_int32), ("r", ctypes.c_int32)]
+
+
+class qail_w16a16(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("activation", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class qail_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
 _lib = None
@@ -158,6 +168,15 @@ def lib() -> ctypes.CDLL:
         L.qail_paged_attention.argtypes = [pc, pb, vp, i64, i32, f32, vp, vp, vp, sz, vp]
         L.qail_w4a16_adapters_workspace.argtypes = [ctypes.POINTER(qail_w4a16_item), ctypes.POINTER(qail_adapters), i32, i32, psz]
         L.qail_w4a16_linear_adapters_batch.argtypes = [ctypes.POINTER(qail_w4a16_item), ctypes.POINTER(qail_adapters), vp, i32, i32, vp, sz, vp]
+        pl, ps = ctypes.POINTER(qail_w16a16), ctypes.POINTER(qail_sampling)
+        L.qail_embed.argtypes = [vp, i32, i32, vp, i32, f32, vp, vp, vp]
+        L.qail_embed_backward_workspace.argtypes = [i32, i32, i32, psz]
+        L.qail_embed_backward.argtypes = [vp, vp, i32, f32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.qail_w16a16_workspace.argtypes = [pl, i32, psz]
+        L.qail_w16a16_linear.argtypes = [pl, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.qail_w16a16_backward_workspace.argtypes = [pl, i32, psz]
+        L.qail_w16a16_backward.argtypes = [pl, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.qail_sample.argtypes = [vp, i32, i64, i32, i32, ps, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             if name not in ("qail_status_string",):
                 getattr(L, name).restype = ctypes.c_int
@@ -826,3 +845,104 @@ def qail_w4a16_linear_adapters_batch(items, adapters, row_adapter: torch.Tensor,
     wsb = workspace.nbytes if workspace is not None else 0
     _check(lib().qail_w4a16_linear_adapters_batch(items, adapters, _int32(row_adapter, M, "row_adapter"), count, M, _ptr(workspace), wsb,
                                                   _stream() if stream is None else stream), "qail_w4a16_linear_adapters_batch")
+
+
+# ------------------------------------------------------------------------- the policy's ends, in 16 bits --
+
+QAIL_ACT_NONE = 0
+QAIL_ACT_RELU = 1
+QAIL_ACT_GELU = 2
+QAIL_ACT_GELU_TANH = 3
+QAIL_ACT_SILU = 4
+ACTIVATIONS = {"none": QAIL_ACT_NONE, "relu": QAIL_ACT_RELU, "gelu": QAIL_ACT_GELU, "gelu_tanh": QAIL_ACT_GELU_TANH, "silu": QAIL_ACT_SILU}
+
+QAIL_LOGITS_BF16 = 0
+QAIL_LOGITS_F32 = 1
+
+
+def qail_embed(table: torch.Tensor, ids: torch.Tensor, h: torch.Tensor, scale: float = 1.0, errors: Optional[torch.Tensor] = None) -> None:
+    """table: bf16 [V, K]; ids: int32, any shape; h: bf16, K values for each id.  A row whose id is negative is left as it was."""
+    V, K = table.shape
+    T = ids.numel()
+    _check(lib().qail_embed(_bf16(table, V * K, "table"), V, K, _int32(ids, T, "ids"), T, scale, _bf16(h, T * K, "h"), _errors(errors), _stream()),
+           "qail_embed")
+
+
+def qail_embed_backward_workspace(V: int, K: int, T: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_embed_backward_workspace(V, K, T, ctypes.byref(b)), "qail_embed_backward_workspace")
+    return b.value
+
+
+def qail_embed_backward(ids: torch.Tensor, dh: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                        errors: Optional[torch.Tensor] = None) -> None:
+    """ids: int32, any shape; dh: bf16, K values for each id; dtable: fp32 [V, K], overwritten or, with `accumulate`, added to."""
+    V, K = dtable.shape
+    T = ids.numel()
+    _check(lib().qail_embed_backward(_int32(ids, T, "ids"), _bf16(dh, T * K, "dh"), T, scale, V, K, int(bool(accumulate)), _fp32(dtable, V * K, "dtable"),
+                                     _errors(errors), _ptr(workspace), workspace.nbytes, _stream()), "qail_embed_backward")
+
+
+def make_w16a16(weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none") -> qail_w16a16:
+    """weight: bf16 [N, K]; bias: bf16 [N]; activation: a key of ACTIVATIONS.  The result can be passed to any number of calls (the tensors must be
+    kept alive by the caller)."""
+    N, K = weight.shape
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation: one of {', '.join(ACTIVATIONS)} expected, {activation!r} given")
+    return qail_w16a16(N, K, ACTIVATIONS[activation], _bf16(weight, N * K, "weight"), _bf16(bias, N, "bias"))
+
+
+def qail_w16a16_workspace(linear: qail_w16a16, M: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_w16a16_workspace(ctypes.byref(linear), M, ctypes.byref(b)), "qail_w16a16_workspace")
+    return b.value
+
+
+def _bf16_or_fp32(t: torch.Tensor, count: int, what: str) -> Tuple[Optional[int], Optional[int]]:
+    """(address as bf16, address as fp32), one of them None."""
+    _typed(t, what, torch.bfloat16, torch.int16, torch.float32)
+    return (None, _fp32(t, count, what)) if t.dtype == torch.float32 else (_bf16(t, count, what), None)
+
+
+def qail_w16a16_linear(linear: qail_w16a16, x: torch.Tensor, y: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                       residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None) -> None:
+    """x: bf16 [M, K]; y: bf16 or fp32 [M, N]; residual, z (what the activation is applied to, for the backward call): bf16 [M, N]."""
+    M, N, K = x.shape[0], linear.N, linear.K
+    half, whole = _bf16_or_fp32(y, M * N, "y")
+    ws, wsb = (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
+    _check(lib().qail_w16a16_linear(ctypes.byref(linear), _bf16(x, M * K, "x"), M, _bf16(residual, M * N, "residual"), _bf16(z, M * N, "z"), half, whole,
+                                    ws, wsb, _stream()), "qail_w16a16_linear")
+
+
+def qail_w16a16_backward_workspace(linear: qail_w16a16, M: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qail_w16a16_backward_workspace(ctypes.byref(linear), M, ctypes.byref(b)), "qail_w16a16_backward_workspace")
+    return b.value
+
+
+def qail_w16a16_backward(linear: qail_w16a16, x: Optional[torch.Tensor], dy: torch.Tensor, workspace: torch.Tensor, z: Optional[torch.Tensor] = None,
+                         dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None) -> None:
+    """x, dx: bf16 [M, K]; dy: bf16 or fp32 [M, N]; z: bf16 [M, N]; dweight: bf16 [N, K]; dbias: fp32 [N]."""
+    M, N, K = dy.shape[0], linear.N, linear.K
+    half, whole = _bf16_or_fp32(dy, M * N, "dy")
+    _check(lib().qail_w16a16_backward(ctypes.byref(linear), _bf16(x, M * K, "x"), _bf16(z, M * N, "z"), half, whole, M, _bf16(dx, M * K, "dx"),
+                                      _bf16(dweight, N * K, "dweight"), _fp32(dbias, N, "dbias"), _ptr(workspace), workspace.nbytes, _stream()),
+           "qail_w16a16_backward")
+
+
+def qail_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor, logprob: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                errors: Optional[torch.Tensor] = None) -> None:
+    """logits: bf16 or fp32 [R, V], rows of a wider tensor among them; u: fp32 [R], in [0, 1); token: int32 [R]; logprob: fp32 [R]; temperature, top_p, min_p: fp32
+    [R], top_k: int32 [R], None for off."""
+    _typed(logits, "logits", torch.bfloat16, torch.float32)
+    if not logits.is_cuda:
+        raise ValueError("device tensor expected")
+    R, V = logits.shape
+    if logits.stride(1) != 1 and V > 1:
+        raise ValueError("logits: the values of a row must be contiguous")
+    s = qail_sampling(_fp32(temperature, R, "temperature"), None if top_k is None else _int32(top_k, R, "top_k"), _fp32(top_p, R, "top_p"),
+                      _fp32(min_p, R, "min_p"))
+    _check(lib().qail_sample(logits.data_ptr(), QAIL_LOGITS_F32 if logits.dtype == torch.float32 else QAIL_LOGITS_BF16, logits.stride(0) if R > 1 else V, R, V,
+                             ctypes.byref(s), _fp32(u, R, "u"), _int32(token, R, "token"), _fp32(logprob, R, "logprob"), _errors(errors), _stream()),
+           "qail_sample")

@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libqail.so")
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # another Python does not look at it
 
 SOURCES = ("api.hip", "quantize.hip", "w4a16_gemv.hip", "w4a16_decode4.hip", "w4a16_smallm.hip", "w4a16_midm.hip", "w4a16_gemm.hip", "w4a16_generic.hip", "w4a16_lora.hip", "w8.hip", "w8a16_gemv.hip", "train_ops.hip", "w4a4_conv.hip",
-           "serve_api.hip", "rmsnorm.hip", "kv_append.hip", "paged_attention.hip", "adapters.hip")
+           "serve_api.hip", "rmsnorm.hip", "kv_append.hip", "paged_attention.hip", "adapters.hip",
+           "ends_api.hip", "embed.hip", "w16a16.hip", "sample.hip")
 
 HIPCC_FLAGS = (
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

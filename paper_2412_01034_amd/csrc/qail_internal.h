@@ -163,4 +163,18 @@ size_t adapters_workspace(const qail_w4a16_item* items, const qail_adapters* ad,
 hipError_t launch_adapters_down(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
 hipError_t launch_adapters_up(const qail_w4a16_item* items, const qail_adapters* ad, const int32_t* rows, int count, int M, float* t, hipStream_t st);
 
+// The policy's ends in 16 bits.
+hipError_t launch_embed(const uint16_t* table, int V, int K, const int32_t* ids, int T, float scale, uint16_t* h, uint32_t* errors, hipStream_t st);
+size_t embed_back_workspace(int K, int T);
+hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, float scale, int V, int K, bool accumulate, float* dtable, uint32_t* errors, void* ws,
+                             hipStream_t st);
+size_t w16a16_workspace(const qail_w16a16& d, int M);
+hipError_t launch_w16a16(const qail_w16a16& d, const uint16_t* x, int M, const uint16_t* residual, uint16_t* z_out, uint16_t* y, float* y_f32, void* ws,
+                         hipStream_t st);
+size_t w16a16_back_workspace(const qail_w16a16& d, int M);
+hipError_t launch_w16a16_back(const qail_w16a16& d, const uint16_t* x, const uint16_t* z, const uint16_t* dy, const float* dy_f32, int M, uint16_t* dx,
+                              uint16_t* dweight, float* dbias, void* ws, hipStream_t st);
+hipError_t launch_sample(const void* logits, int type, int64_t stride, int R, int V, const qail_sampling& s, const float* u, int32_t* token, float* logprob,
+                         uint32_t* errors, hipStream_t st);
+
 }  // namespace qail

@@ -1,0 +1,459 @@
+// Linears whose weights stay in 16 bits, with bias, activation and residual in the epilogue, and their gradients:
+//     y = act(x W^T + b) + residual,   dz = dy act'(z),   dx = dz W,   dW = dz^T x,   db = sum of dz over the rows.
+//
+// All three products are C[p][q] = sum_r A(p, r) B(q, r), whose operands either have r contiguous ("straight": x and W of the
+// forward product, dz of dx) or lie row by row of r ("turned": W of dx, dz and x of dW).  One kernel computes them: 64 r at a time go from
+// memory straight into LDS, and a turned operand is read from there transposed by the hardware, so that nothing is transposed in memory.
+#include <algorithm>
+
+#include "qail_internal.h"
+#include "w16a16_plan.h"
+
+namespace qail {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(8))) short s16x8_t;
+typedef __attribute__((address_space(3))) uint8_t lds_t;
+
+// s_waitcnt immediate: vmcnt(n), lgkmcnt(0), expcnt untouched.
+__host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
+
+// ------------------------------------------------------------------------------------------------ activations --
+
+__device__ __forceinline__ float activated(int act, float z) {
+    switch (act) {
+        case QAIL_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+        case QAIL_ACT_GELU: return 0.5f * z * erfcf(-0.70710678f * z);       // 1 + erf(v) = erfc(-v): no cancellation below zero
+        case QAIL_ACT_GELU_TANH: {
+            const float v = 1.5957691f * (z + 0.044715f * z * z * z);        // (1 + tanh(v / 2)) / 2 = 1 / (1 + exp(-v))
+            return z / (1.f + expf(-v));
+        }
+        case QAIL_ACT_SILU: return z / (1.f + expf(-z));
+        default: return z;
+    }
+}
+
+__device__ __forceinline__ float slope(int act, float z) {
+    switch (act) {
+        case QAIL_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case QAIL_ACT_GELU: {
+            const float p = 0.5f * erfcf(-0.70710678f * z), d = expf(-0.5f * z * z);
+            return d > 0.f ? p + 0.39894228f * z * d : p;
+        }
+        case QAIL_ACT_GELU_TANH: {
+            const float v = 1.5957691f * (z + 0.044715f * z * z * z), s = 1.f / (1.f + expf(-v)), t = 1.f / (1.f + expf(v));
+            return s * t > 0.f ? s + z * (s * t) * 1.5957691f * (1.f + 0.134145f * z * z) : s;   // (no zero times an infinity)
+        }
+        case QAIL_ACT_SILU: {
+            const float s = 1.f / (1.f + expf(-z)), t = 1.f / (1.f + expf(z));
+            return s * t > 0.f ? s + z * (s * t) : s;
+        }
+        default: return 1.f;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------- epilogue --
+
+struct Epilogue {
+    const uint16_t* bias;       // [Q] or NULL
+    const uint16_t* residual;   // [P][Q] or NULL
+    uint16_t* z;                // [P][Q] or NULL
+    uint16_t* y;                // [P][Q], or y32
+    float* y32;
+    int act, Q;
+};
+
+// Outputs p, q .. q + 7 from their sums.  Rows of Q % 8 == 0 start on 16 bytes; others go value by value.
+__device__ __forceinline__ void finish8(const Epilogue& e, long long p, int q, float* v) {
+    const size_t at = (size_t)p * e.Q + q;
+    if (e.Q % 8 == 0) {
+        float t[8];
+        if (e.bias) {
+            unpack8(*reinterpret_cast<const uint4*>(e.bias + q), t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        if (e.z) *reinterpret_cast<uint4*>(e.z + at) = pack8(v);
+        if (e.act != QAIL_ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activated(e.act, v[i]);
+        }
+        if (e.residual) {
+            unpack8(*reinterpret_cast<const uint4*>(e.residual + at), t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        if (e.y) {
+            *reinterpret_cast<uint4*>(e.y + at) = pack8(v);
+        } else {
+            reinterpret_cast<float4*>(e.y32 + at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(e.y32 + at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (q + i >= e.Q) return;
+        float t = v[i];
+        if (e.bias) t += bf16_bits_to_f32(e.bias[q + i]);
+        if (e.z) e.z[at + i] = (uint16_t)f32x2_to_bf16x2_rne(t, 0.f);
+        if (e.act != QAIL_ACT_NONE) t = activated(e.act, t);
+        if (e.residual) t += bf16_bits_to_f32(e.residual[at + i]);
+        if (e.y) e.y[at + i] = (uint16_t)f32x2_to_bf16x2_rne(t, 0.f);
+        else e.y32[at + i] = t;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------- products --
+
+struct ProductArgs {
+    const uint16_t* a;      // straight: [P][lda], turned: [R][lda] (lda >= P rounded up to 8)
+    const uint16_t* b;      // likewise with Q
+    long long lda, ldb;
+    int P, Q, R;            // R: of a straight operand a multiple of 8 that its rows have
+    ProductPlan plan;
+    float* partial;         // [splits][P][Q rounded up to 8], where splits > 1
+    Epilogue e;
+};
+
+__device__ const uint4 kNothing = {0, 0, 0, 0};   // what is loaded beyond the end of r
+
+// 16 bytes of each lane from memory into LDS, lane i's at lds + 16 i.  As assembly: the compiler would make every LDS read wait for all
+// copies in flight, since it does not see that the slots of the ring differ.  The waits are the explicit s_waitcnt vmcnt(n).
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+__device__ __forceinline__ void copy16(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy16_from(const void* p, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
+}
+
+// One operand's part of a step in LDS: kB rows (p or q) of 64 r.  Straight: kB rows of 128 bytes, piece s (16 bytes) of row i at s ^ (i & 7), so
+// that 8 consecutive rows' reads of one s hit 8 places.  Turned: 64 rows (r) of 2 kB bytes, piece s of row i at s ^ ((i & 3) << 2): a transposed read takes
+// 64 bytes of each of four rows, which lie in four places of 256 bytes then.
+template <int kB, bool kTurned, int kThreads>
+struct Operand {
+    static constexpr int kBytes = kB * 2 * kStepR;
+    static constexpr int kLoads = kBytes / 16 / kThreads;
+    static constexpr int kPieces = kTurned ? kB / 8 : kStepR / 8;   // of a row
+    static_assert(kLoads * 16 * kThreads == kBytes && (!kTurned || kB >= 128), "whole loads, whole swizzles");
+    __device__ static __forceinline__ int place(int row, int piece) { return piece ^ (kTurned ? (row & 3) << 2 : row & 7); }
+
+    const uint16_t* base;     // row 0 of the tile (straight) or its column 0 in row 0 (turned), at r = 0
+    long long ld;
+    uint32_t off[kLoads];     // bytes of a thread's pieces of a step from there
+    int R;
+
+    __device__ __forceinline__ Operand(const uint16_t* m, long long ld_, int first, int count, int R_) : ld(ld_), R(R_) {
+        base = kTurned ? m + first : m + (long long)first * ld;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int id = i * kThreads + threadIdx.x, row = id / kPieces, piece = place(row, id % kPieces);
+            if constexpr (kTurned) {
+                const int last = (count - 1 - first) / 8;   // pieces behind the matrix repeat its last one: outputs that nobody writes
+                off[i] = (uint32_t)((long long)row * ld * 2) + 16u * (piece < last ? piece : last);
+            } else {
+                const int last = count - 1 - first;
+                off[i] = (uint32_t)((long long)(row < last ? row : last) * ld * 2) + 16u * piece;
+            }
+        }
+    }
+    // Step `step` into LDS at `lds` (of the block); what lies beyond R is zero.
+    __device__ __forceinline__ void load(int step, uint32_t lds) const {
+        const int r0 = step * kStepR;
+        const uint16_t* const from = base + (kTurned ? (long long)r0 * ld : (long long)r0);
+        const uint32_t to = lds + (threadIdx.x / kWave) * (16 * kWave);
+        if (r0 + kStepR <= R) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) copy16(from, off[i], __builtin_amdgcn_readfirstlane(to + i * kThreads * 16));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int id = i * kThreads + threadIdx.x, row = id / kPieces;
+                const int r = kTurned ? r0 + row : r0 + 8 * place(row, id % kPieces);
+                const void* const p = r < R ? reinterpret_cast<const char*>(from) + off[i] : reinterpret_cast<const char*>(&kNothing);
+                copy16_from(p, __builtin_amdgcn_readfirstlane(to + i * kThreads * 16));
+            }
+        }
+    }
+    // The fragment of rows first .. first + 31 and r 16 kk .. 16 kk + 15: lane l has row l % 32 and 8 r from 8 (l / 32) on.
+    __device__ static __forceinline__ bf16x8_t fragment(const uint8_t* s, int first, int kk, int lane) {
+        if constexpr (!kTurned) {
+            const int row = first + lane % 32;
+            return *reinterpret_cast<const bf16x8_t*>(s + row * 128 + place(row, 2 * kk + lane / 32) * 16);
+        } else {
+            s16x4_t part[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int row = 16 * kk + 8 * (lane / 32) + 4 * t + lane % 16 / 4, col = first + lane % 32 / 16 * 16 + lane % 4 * 4;
+                part[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4_t*)(lds_t*)(s + row * (2 * kB) + place(row, col / 8) * 16 + col % 8 * 2));
+            }
+            const s16x8_t both = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(bf16x8_t, both);
+        }
+    }
+};
+
+// kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied.
+// The matrix cores get B's rows as rows: a lane then has one p and groups of four neighbouring q, and after an exchange between the wave's
+// halves eight, the 16 bytes of an output row.
+template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
+__global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a16_product_kernel(const ProductArgs g) {
+    constexpr int kThreads = kWP * kWQ * kWave, FP = kBP / kWP / 32, FQ = kBQ / kWQ / 32;
+    using A = Operand<kBP, kTA, kThreads>;
+    using Bo = Operand<kBQ, kTB, kThreads>;
+    constexpr int kSlot = A::kBytes + Bo::kBytes, kLoads = A::kLoads + Bo::kLoads;
+    extern __shared__ __attribute__((aligned(16))) uint8_t ring[];
+    const TilePlace t = tile_place(g.plan, blockIdx.x);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int p0 = t.tp * kBP, q0 = t.tq * kBQ, wp = wave / kWQ * (32 * FP), wq = wave % kWQ * (32 * FQ);
+    const A a(g.a, g.lda, p0, g.P, g.R);
+    const Bo b(g.b, g.ldb, q0, g.Q, g.R);
+    const int first = g.plan.first_step(t.split), steps = g.plan.first_step(t.split + 1) - first;
+    const uint32_t lds = lds_addr(ring);
+
+    f32x16_t acc[FP][FQ] = {};
+    auto load = [&](int i) {
+        const int slot = i % kSlots;
+        a.load(first + i, lds + slot * kSlot);
+        b.load(first + i, lds + slot * kSlot + A::kBytes);
+    };
+#pragma unroll
+    for (int i = 0; i < kSlots - 1; ++i)
+        if (i < steps) load(i);
+    for (int i = 0; i < steps; ++i) {
+        // step i is there once at most the later ones are on their way; after the barrier all waves' parts of it are, and nobody reads step i - 1
+        const int later = steps - 1 - i;
+        if (kSlots >= 4 && later >= 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kLoads));
+        else if (kSlots >= 3 && later >= 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+        else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        asm volatile("s_barrier" ::: "memory");
+        if (i + kSlots - 1 < steps) load(i + kSlots - 1);
+        const uint8_t* const sa = ring + i % kSlots * kSlot;
+        const uint8_t* const sb = sa + A::kBytes;
+#pragma unroll
+        for (int kk = 0; kk < kStepR / 16; ++kk) {
+            bf16x8_t fa[FP], fb[FQ];
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fb[j] = Bo::fragment(sb, wq + 32 * j, kk, lane);
+#pragma unroll
+            for (int j = 0; j < FP; ++j) fa[j] = A::fragment(sa, wp + 32 * j, kk, lane);
+#pragma unroll
+            for (int x = 0; x < FP; ++x)
+#pragma unroll
+                for (int y = 0; y < FQ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[y], fa[x], acc[x][y], 0, 0, 0);
+        }
+    }
+
+    const int Q8 = (g.Q + 7) / 8 * 8;
+#pragma unroll
+    for (int x = 0; x < FP; ++x) {
+        const int p = p0 + wp + 32 * x + lane % 32;
+#pragma unroll
+        for (int y = 0; y < FQ; ++y) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int q = q0 + wq + 32 * y + 16 * h + 8 * (lane / 32);
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a0 = acc[x][y][8 * h + i], a1 = acc[x][y][8 * h + 4 + i];   // (a bit cast of a vector's element takes its first)
+                    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a0), __builtin_bit_cast(unsigned, a1), false, false);
+                    const unsigned lo = r[0], hi = r[1];
+                    v[i] = __builtin_bit_cast(float, lo);
+                    v[4 + i] = __builtin_bit_cast(float, hi);
+                }
+                if (p < g.P && q < g.Q) {
+                    if (g.plan.splits == 1) {
+                        finish8(g.e, p, q, v);
+                    } else {
+                        float4* const to = reinterpret_cast<float4*>(g.partial + ((size_t)t.split * g.P + p) * Q8 + q);
+                        to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// The shares of the contraction added up, in their order, and the epilogue: 8 outputs a thread.
+__global__ __launch_bounds__(256) void w16a16_sum_kernel(const float* __restrict__ partial, int splits, int P, const Epilogue e) {
+    const int n8 = (e.Q + 7) / 8;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, all = (long long)P * n8;
+    if (i >= all) return;
+    float v[8] = {};
+    const float4* from = reinterpret_cast<const float4*>(partial) + 2 * i;
+    for (int s = 0; s < splits; ++s, from += 2 * all) {
+        const float4 lo = from[0], hi = from[1];
+        v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w;
+        v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+    }
+    finish8(e, i / n8, (int)(i % n8) * 8, v);
+}
+
+// -------------------------------------------------------------------------------------------- dz and db --
+
+constexpr int kDzCols = 256;   // columns of a block: 32 threads of 8; 8 threads share a column's rows
+constexpr int kDzRows = 64;    // rows of a block
+
+// dz = bf16(dy act'(z)), rows of ld values (N rounded up to 8, zeros behind N), and the sums of the unrounded dz over a block's rows.
+__global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restrict__ z, const uint16_t* __restrict__ dy, const float* __restrict__ dy32, int act,
+                                                        int M, int N, int ld, uint16_t* __restrict__ dz, float* __restrict__ sums) {
+    __shared__ float part[8][kDzCols + 8];
+    const int across = (ld + kDzCols - 1) / kDzCols, bx = blockIdx.x % across, by = blockIdx.x / across;
+    const int c = threadIdx.x % 32, n = bx * kDzCols + 8 * c, slice = threadIdx.x / 32;
+    const int m0 = by * kDzRows, m1 = min(M, m0 + kDzRows);
+    float sum[8] = {};
+    if (n < ld) {
+        for (int m = m0 + slice; m < m1; m += 8) {
+            const size_t at = (size_t)m * N + n;
+            float v[8], s[8];
+            if (N % 8 == 0) {
+                if (dy) unpack8(*reinterpret_cast<const uint4*>(dy + at), v);
+                else {
+                    const float4 lo = reinterpret_cast<const float4*>(dy32 + at)[0], hi = reinterpret_cast<const float4*>(dy32 + at)[1];
+                    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+                }
+                if (act != QAIL_ACT_NONE) unpack8(*reinterpret_cast<const uint4*>(z + at), s);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool in = n + i < N;
+                    v[i] = !in ? 0.f : dy ? bf16_bits_to_f32(dy[at + i]) : dy32[at + i];
+                    s[i] = in && act != QAIL_ACT_NONE ? bf16_bits_to_f32(z[at + i]) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (act != QAIL_ACT_NONE) v[i] = n + i < N ? v[i] * slope(act, s[i]) : 0.f;
+                sum[i] += v[i];
+            }
+            if (dz) *reinterpret_cast<uint4*>(dz + (size_t)m * ld + n) = pack8(v);
+        }
+    }
+    if (!sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[slice][8 * c + i] = sum[i];
+    __syncthreads();
+    const int col = bx * kDzCols + threadIdx.x;
+    if (col >= N) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += part[i][threadIdx.x];
+    sums[(size_t)by * N + col] = t;
+}
+
+__global__ __launch_bounds__(256) void w16a16_bias_kernel(const float* __restrict__ sums, int count, int N, float* __restrict__ dbias) {
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    float t = 0.f;
+    for (int i = 0; i < count; ++i) t += sums[(size_t)i * N + n];
+    dbias[n] = t;
+}
+
+// --------------------------------------------------------------------------------------------- launches --
+
+constexpr size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+
+template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
+hipError_t launch_tiles(const ProductArgs& g, hipStream_t st) {
+    constexpr int lds = kSlots * (kBP + kBQ) * 2 * kStepR;
+    static_assert(lds <= 160 * 1024, "the ring fits LDS");
+    const auto kernel = w16a16_product_kernel<kBP, kBQ, kWP, kWQ, kTA, kTB, kSlots>;
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)g.plan.blocks()), dim3(kWP * kWQ * kWave), lds, st, g);
+    return hipGetLastError();
+}
+
+template <bool kTA, bool kTB>
+hipError_t launch_product(ProductArgs g, float* partial, hipStream_t st) {
+    g.plan = plan_product(g.P, g.Q, g.R, kTA, device_cu_count());
+    g.partial = partial;
+    g.e.Q = g.Q;
+    hipError_t e = hipErrorInvalidValue;
+    if (g.plan.bp == 128) e = launch_tiles<128, 128, 2, 2, kTA, kTB, 2>(g, st);
+    if constexpr (!kTA)
+        if (g.plan.bp == 32) e = launch_tiles<32, 128, 1, 4, kTA, kTB, 4>(g, st);
+    if (e != hipSuccess || g.plan.splits == 1) return e;
+    const long long threads = (long long)g.P * ((g.Q + 7) / 8);
+    hipLaunchKernelGGL(w16a16_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, partial, g.plan.splits, g.P, g.e);
+    return hipGetLastError();
+}
+
+size_t partial_bytes(long long P, long long Q, long long R, bool turned) {
+    const ProductPlan pl = plan_product(P, Q, R, turned, device_cu_count());
+    return pl.splits == 1 ? 0 : (size_t)pl.splits * P * ((Q + 7) / 8 * 8) * sizeof(float);
+}
+
+}  // namespace
+
+size_t w16a16_workspace(const qail_w16a16& d, int M) { return partial_bytes(M, d.N, d.K, false); }
+
+hipError_t launch_w16a16(const qail_w16a16& d, const uint16_t* x, int M, const uint16_t* residual, uint16_t* z_out, uint16_t* y, float* y_f32, void* ws,
+                         hipStream_t st) {
+    ProductArgs g = {};
+    g.a = x, g.b = d.weight, g.lda = g.ldb = d.K;
+    g.P = M, g.Q = d.N, g.R = d.K;
+    g.e = {d.bias, residual, z_out, y, y_f32, d.activation, 0};
+    return launch_product<false, false>(g, static_cast<float*>(ws), st);
+}
+
+// The workspace of the backward call: dz, the sums of dz over kDzRows rows each, then the shares of the two products in turn.
+struct BackPlaces {
+    int ld, row_blocks;
+    size_t sums, partial, bytes;
+    BackPlaces(const qail_w16a16& d, int M) {
+        ld = (d.N + 7) / 8 * 8;
+        row_blocks = (M + kDzRows - 1) / kDzRows;
+        sums = round256((size_t)M * ld * 2);
+        partial = sums + round256((size_t)row_blocks * d.N * sizeof(float));
+        bytes = partial + round256(std::max(partial_bytes(M, d.K, d.N, false), partial_bytes(d.N, d.K, M, true)));
+    }
+};
+
+size_t w16a16_back_workspace(const qail_w16a16& d, int M) { return BackPlaces(d, M).bytes; }
+
+hipError_t launch_w16a16_back(const qail_w16a16& d, const uint16_t* x, const uint16_t* z, const uint16_t* dy, const float* dy_f32, int M, uint16_t* dx,
+                              uint16_t* dweight, float* dbias, void* ws, hipStream_t st) {
+    const BackPlaces at(d, M);
+    char* const w = static_cast<char*>(ws);
+    uint16_t* const dz = reinterpret_cast<uint16_t*>(w);
+    float* const sums = reinterpret_cast<float*>(w + at.sums);
+    float* const partial = reinterpret_cast<float*>(w + at.partial);
+    const bool as_it_is = d.activation == QAIL_ACT_NONE && dy && d.N % 8 == 0;   // dz is dy
+    const bool products = dx || dweight;
+    if ((products && !as_it_is) || dbias) {
+        const unsigned blocks = (unsigned)((at.ld + kDzCols - 1) / kDzCols) * (unsigned)at.row_blocks;
+        hipLaunchKernelGGL(w16a16_dz_kernel, dim3(blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, products && !as_it_is ? dz : nullptr,
+                           dbias ? sums : nullptr);
+        if (dbias) hipLaunchKernelGGL(w16a16_bias_kernel, dim3((unsigned)((d.N + 255) / 256)), dim3(256), 0, st, sums, at.row_blocks, d.N, dbias);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const uint16_t* const from = as_it_is ? dy : dz;
+    ProductArgs g = {};
+    if (dx) {
+        g.a = from, g.lda = at.ld, g.b = d.weight, g.ldb = d.K;
+        g.P = M, g.Q = d.K, g.R = d.N;
+        g.e = {nullptr, nullptr, nullptr, dx, nullptr, QAIL_ACT_NONE, 0};
+        const hipError_t e = launch_product<false, true>(g, partial, st);
+        if (e != hipSuccess) return e;
+    }
+    if (dweight) {
+        g.a = from, g.lda = at.ld, g.b = x, g.ldb = d.K;
+        g.P = d.N, g.Q = d.K, g.R = M;
+        g.e = {nullptr, nullptr, nullptr, dweight, nullptr, QAIL_ACT_NONE, 0};
+        const hipError_t e = launch_product<true, true>(g, partial, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace qail
