@@ -1,16 +1,16 @@
 // The next token of each row of logits: temperature, top-k, top-p and min-p, then the inverse of the distribution at a given random number.
 //
-// Every filter keeps a leading part of the tokens in the order (falling logit, rising number).  With key(x) the bits of x in an order of
-// unsigned numbers that part is written as a border: all keys above `key` and the first `ties` tokens with that key.  A border is found without a sort: the
+// Every filter keeps a leading part of the tokens in the order (falling logit, rising number).  That
+// part is written as a border: all tokens above a value and the first `ties` of those with it.  A border is found without a sort: the
 // tokens are counted, or their weights added up, in bins of 1 / 64 of an octave of the weight; the bin in which the sum passes its aim
-// is found, and the few tokens in it are compared with each other.  Where they are more than kList (equal logits) the border is searched by keys instead, kRanges
-// parts of their range at a time.
+// is found, and the few tokens in it are searched by their keys, kRanges parts of their range at a time; where they are more than kList (equal logits) the
+// whole row is.
 //
 // Weights are exponentials in 64 bits, as whole multiples of 2^-44: sums of whole numbers do not depend on their order, and a token is found as in
 // exact arithmetic but for those 2^-44.  In 32 bits the sums would be off by 2^-24 or so of themselves, and of 32000 tokens without a filter one row in some thousands
-// would get a neighbouring one.  An exponential is a table of 64 and a polynomial, which 64 bits cost no more cycles than 32 here.
+// would get a neighbouring one.  An exponential is a table of 512 and a polynomial; 64 bits cost no more cycles than 32 here.
 //
-// One block a row, whose keys stay in registers up to 32768 tokens; a longer row is read again in every pass, and lies in L2 by then.
+// One block a row, whose values stay in registers up to 32768 tokens; a longer row is read again in every pass, and lies in L2 by then.
 #include <type_traits>
 
 #include "qail_internal.h"
@@ -23,14 +23,18 @@ constexpr int kBlock = 1024, kWaves = kBlock / kWave;
 constexpr int kPiece = 8;                          // neighbouring tokens of a thread
 constexpr int kChunk = kBlock * kPiece;            // tokens of a pass over the block
 constexpr int kMostChunks = (1 << 18) / kChunk;
+constexpr int kGroup = 4;                          // chunks that are looked at together
+static_assert(kGroup * kPiece == 32, "a bit for each of a thread's tokens of a group");
 constexpr int kBins = 3 * kBlock;
-constexpr int kParts = 64;                         // of an octave: a bin of weights
+constexpr int kParts = 512;                        // of an octave
+constexpr int kBinParts = 8;                       // of a bin
 constexpr int kLowestPart = -45 * kParts;          // of a weight of 2^-45; below, weights are 0
-static_assert(-kLowestPart < kBins, "a bin for each part");
+constexpr int kLowestBin = (kLowestPart - 1) / kBinParts - 1;
+static_assert(-kLowestBin < kBins, "bins for all parts");
 constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
-constexpr int kList = kBlock;                      // tokens of a bin that are compared with each other
-constexpr int kRanges = 2 * kBlock;
-constexpr int kKept = 2 * kBlock;                  // kept tokens that are listed
+constexpr int kList = kBlock;                      // tokens of a bin that are listed: one a thread
+constexpr int kRanges = kBlock;
+constexpr int kKept = 4 * kBlock;                  // kept tokens of a group that are listed
 
 struct SampleArgs {
     const void* logits;
@@ -53,22 +57,26 @@ constexpr uint32_t kLowest = 0x007FFFFFu, kHighest = 0xFF800000u;   // keys of m
 
 typedef unsigned long long u64;
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int n) {
-    const uint32_t lo = __shfl_up((uint32_t)v, n, kWave), hi = __shfl_up((uint32_t)(v >> 32), n, kWave);
-    return (u64)hi << 32 | lo;
+// v plus, in each lane, the value of the lane that kDpp names (0 where there is none, or the row is not in kRows).
+template <int kDpp, int kRows>
+__device__ __forceinline__ u64 add_from(u64 v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, kDpp, kRows, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), kDpp, kRows, 0xF, false);
+    return v + ((u64)hi << 32 | lo);
 }
-__device__ __forceinline__ u64 shfl64(u64 v, int from) {
-    const uint32_t lo = __shfl((uint32_t)v, from, kWave), hi = __shfl((uint32_t)(v >> 32), from, kWave);
-    return (u64)hi << 32 | lo;
+__device__ __forceinline__ u64 row_scan(u64 v) {     // inclusive sums over 16 lanes
+    v = add_from<0x111, 0xF>(v);                     // row_shr:1, 2, 4, 8
+    v = add_from<0x112, 0xF>(v);
+    v = add_from<0x114, 0xF>(v);
+    return add_from<0x118, 0xF>(v);
 }
-__device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
-    const int lane = threadIdx.x % kWave;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 t = shfl_up64(v, o);
-        if (lane >= o) v += t;
-    }
-    return v;
+__device__ __forceinline__ u64 wave_scan(u64 v) {    // ... over the wave
+    v = row_scan(v);
+    v = add_from<0x142, 0xA>(v);                     // row_bcast:15 into rows 1 and 3
+    return add_from<0x143, 0xC>(v);                  // row_bcast:31 into rows 2 and 3
+}
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
 
 struct Shared {
@@ -77,35 +85,27 @@ struct Shared {
     u64 wave_sum[kWaves];
     u64 segment[kMostChunks * kWaves];       // weight above the border of 512 neighbouring tokens each
     uint32_t ties[kMostChunks * kWaves];     // ... and how many lie on it
-    double part[kParts];                     // 2^(i / 64)
+    double part[kParts];                     // 2^(i / 512)
     union {
-        struct {
-            u64 weight[kList];
-            uint32_t key[kList], number[kList];
-        } in_bin;
         u64 ranges[kRanges];                 // of keys
-        uint2 kept[kKept];                   // key, segment
+        uint32_t list[kKept];                // numbers of tokens
     };
-    uint32_t wave_key[kWaves];
+    float wave_most[kWaves];
     u64 before;                              // what the chosen bin or segment has in front of it
-    int chosen, ties_before, listed, border_ties;
-    uint32_t first, border_key;
+    int chosen, ties_before, listed;
+    uint32_t first;
 };
 
 // Inclusive sums over the block's threads in their order; `total`: of all of them.  The threads have met before.
 __device__ __forceinline__ u64 block_scan(Shared& sh, u64 v, u64& total) {
-    const int wave = threadIdx.x / kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const u64 in = wave_scan(v);
-    if (threadIdx.x % kWave == kWave - 1) sh.wave_sum[wave] = in;
+    if (lane == kWave - 1) sh.wave_sum[wave] = in;
     __syncthreads();
-    u64 front = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const u64 t = sh.wave_sum[w];
-        front += w < wave ? t : 0;
-        total += t;
-    }
+    static_assert(kWaves == 16, "a row of lanes holds the waves' sums");
+    const u64 waves = row_scan(sh.wave_sum[lane % 16]);
+    total = lane_of(waves, 15);
+    const u64 front = wave > 0 ? lane_of(waves, wave - 1) : 0;
     __syncthreads();
     return in + front;
 }
@@ -131,16 +131,15 @@ __device__ __forceinline__ u64 find(Shared& sh, Get get, Aim aim_of) {
     return total;
 }
 
-// The keys of a row, 8 neighbouring tokens of a thread in each of its chunks; kLowest behind the row.  kChunks of them stay in registers; 0: none.
+// The values of a row, 8 neighbouring tokens of a thread in each of its chunks; minus infinity behind the row.  kChunks of them stay in registers; 0: none.
 template <bool kBf16, bool kAligned, int kChunks>
 struct Row {
     const uint8_t* p;
     int V, chunks;
-    uint32_t kept[kChunks > 0 ? kChunks : 1][kPiece];
+    float kept[kChunks > 0 ? kChunks : 1][kPiece];
 
-    __device__ __forceinline__ void read(int c, uint32_t* k) const {
+    __device__ __forceinline__ void values(int c, float* f) const {
         const int j = (c * kBlock + threadIdx.x) * kPiece;
-        float f[kPiece];
         if (kAligned && j + kPiece <= V) {
             if constexpr (kBf16) {
                 unpack8(*reinterpret_cast<const uint4*>(p + 2ll * j), f);
@@ -155,163 +154,203 @@ struct Row {
                        : kBf16    ? bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p)[j + i])
                                   : reinterpret_cast<const float*>(p)[j + i];
         }
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) k[i] = key_of(f[i]);
     }
     __device__ __forceinline__ explicit Row(const void* at, int V_) : p(static_cast<const uint8_t*>(at)), V(V_), chunks((V_ + kChunk - 1) / kChunk) {
         static_assert(kChunks <= 4, "one by one: a loop is unrolled too late for registers");
-        if constexpr (kChunks > 0) read(0, kept[0]);
-        if constexpr (kChunks > 1) read(1, kept[1]);
-        if constexpr (kChunks > 2) read(2, kept[2]);
-        if constexpr (kChunks > 3) read(3, kept[3]);
+        if constexpr (kChunks > 0) values(0, kept[0]);
+        if constexpr (kChunks > 1) values(1, kept[1]);
+        if constexpr (kChunks > 2) values(2, kept[2]);
+        if constexpr (kChunks > 3) values(3, kept[3]);
     }
+    // f(chunk, values) for the kGroup chunks from `first` on, those behind the row among them (minus infinity): unrolled, the loads in front.  For passes that do little with a value.
     template <typename F>
-    __device__ __forceinline__ void each(F f) const {   // f(chunk, keys)
+    __device__ __forceinline__ void group(int first, F f) const {
         if constexpr (kChunks > 0) {
-const auto one = [&](auto chunk) __attribute__((always_inline)) {
-                constexpr int c = decltype(chunk)::value;
-                if constexpr (c < kChunks) {
-                    uint32_t k[kPiece];
-#pragma unroll
-                    for (int i = 0; i < kPiece; ++i) {
-                        k[i] = kept[c][i];
-                        asm volatile("" : "+v"(k[i]));   // else what a pass computes of all keys is kept for the next one, in scratch memory
-                    }
-                    f(c, k);
-                }
-            };
-            one(std::integral_constant<int, 0>{});
-            one(std::integral_constant<int, 1>{});
-            one(std::integral_constant<int, 2>{});
-            one(std::integral_constant<int, 3>{});
+            if constexpr (kChunks > 0) f(0, kept[0]);
+            if constexpr (kChunks > 1) f(1, kept[1]);
+            if constexpr (kChunks > 2) f(2, kept[2]);
+            if constexpr (kChunks > 3) f(3, kept[3]);
         } else {
-            for (int c = 0; c < chunks; ++c) {
-                uint32_t k[kPiece];
-                read(c, k);
-                f(c, k);
-            }
+            float v[kGroup][kPiece];
+            values(first, v[0]);
+            values(first + 1, v[1]);
+            values(first + 2, v[2]);
+            values(first + 3, v[3]);
+            f(first, v[0]);
+            f(first + 1, v[1]);
+            f(first + 2, v[2]);
+            f(first + 3, v[3]);
+        }
+    }
+    // The same for the whole row.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        if constexpr (kChunks > 0) {
+            group(0, f);
+        } else {
+            for (int c = 0; c < chunks; c += kGroup) group(c, f);
+        }
+    }
+    // One bit for each of a thread's tokens of a group, the first one's the highest.
+    template <typename P>
+    __device__ __forceinline__ uint32_t select(int first, P chosen) const {
+        uint32_t bits = 0;
+        group(first, [&](int, const float* x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) bits = bits << 1 | (chosen(x[i]) ? 1u : 0u);
+        });
+        return kChunks > 0 ? bits << (32 - kPiece * kChunks) : bits;
+    }
+    __device__ __forceinline__ float at(uint32_t number) const {
+        if constexpr (kBf16) return bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p)[number]);
+        else return reinterpret_cast<const float*>(p)[number];
+    }
+    // f(chunk, values) for chunks first .. end - 1 from memory.  For passes with exponentials: unrolled over the kept chunks their code is long.
+    template <typename F>
+    __device__ __forceinline__ void each_again(int first, int end, F f) const {
+#pragma unroll 1
+        for (int c = first; c < end; ++c) {
+            float v[kPiece];
+            values(c, v);
+            f(c, v);
         }
     }
 };
 
 struct Weight {
-    double most, inverse, scale;     // the largest logit, 1 / temperature, 64 log2(e) / temperature
+    double most, inverse, scale;     // the largest logit, 1 / temperature, 512 log2(e) / temperature
+    double step;                     // 1 / scale
+    float low;                       // the least value from one part below kLowestPart on: below it weights are 0
     const double* part;
-    __device__ __forceinline__ double down(uint32_t key) const { return ((double)value_of(key) - most) * inverse; }
-    __device__ __forceinline__ double parts(uint32_t key) const { return ((double)value_of(key) - most) * scale; }   // of an octave, below the largest
-    // Of t parts, whose nearest whole number is n >= kLowestPart: 2^(n / 64) from the table, 2^((t - n) / 64) by its series (to 2^-54).  Adding 2^52 rounds
-    // to a whole number, which is then the low bits.
-    __device__ __forceinline__ u64 of(double t, int n) const {
-        const double x = (t - (double)n) * 0.010830424696249145;   // ln(2) / 64
-        double e = fma(x, 1.0 / 120.0, 1.0 / 24.0);
-        e = fma(x, e, 1.0 / 6.0);
-        e = fma(x, e, 0.5);
-        e = fma(x, e, 1.0);
-        e = fma(x, e, 1.0);
-        const double octave = __builtin_bit_cast(double, (u64)(1023 + 44 + (n >> 6)) << 52);
+    __device__ __forceinline__ Weight(float most_, float temperature, const double* part_) : most(most_), part(part_) {
+        inverse = 1.0 / (double)temperature;
+        scale = inverse * 738.65986093514926;
+        step = (double)temperature * 0.0013538030870311431;
+        const double end = most + (kLowestPart - 1) * step;
+        low = fmaxf((float)end, -3.4028235e38f);
+        if ((double)low < end) low = value_of(key_of(low) + 1);
+    }
+    __device__ __forceinline__ double down(float x) const { return ((double)x - most) * inverse; }
+    // x >= low lies n + rest parts of an octave from the largest logit, n the nearest whole number (adding 1.5 * 2^52 rounds to it, in the low bits).
+    __device__ __forceinline__ void parts(float x, int& n, double& rest) const {
+        constexpr double kRound = 6755399441055744.0;
+        const double d = (double)x - most, r = fma(d, scale, kRound);
+        n = (int)(uint32_t)__builtin_bit_cast(u64, r);
+        rest = fma(d, scale, kRound - r);
+    }
+    // The weight of n parts and a rest: 2^(n / 512) from the table, 2^(rest / 512) by its series (to 2^-46).  Adding 2^52 rounds to a whole number, which is
+    // then the low bits.
+    __device__ __forceinline__ u64 of(int n, double rest) const {
+        constexpr double c = 0.0013538030870311431;   // ln(2) / 512
+        double e = fma(rest, c * c * c / 6, c * c / 2);
+        e = fma(rest, e, c);
+        e = fma(rest, e, 1.0);
+        const double octave = __builtin_bit_cast(double, (u64)(uint32_t)(((1023 + 44) << 20) + ((n & -kParts) << (20 - 9))) << 32);
         return __builtin_bit_cast(u64, fma(part[n & (kParts - 1)] * e, octave, 4503599627370496.0)) & ((1ull << 52) - 1);
     }
-    __device__ __forceinline__ int nearest(double t) const { return t < kLowestPart - 1 ? kLowestPart - 1 : (int)rint(t); }
-    __device__ __forceinline__ u64 operator()(uint32_t key) const {
-        const double t = parts(key);
-        const int n = nearest(t);
-        return n < kLowestPart ? 0 : of(t, n);
+    __device__ __forceinline__ u64 operator()(float x) const {
+        int n;
+        double rest;
+        parts(x, n, rest);
+        const u64 w = of(n, rest);
+        return x < low ? 0 : w;
     }
 };
+__device__ __forceinline__ int bin_of(int part) { return -(part >> 3); }   // 0 for the largest logits
+static_assert(kBinParts == 1 << 3 && kParts == 1 << 9, "shifts");
+
+// The numbers of the tokens that a wave's threads have chosen from a group (Row::select) into list[0 .. most), in any order; sh.listed counts them all.
+__device__ __forceinline__ void append(Shared& sh, uint32_t* list, int most, int first, uint32_t bits) {
+    const int lane = threadIdx.x % kWave, mine = __popc(bits);
+    const int upto = (int)wave_scan((u64)mine), total = __builtin_amdgcn_readlane(upto, kWave - 1);
+    if (total == 0) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.listed, total);
+    at = __builtin_amdgcn_readfirstlane(at) + upto - mine;
+    for (; bits != 0; ++at) {
+        const int i = __clz(bits);
+        bits &= ~(0x80000000u >> i);
+        if (at < most) list[at] = ((first + i / kPiece) * kBlock + threadIdx.x) * kPiece + i % kPiece;
+    }
+}
 
 struct Border {
-    uint32_t key;
-    int ties;     // tokens with that key that are kept
+    float value;  // what lies above it is kept
+    int ties;     // ... and so many tokens with that value
 };
 
-// The shortest leading part of the tokens inside `in` whose count (kCount) or weight is at least `aim` (> 0 and no more than all of them have), by their keys.
-template <bool kCount, typename R>
-__device__ __forceinline__ Border border_by_keys(Shared& sh, const R row, uint32_t top, Border in, const Weight weight, u64 aim) {
-    uint32_t base = top;                              // the largest key of the range
-    uint32_t width = top - in.key;                    // ... and how far it goes below
+// The shortest leading part of some tokens whose sum is at least `aim` (> 0 and no more than all of them have), by ranges of their keys.  each(f): f(key, what the
+// token adds to the sum) for a thread's tokens, all of which have keys from low to base; one: what a token of a key adds.
+template <typename Each, typename One>
+__device__ __forceinline__ Border border_by_keys(Shared& sh, Each each, uint32_t base, uint32_t low, u64 aim, One one) {
+    uint32_t width = base - low;                      // base: the largest key of the range; width: how far it goes below
     for (;;) {
-        const int shift = max(0, 21 - __builtin_clz(width | 1));   // width >> shift < kRanges = 2^11
-        for (int i = threadIdx.x; i < kRanges; i += kBlock) sh.ranges[i] = 0;
+        const int shift = max(0, 22 - __builtin_clz(width | 1));   // width >> shift < kRanges = 2^10
+        sh.ranges[threadIdx.x] = 0;
         __syncthreads();
-        row.each([&](int, const uint32_t* k) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (k[i] > in.key && k[i] <= base && base - k[i] <= width) atomicAdd(&sh.ranges[(base - k[i]) >> shift], kCount ? 1ull : weight(k[i]));
+        each([&](uint32_t key, u64 adds) __attribute__((always_inline)) {
+            if (key <= base && base - key <= width) atomicAdd(&sh.ranges[(base - key) >> shift], adds);
         });
         __syncthreads();
-        if (threadIdx.x == 0 && in.ties > 0 && in.key <= base && base - in.key <= width)
-            sh.ranges[(base - in.key) >> shift] += (u64)in.ties * (kCount ? 1ull : weight(in.key));
-        __syncthreads();
-        find<2>(sh, [&](int i) { return sh.ranges[i]; }, [&](u64) { return aim; });
+        find<1>(sh, [&](int i) { return sh.ranges[i]; }, [&](u64) { return aim; });
         const uint32_t at = sh.chosen;
         aim -= sh.before;
         __syncthreads();
         base -= at << shift;
-        if (shift == 0) return {base, (int)(kCount ? aim : (aim - 1) / weight(base) + 1)};
+        if (shift == 0) return {value_of(base), (int)((aim - 1) / one(base) + 1)};
         width = min(width - (at << shift), (1u << shift) - 1);
     }
 }
 
-// The same where it lies in a bin of weights, whose tokens are to count or weigh `aim` > 0; ahead: what those up to the border weigh.  false: the bin has
+// The border in a bin of weights, whose tokens are to count (kCount) or weigh `aim` > 0; ahead: what those up to the border weigh (with kWeigh).  false: the bin has
 // more than about kList tokens.
-template <bool kCount, typename R>
+template <bool kCount, bool kWeigh, typename R>
 __device__ __forceinline__ bool border_in_bin(Shared& sh, const R& row, int bin, const Weight& weight, u64 aim, Border& b, u64& ahead) {
-    // the bin's keys, and two more at either end for the roundings of its bounds; they are looked at one by one below
-    const uint32_t hi = key_of((float)(weight.most + (0.5 - bin) / weight.scale)), lo = key_of((float)(weight.most - (0.5 + bin) / weight.scale));
-    const uint32_t from = max(lo - 2, kLowest + 1), to = min(hi + 2, kHighest - 1);
+    // the bin's values, and two keys more at either end for the roundings of its bounds; they are looked at one by one below
+    const uint32_t hi = key_of((float)(weight.most + (kBinParts - 0.5 - kBinParts * bin) * weight.step)) + 2;
+    const uint32_t lo = key_of((float)(weight.most - (0.5 + kBinParts * bin) * weight.step)) - 2;
+    const float from = value_of(max(lo, kLowest + 1)), to = value_of(min(hi, kHighest - 1));
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    row.each([&](int c, const uint32_t* k) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i)
-            if (k[i] >= from && k[i] <= to) {
-                const int at = atomicAdd(&sh.listed, 1);
-                if (at < kList) sh.in_bin.key[at] = k[i], sh.in_bin.number[at] = (c * kBlock + threadIdx.x) * kPiece + i;
-            }
-    });
+    for (int g = 0; g < row.chunks; g += kGroup)
+        append(sh, sh.list, kList, g, row.select(g, [&](float x) { return __builtin_amdgcn_fmed3f(x, from, to) == x; }));
     __syncthreads();
     const int n = sh.listed;
     if (n > kList) {
         __syncthreads();
         return false;
     }
-    uint32_t key = 0, number = 0;
+    uint32_t key = 0;
     u64 mine = 0;
+    bool held = false;
     if ((int)threadIdx.x < n) {
-        key = sh.in_bin.key[threadIdx.x], number = sh.in_bin.number[threadIdx.x];
-        const double t = weight.parts(key);
-        const int part = weight.nearest(t);
-        if (-part == bin) mine = weight.of(t, part);
-        else sh.in_bin.key[threadIdx.x] = key = 0;
-        sh.in_bin.weight[threadIdx.x] = mine;
+        const float x = row.at(sh.list[threadIdx.x]);
+        int part;
+        double rest;
+        weight.parts(x, part, rest);
+        held = x >= weight.low && bin_of(part) == bin;
+        key = key_of(x);
+        mine = weight.of(part, rest);
     }
-    __syncthreads();
-    if (key != 0) {
-        u64 front = 0, heavy = 0;
-        int equal = 0;
-        for (int i = 0; i < n; ++i) {
-            const uint32_t other = sh.in_bin.key[i];
-            const bool before = other > key || (other == key && sh.in_bin.number[i] < number);
-            front += before ? 1 : 0;
-            heavy += before ? sh.in_bin.weight[i] : 0;
-            equal += before && other == key;
-        }
-        const u64 at = kCount ? front : heavy;
-        if (at < aim && aim <= at + (kCount ? 1 : mine)) sh.border_key = key, sh.border_ties = equal + 1, sh.before = heavy + mine;   // one thread
+    __syncthreads();                                  // the list has been read: the ranges lie there as well
+    b = border_by_keys(
+        sh,
+        [&](auto f) __attribute__((always_inline)) {
+            if (held) f(key, kCount ? 1 : mine);
+        },
+        key_of(to), key_of(from), aim, [&](uint32_t k) { return kCount ? 1 : weight(value_of(k)); });
+    if constexpr (kWeigh) {
+        block_scan(sh, held && key > key_of(b.value) ? mine : 0, ahead);
+        ahead += (u64)b.ties * weight(b.value);
     }
-    __syncthreads();
-    b = {sh.border_key, sh.border_ties};
-    ahead = sh.before;
-    __syncthreads();
     return true;
 }
 
 template <bool kBf16, bool kAligned, int kChunks>
 __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     __shared__ Shared sh;
-    const int r = blockIdx.x, V = a.V, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int r = blockIdx.x, V = a.V, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const Row<kBf16, kAligned, kChunks> row(static_cast<const uint8_t*>(a.logits) + (long long)r * a.stride * (kBf16 ? 2 : 4), V);
-    const Row<kBf16, kAligned, 0> again(row.p, V);   // the same from memory
     const float temperature = a.s.temperature ? a.s.temperature[r] : 1.f, top_p = a.s.top_p ? a.s.top_p[r] : 1.f, min_p = a.s.min_p ? a.s.min_p[r] : 0.f;
     const float u = a.u[r];
     const int top_k = a.s.top_k ? a.s.top_k[r] : 0;
@@ -319,19 +358,23 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     for (int i = threadIdx.x; i < kBins; i += kBlock) sh.bins[i] = 0, sh.counts[i] = 0;
     if (threadIdx.x < kParts) sh.part[threadIdx.x] = exp2((double)threadIdx.x / kParts);
     if (threadIdx.x == 0) sh.first = 0xFFFFFFFFu;
-    uint32_t most = 0;
-    row.each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+    float mine = -__builtin_inff();
+    bool bad = false;
+    row.each([&](int, const float* x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) most = max(most, k[i]);
+        for (int i = 0; i < kPiece; ++i) {
+            mine = fmaxf(mine, x[i]);                                  // (passes by NaN)
+            bad |= x[i] != x[i];
+        }
     });
-    uint32_t m = most;
+    float m = bad ? __builtin_inff() : mine;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
-    if (lane == 0) sh.wave_key[wave] = m;
+    for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+    if (lane == 0) sh.wave_most[wave] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = max(m, sh.wave_key[w]);
-    const bool numbers = m > kLowest && m < kHighest && temperature >= 0.f && temperature <= 3.4028235e38f && top_p == top_p && min_p == min_p;
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sh.wave_most[w]);
+    const bool numbers = m >= -3.4028235e38f && m <= 3.4028235e38f && temperature >= 0.f && temperature <= 3.4028235e38f && top_p == top_p && min_p == min_p;
     if (!numbers || (temperature > 0.f && !(u >= 0.f && u < 1.f))) {   // the same for the whole block, as all that follows
         if (threadIdx.x == 0) {
             a.token[r] = -1;
@@ -341,14 +384,10 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
         return;
     }
     if (temperature == 0.f || min_p > 1.f || top_k == 1) {             // the first of the order
-        if (most == m) {
-            uint32_t place = 0xFFFFFFFFu;
-            row.each([&](int c, const uint32_t* k) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i)
-                    if (k[i] == m) place = min(place, (uint32_t)((c * kBlock + threadIdx.x) * kPiece + i));
-            });
-            atomicMin(&sh.first, place);
+        for (int g = 0; g < row.chunks; g += kGroup) {
+            const uint32_t bits = row.select(g, [&](float x) { return x == m; });
+            const int i = bits != 0 ? __clz(bits) : 0;
+            if (bits != 0) atomicMin(&sh.first, ((g + i / kPiece) * kBlock + threadIdx.x) * kPiece + i % kPiece);
         }
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -358,56 +397,73 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
         return;
     }
 
-    const double inverse = 1.0 / (double)temperature;
-    const Weight weight = {(double)value_of(m), inverse, inverse * 92.332482616893658, sh.part};   // 64 log2(e)
+    const Weight weight(m, temperature, sh.part);
     const bool by_count = top_k > 0 && top_k < V, by_share = top_p < 1.f;
-    Border b = {kLowest, 0};
+    Border b = {-__builtin_inff(), 0};
     u64 kept = 0;                      // what the first top_k weigh
-    if (by_count || by_share) {
-        row.each([&](int, const uint32_t* k) __attribute__((always_inline)) {
+    const auto all_keys = [&](bool weigh) {   // of the row, for where a bin has too many tokens
+        return [&, weigh](auto f) __attribute__((always_inline)) {
+            row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
+#pragma unroll 1
+                for (int i = 0; i < kPiece; ++i)
+                    if (x[i] >= weight.low) f(key_of(x[i]), weigh ? weight(x[i]) : 1);
+            });
+        };
+    };
+    if (by_share) {
+        row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) {
-                const double t = weight.parts(k[i]);
-                const int n = weight.nearest(t);
-                if (n < kLowestPart) continue;
-                if (by_share) atomicAdd(&sh.bins[-n], weight.of(t, n));
-                if (by_count) atomicAdd(&sh.counts[-n], 1u);
-            }
+            for (int i = 0; i < kPiece; ++i)
+                if (x[i] >= weight.low) {
+                    int n;
+                    double rest;
+                    weight.parts(x[i], n, rest);
+                    atomicAdd(&sh.bins[bin_of(n)], weight.of(n, rest));
+                }
         });
-        __syncthreads();
     }
+    if (by_count) {
+        row.each([&](int, const float* x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i)
+                if (x[i] >= weight.low) {
+                    int n;
+                    double rest;
+                    weight.parts(x[i], n, rest);
+                    atomicAdd(&sh.counts[bin_of(n)], 1u);
+                }
+        });
+    }
+    __syncthreads();
     if (by_count) {
         const u64 counted = find<kBins / kBlock>(sh, [&](int i) { return (u64)sh.counts[i]; }, [&](u64) { return (u64)top_k; });
         if (counted >= (u64)top_k) {   // else all that has a weight is among the first top_k
             const int bin = sh.chosen;
             const u64 aim = (u64)top_k - sh.before;
             __syncthreads();
-            if (border_in_bin<true>(sh, row, bin, weight, aim, b, kept)) {
-                if (by_share) {
-                    u64 mine = 0, front;
-                    for (int i = threadIdx.x; i < bin; i += kBlock) mine += sh.bins[i];
-                    block_scan(sh, mine, front);
-                    kept += front;
-                }
-            } else {
-                b = border_by_keys<true>(sh, again, m, {kLowest, 0}, weight, (u64)top_k);
-                if (by_share) {
-                    u64 mine = 0;
-                    again.each([&](int, const uint32_t* k) __attribute__((always_inline)) {
-#pragma unroll
+            if (!(by_share ? border_in_bin<true, true>(sh, row, bin, weight, aim, b, kept) : border_in_bin<true, false>(sh, row, bin, weight, aim, b, kept))) {
+                b = border_by_keys(sh, all_keys(false), key_of(m), kLowest, (u64)top_k, [&](uint32_t) { return 1; });
+                u64 some = 0;
+                if (by_share)
+                    row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
+#pragma unroll 1
                         for (int i = 0; i < kPiece; ++i)
-                            if (k[i] > b.key) mine += weight(k[i]);
+                            if (x[i] > b.value) some += weight(x[i]);
                     });
-                    block_scan(sh, mine, kept);
-                    kept += (u64)b.ties * weight(b.key);
-                }
+                block_scan(sh, some, kept);
+                kept += (u64)b.ties * weight(b.value);
+            } else if (by_share) {
+                u64 some = 0, front;
+                for (int i = threadIdx.x; i < bin; i += kBlock) some += sh.bins[i];
+                block_scan(sh, some, front);
+                kept += front;
             }
         } else {
             __syncthreads();
         }
     }
     if (by_share) {
-        u64 aim = 0, ahead;
+        u64 aim = 0, none;
         find<kBins / kBlock>(sh, [&](int i) { return sh.bins[i]; }, [&](u64 total) {
             const double share = ceil((double)top_p * (double)(b.ties > 0 ? kept : total));
             return aim = share > 1.0 ? (u64)share : 1;
@@ -415,76 +471,84 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
         const int bin = sh.chosen;
         const u64 rest = aim - sh.before;
         __syncthreads();
-        const Border in = b;
-        if (!border_in_bin<false>(sh, row, bin, weight, rest, b, ahead)) b = border_by_keys<false>(sh, again, m, in, weight, aim);
+        // (the border of top_k, which may lie in the same bin, is not reached: the aim is less than what is in front of it weighs)
+        if (!border_in_bin<false, false>(sh, row, bin, weight, rest, b, none))
+            b = border_by_keys(sh, all_keys(true), key_of(m), kLowest, aim, [&](uint32_t k) { return weight(value_of(k)); });
     }
 
     // The kept weight of every 512 neighbouring tokens, then the one in which the sum passes u.  Where few are kept they are listed first, so that no
     // exponential is computed for the others beside them.
+    const bool filtered = by_count || by_share || min_p > 0.f;
     const double least = min_p > 0.f ? log((double)min_p) : -__builtin_inf();
-    const u64 on = b.ties > 0 && weight.down(b.key) >= least ? weight(b.key) : 0;
-    const uint32_t low = min_p > 0.f ? key_of((float)(weight.most + least * (double)temperature)) - 2 : 0;   // no key below it is kept: two steps for its rounding
+    const u64 on = b.ties > 0 && weight.down(b.value) >= least ? weight(b.value) : 0;
+    float low = fmaxf(weight.low, b.ties > 0 ? value_of(key_of(b.value) + 1) : b.value);   // what is kept beside the ties; of min_p's border two steps below for its rounding
+    if (min_p > 0.f) low = fmaxf(low, value_of(max(key_of((float)(weight.most + least * (double)temperature)), kLowest + 3) - 2));
+    const float from = on > 0 ? fminf(low, b.value) : low;   // (between them there may be what min_p does not keep)
     const int segments = row.chunks * kWaves;           // at most 512: one a thread
-    if (threadIdx.x == 0) sh.listed = 0;
     if ((int)threadIdx.x < segments) sh.segment[threadIdx.x] = 0, sh.ties[threadIdx.x] = 0;
-    __syncthreads();
-    if (by_count || by_share || min_p > 0.f) {
-        row.each([&](int c, const uint32_t* k) __attribute__((always_inline)) {
-            uint32_t ties = 0;
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i) {
-                ties += __popcll(__ballot(k[i] == b.key));
-                const bool keep = k[i] > b.key && k[i] >= low;
-                const u64 all = __ballot(keep);
-                if (all == 0) continue;
-                int at = 0;
-                if (lane == 0) at = atomicAdd(&sh.listed, __popcll(all));
-                at = __shfl(at, 0, kWave) + __popcll(all & ((1ull << lane) - 1));
-                if (keep && at < kKept) sh.kept[at] = make_uint2(k[i], c * kWaves + wave);
+    for (int g = 0; g < row.chunks; g += kGroup) {
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+        if (filtered) append(sh, sh.list, kKept, g, row.select(g, [&](float x) { return x >= from; }));
+        __syncthreads();
+        const int listed = sh.listed;
+        if (filtered && listed <= kKept) {
+            for (int i = threadIdx.x; i < listed; i += kBlock) {
+                const uint32_t number = sh.list[i], at = number / (kWave * kPiece);
+                const float x = row.at(number);
+                if (x < low) {
+                    atomicAdd(&sh.ties[at], x == b.value ? 1u : 0u);
+                } else if (weight.down(x) >= least) {
+                    atomicAdd(&sh.segment[at], weight(x));
+                }
             }
-            if (lane == 0 && c < row.chunks) sh.ties[c * kWaves + wave] = ties;
-        });
+        } else {
+            row.each_again(g, min(g + kGroup, row.chunks), [&](int c, const float* x) __attribute__((always_inline)) {
+                u64 some = 0;
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) {
+                    const u64 w = weight(x[i]);
+                    some += x[i] >= low && weight.down(x[i]) >= least ? w : 0;
+                }
+                some = lane_of(wave_scan(some), kWave - 1);
+                if (lane == 0) sh.segment[c * kWaves + wave] = some;
+            });
+            if (b.ties > 0) {
+                const uint32_t bits = row.select(g, [&](float x) { return x == b.value; });
+                u64 four = 0;                           // a chunk's count in 16 bits each
+#pragma unroll
+                for (int c = 0; c < kGroup; ++c) four |= (u64)__popc(bits >> (24 - kPiece * c) & 0xFFu) << (16 * c);
+                four = lane_of(wave_scan(four), kWave - 1);
+                if (lane < kGroup && g + lane < row.chunks) sh.ties[(g + lane) * kWaves + wave] = four >> (16 * lane) & 0xFFFF;
+            }
+        }
         __syncthreads();
     }
-    const int listed = sh.listed;
-    if ((by_count || by_share || min_p > 0.f) && listed <= kKept) {
-        for (int i = threadIdx.x; i < listed; i += kBlock) {
-            const uint2 t = sh.kept[i];
-            if (weight.down(t.x) >= least) atomicAdd(&sh.segment[t.y], weight(t.x));
-        }
-    } else {
-        row.each([&](int c, const uint32_t* k) __attribute__((always_inline)) {
-            u64 mine = 0;
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i)
-                if (k[i] > b.key && k[i] >= low && weight.down(k[i]) >= least) mine += weight(k[i]);
-            mine = shfl64(wave_scan(mine), kWave - 1);
-            if (lane == 0 && c < row.chunks) sh.segment[c * kWaves + wave] = mine;
-        });
-    }
-    __syncthreads();
     const bool held = (int)threadIdx.x < segments;
-    const u64 above = held ? sh.segment[threadIdx.x] : 0, equal = held ? sh.ties[threadIdx.x] : 0, room = b.ties;
-    u64 all;
-    const u64 ties_upto = block_scan(sh, equal, all), ties_front = ties_upto - equal;
-    const u64 here = above + ((ties_upto < room ? ties_upto : room) - (ties_front < room ? ties_front : room)) * on;
+    const u64 above = held ? sh.segment[threadIdx.x] : 0, room = b.ties;
+    u64 ties_front = 0, here = above, all;
+    if (b.ties > 0) {                                   // else nobody asks
+        const u64 equal = held ? sh.ties[threadIdx.x] : 0, ties_upto = block_scan(sh, equal, all);
+        ties_front = ties_upto - equal;
+        here += (min(ties_upto, room) - min(ties_front, room)) * on;
+    }
     const u64 upto = block_scan(sh, here, all);
     const u64 aim = (u64)((double)u * (double)all);
     if (upto - here <= aim && aim < upto) sh.chosen = threadIdx.x, sh.before = upto - here, sh.ties_before = (int)ties_front;
     __syncthreads();
     if (wave != sh.chosen % kWaves) return;
     const int c = sh.chosen / kWaves;
-    uint32_t k[kPiece];
-    again.read(c, k);
+    float x[kPiece];
+    row.values(c, x);
     u64 equal_here = 0;
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) equal_here += k[i] == b.key;
+    for (int i = 0; i < kPiece; ++i) equal_here += x[i] == b.value;
     u64 number = sh.ties_before + wave_scan(equal_here) - equal_here;
     u64 w[kPiece], sum = 0;
 #pragma unroll
     for (int i = 0; i < kPiece; ++i) {
-        w[i] = k[i] > b.key ? (weight.down(k[i]) >= least ? weight(k[i]) : 0) : k[i] == b.key && number < room ? on : 0;
-        number += k[i] == b.key;
+        w[i] = x[i] >= low ? (weight.down(x[i]) >= least ? weight(x[i]) : 0) : x[i] == b.value && number < room ? on : 0;
+        number += x[i] == b.value;
         sum += w[i];
     }
     u64 at = sh.before + wave_scan(sum) - sum;
@@ -492,7 +556,7 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     for (int i = 0; i < kPiece; ++i) {
         if (at <= aim && aim < at + w[i]) {              // one token
             a.token[r] = (c * kBlock + threadIdx.x) * kPiece + i;
-            if (a.logprob) a.logprob[r] = (float)(weight.down(k[i]) - log((double)all / kOne));
+            if (a.logprob) a.logprob[r] = (float)(weight.down(x[i]) - log((double)all / kOne));
         }
         at += w[i];
     }

@@ -152,6 +152,18 @@ def test_rows_of_wider_tensors(B, dtype):
     check(B, wide[::2, :777], randoms(3, 4), None, [20] * 3)
 
 
+def test_temperatures_next_to_the_steps_of_the_logits(B):
+    """Neighbouring logits whose distance is tens of temperatures: the next one's weight is around the least that counts, and below."""
+    for most in (1e6, -1e6, 37.0):
+        step = np.spacing(np.float32(most))
+        x = torch.tensor([[most - i * step for i in range(40)]], dtype=torch.float32, device="cuda").expand(60, -1).contiguous()
+        t = [abs(float(step)) / d for d in np.linspace(0.5, 60.0, 60)]
+        for k, p in ((None, None), ([3] * 60, None), (None, [0.97] * 60), ([3] * 60, [0.97] * 60)):
+            check(B, x, randoms(60, 8), t, k, p)
+            check(B, x, [1 - 2.0 ** -24] * 60, t, k, p)
+    check(B, rows(4, 500, 1, torch.float32), randoms(4, 1), [1e-45, 1e-38, 3e38, 1e30], [0, 20, 0, 20], [0.9] * 4)
+
+
 def test_frequencies(B):
     """64 equal steps of u over one row: the tokens come as often as their probabilities say, to one step."""
     p = torch.tensor([0.5, 0.25, 0.125, 0.0625, 0.0625], device="cuda")
