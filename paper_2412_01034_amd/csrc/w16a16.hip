@@ -22,36 +22,75 @@ __host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4
 
 // ------------------------------------------------------------------------------------------------ activations --
 
+// A tile has as many outputs as its waves have cycles to spare, so these are short: products and sums with one rounding, the hardware's 2^x and 1 / x
+// (1 ulp each).  Relative errors are about 2^-21 everywhere; the arguments of exponentials are kept in two parts, since 2^x loses 2^-24 x.
+
+// exp(x); 0 and infinity beyond 126.
+__device__ __forceinline__ float exp_of(float x) {
+    constexpr float k = 1.44269504f, k_lo = 1.92596299e-8f;   // log2(e)
+    x = __builtin_amdgcn_fmed3f(x, -126.f, 126.f);
+    const float hi = x * k, lo = fmaf(x, k, -hi) + x * k_lo;
+    return __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147181f, 1.f);
+}
+
+// x = |z| <= 20: exp(-z^2 / 2), and beside it erfc(x / sqrt(2)) / 2, the share of the normal distribution beyond x.  erfc(v) exp(v^2) is t P(t), t = 1 / (1 + 0.3 v), with
+// a polynomial of degree 8 that is fitted to v <= 10 with the least largest relative error (2^-25.6).
+__device__ __forceinline__ float normal_tail(float x, float& bell) {
+    constexpr float k = -0.721347520f, k_lo = -9.62981495e-9f;   // -log2(e) / 2
+    const float s = x * x, s_lo = fmaf(x, x, -s), hi = s * k, lo = fmaf(s, k, -hi) + fmaf(s_lo, k, s * k_lo);
+    bell = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147181f, 1.f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(x, 0.212132034f, 1.f));
+    float q = -0.0647618126f;
+    q = fmaf(q, t, 0.242783429f);
+    q = fmaf(q, t, -0.256142925f);
+    q = fmaf(q, t, 0.273864594f);
+    q = fmaf(q, t, -0.0473286336f);
+    q = fmaf(q, t, 0.107464472f);
+    q = fmaf(q, t, 0.0741692019f);
+    q = fmaf(q, t, 0.0853576683f);
+    q = fmaf(q, t, 0.0845939992f);
+    return q * t * bell;
+}
+
+__device__ __forceinline__ float gelu_tanh_argument(float z) { return z * fmaf(0.0713548163f * z, z, 1.59576912f); }   // (1 + tanh(v / 2)) / 2 = 1 / (1 + exp(-v))
+
 __device__ __forceinline__ float activated(int act, float z) {
     switch (act) {
-        case QAIL_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-        case QAIL_ACT_GELU: return 0.5f * z * erfcf(-0.70710678f * z);       // 1 + erf(v) = erfc(-v): no cancellation below zero
-        case QAIL_ACT_GELU_TANH: {
-            const float v = 1.5957691f * (z + 0.044715f * z * z * z);        // (1 + tanh(v / 2)) / 2 = 1 / (1 + exp(-v))
-            return z / (1.f + expf(-v));
+        case QAIL_ACT_RELU: return z < 0.f ? 0.f : z;
+        case QAIL_ACT_GELU: {
+            float bell;
+            const float h = normal_tail(fminf(fabsf(z), 20.f), bell);
+            return z > 0.f ? fmaf(-z, h, z) : z * h;
         }
-        case QAIL_ACT_SILU: return z / (1.f + expf(-z));
+        case QAIL_ACT_GELU_TANH: return z * __builtin_amdgcn_rcpf(1.f + exp_of(-gelu_tanh_argument(z)));
+        case QAIL_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
         default: return z;
     }
 }
 
+// act'(z).  Terms that vanish far out are taken at the ends of the range in which they do not, so that no infinity meets a zero.
 __device__ __forceinline__ float slope(int act, float z) {
+    float r;
     switch (act) {
-        case QAIL_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case QAIL_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
         case QAIL_ACT_GELU: {
-            const float p = 0.5f * erfcf(-0.70710678f * z), d = expf(-0.5f * z * z);
-            return d > 0.f ? p + 0.39894228f * z * d : p;
+            float bell;
+            const float near = __builtin_amdgcn_fmed3f(z, -20.f, 20.f), h = normal_tail(fabsf(near), bell);
+            r = fmaf(0.398942280f * near, bell, z > 0.f ? 1.f - h : h);
+            break;
         }
-        case QAIL_ACT_GELU_TANH: {
-            const float v = 1.5957691f * (z + 0.044715f * z * z * z), s = 1.f / (1.f + expf(-v)), t = 1.f / (1.f + expf(v));
-            return s * t > 0.f ? s + z * (s * t) * 1.5957691f * (1.f + 0.134145f * z * z) : s;   // (no zero times an infinity)
-        }
+        case QAIL_ACT_GELU_TANH:
         case QAIL_ACT_SILU: {
-            const float s = 1.f / (1.f + expf(-z)), t = 1.f / (1.f + expf(z));
-            return s * t > 0.f ? s + z * (s * t) : s;
+            const float near = __builtin_amdgcn_fmed3f(z, -80.f, 80.f);
+            const float v = act == QAIL_ACT_SILU ? near : __builtin_amdgcn_fmed3f(gelu_tanh_argument(near), -80.f, 80.f);
+            const float dv = act == QAIL_ACT_SILU ? 1.f : fmaf(0.214064449f * near, near, 1.59576912f);
+            const float e = exp_of(-v), share = __builtin_amdgcn_rcpf(1.f + e);
+            r = fmaf(near * dv, share * (e * share), share);
+            break;
         }
         default: return 1.f;
     }
+    return z != z ? z : r;
 }
 
 // ------------------------------------------------------------------------------------------------- epilogue --
@@ -132,14 +171,14 @@ __device__ __forceinline__ void copy16_from(const void* p, uint32_t lds) {
 
 // One operand's part of a step in LDS: kB rows (p or q) of 64 r.  Straight: kB rows of 128 bytes, piece s (16 bytes) of row i at s ^ (i & 7), so
 // that 8 consecutive rows' reads of one s hit 8 places.  Turned: 64 rows (r) of 2 kB bytes, piece s of row i at s ^ ((i & 3) << 2): a transposed read takes
-// 64 bytes of each of four rows, which lie in four places of 256 bytes then.
+// 64 bytes of each of four rows, which lie in four places of 256 bytes then (of 128, two rows, where kB is 64).
 template <int kB, bool kTurned, int kThreads>
 struct Operand {
     static constexpr int kBytes = kB * 2 * kStepR;
     static constexpr int kLoads = kBytes / 16 / kThreads;
     static constexpr int kPieces = kTurned ? kB / 8 : kStepR / 8;   // of a row
-    static_assert(kLoads * 16 * kThreads == kBytes && (!kTurned || kB >= 128), "whole loads, whole swizzles");
-    __device__ static __forceinline__ int place(int row, int piece) { return piece ^ (kTurned ? (row & 3) << 2 : row & 7); }
+    static_assert(kLoads * 16 * kThreads == kBytes && (!kTurned || kB >= 64), "whole loads, whole swizzles");
+    __device__ static __forceinline__ int place(int row, int piece) { return piece ^ (!kTurned ? row & 7 : kB == 64 ? (row & 2) << 1 : (row & 3) << 2); }
 
     const uint16_t* base;     // row 0 of the tile (straight) or its column 0 in row 0 (turned), at r = 0
     long long ld;
@@ -198,8 +237,7 @@ struct Operand {
 };
 
 // kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied.
-// The matrix cores get B's rows as rows: a lane then has one p and groups of four neighbouring q, and after an exchange between the wave's
-// halves eight, the 16 bytes of an output row.
+// The matrix cores get B's rows as rows: a lane then has one p and groups of four neighbouring q.
 template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
 __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a16_product_kernel(const ProductArgs g) {
     constexpr int kThreads = kWP * kWQ * kWave, FP = kBP / kWP / 32, FQ = kBQ / kWQ / 32;
@@ -216,67 +254,94 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
     const uint32_t lds = lds_addr(ring);
 
     f32x16_t acc[FP][FQ] = {};
+    bf16x8_t fa[2][FP] = {}, fb[2][FQ] = {};
     auto load = [&](int i) {
         const int slot = i % kSlots;
         a.load(first + i, lds + slot * kSlot);
         b.load(first + i, lds + slot * kSlot + A::kBytes);
     };
-#pragma unroll
-    for (int i = 0; i < kSlots - 1; ++i)
-        if (i < steps) load(i);
-    for (int i = 0; i < steps; ++i) {
-        // step i is there once at most the later ones are on their way; after the barrier all waves' parts of it are, and nobody reads step i - 1
-        const int later = steps - 1 - i;
-        if (kSlots >= 4 && later >= 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kLoads));
-        else if (kSlots >= 3 && later >= 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
+    // All of the steps up to i have arrived (at most kSlots - 1 later ones are on their way), and nobody reads the step in front of them.
+    auto wait_for = [&](int i, int issued) {
+        const int later = min(issued, steps) - 1 - i;
+        static_assert(kSlots == 2 || kSlots == 4, "");
+        if (kSlots == 4 && later >= 3) __builtin_amdgcn_s_waitcnt(waitcnt_vm(3 * kLoads));
+        else if (kSlots == 4 && later == 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kLoads));
+        else if (later >= 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoads));
         else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         asm volatile("s_barrier" ::: "memory");
-        if (i + kSlots - 1 < steps) load(i + kSlots - 1);
+    };
+    auto multiply = [&](int set) {
+#pragma unroll
+        for (int x = 0; x < FP; ++x)
+#pragma unroll
+            for (int y = 0; y < FQ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][y], fa[set][x], acc[x][y], 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i)
+        if (i < steps) load(i);
+    wait_for(0, kSlots);
+    // The fragments of 16 r are read while those before them are multiplied, the first ones of a step beside the last products of the step before
+    // (zeros at the beginning), so that the matrix cores do not wait for the barrier's reads.
+    for (int i = 0; i < steps; ++i) {
         const uint8_t* const sa = ring + i % kSlots * kSlot;
         const uint8_t* const sb = sa + A::kBytes;
 #pragma unroll
         for (int kk = 0; kk < kStepR / 16; ++kk) {
-            bf16x8_t fa[FP], fb[FQ];
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) fb[j] = Bo::fragment(sb, wq + 32 * j, kk, lane);
+            for (int j = 0; j < FQ; ++j) fb[kk % 2][j] = Bo::fragment(sb, wq + 32 * j, kk, lane);
 #pragma unroll
-            for (int j = 0; j < FP; ++j) fa[j] = A::fragment(sa, wp + 32 * j, kk, lane);
+            for (int j = 0; j < FP; ++j) fa[kk % 2][j] = A::fragment(sa, wp + 32 * j, kk, lane);
+            multiply((kk + 1) % 2);
+            constexpr int kReads = FP * (kTA ? 2 : 1) + FQ * (kTB ? 2 : 1), kProducts = FP * FQ;
 #pragma unroll
-            for (int x = 0; x < FP; ++x)
-#pragma unroll
-                for (int y = 0; y < FQ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[y], fa[x], acc[x][y], 0, 0, 0);
-        }
-    }
-
-    const int Q8 = (g.Q + 7) / 8 * 8;
-#pragma unroll
-    for (int x = 0; x < FP; ++x) {
-        const int p = p0 + wp + 32 * x + lane % 32;
-#pragma unroll
-        for (int y = 0; y < FQ; ++y) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int q = q0 + wq + 32 * y + 16 * h + 8 * (lane / 32);
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float a0 = acc[x][y][8 * h + i], a1 = acc[x][y][8 * h + 4 + i];   // (a bit cast of a vector's element takes its first)
-                    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a0), __builtin_bit_cast(unsigned, a1), false, false);
-                    const unsigned lo = r[0], hi = r[1];
-                    v[i] = __builtin_bit_cast(float, lo);
-                    v[4 + i] = __builtin_bit_cast(float, hi);
-                }
-                if (p < g.P && q < g.Q) {
-                    if (g.plan.splits == 1) {
-                        finish8(g.e, p, q, v);
-                    } else {
-                        float4* const to = reinterpret_cast<float4*>(g.partial + ((size_t)t.split * g.P + p) * Q8 + q);
-                        to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                        to[1] = make_float4(v[4], v[5], v[6], v[7]);
-                    }
+            for (int j = 0; j < kProducts; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a product, then its share of the reads
+                if (kReads * (j + 1) / kProducts > kReads * j / kProducts) {
+                    if (kReads * (j + 1) / kProducts - kReads * j / kProducts == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 }
             }
         }
+        if (i + 1 < steps) {
+            wait_for(i + 1, i + kSlots);
+            if (i + kSlots < steps) load(i + kSlots);
+        }
+    }
+    multiply(1);
+
+    // Out through LDS, 32 rows of a wave at a time: the lanes then have 8 neighbouring outputs of a row, a row's lanes lie beside each other, and the
+    // epilogue is a loop (unrolled over the registers its code was ten times the instruction cache).  Piece c (16 bytes) of row p lies at c ^ (p & 15).
+    constexpr int kRow = 32 * FQ, kPiecesOut = kRow / 4, kLanes = kRow / 8;   // floats and pieces of a row; lanes that share one
+    static_assert(kWP * kWQ * 32 * kRow * 4 <= kSlots * kSlot && kPiecesOut >= 8, "the waves' rows fit the ring");
+    constexpr int kMask = kPiecesOut < 16 ? kPiecesOut - 1 : 15;
+    float4* const mine = reinterpret_cast<float4*>(ring + wave * (32 * kRow * 4));
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");           // nobody reads the last step any more
+#pragma unroll
+    for (int x = 0; x < FP; ++x) {
+        const int row = lane % 32;
+#pragma unroll
+        for (int y = 0; y < FQ; ++y)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                mine[row * kPiecesOut + ((8 * y + 2 * i + lane / 32) ^ (row & kMask))] =
+                    make_float4(acc[x][y][4 * i], acc[x][y][4 * i + 1], acc[x][y][4 * i + 2], acc[x][y][4 * i + 3]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int c = lane % kLanes, q = q0 + wq + 8 * c, Q8 = (g.Q + 7) / 8 * 8;
+#pragma unroll 1
+        for (int r = lane / kLanes; r < 32; r += kWave / kLanes) {
+            const int p = p0 + wp + 32 * x + r;
+            const float4 lo = mine[r * kPiecesOut + ((2 * c) ^ (r & kMask))], hi = mine[r * kPiecesOut + ((2 * c + 1) ^ (r & kMask))];
+            if (p >= g.P || q >= g.Q) continue;
+            if (g.plan.splits == 1) {
+                float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                finish8(g.e, p, q, v);
+            } else {
+                float4* const to = reinterpret_cast<float4*>(g.partial + ((size_t)t.split * g.P + p) * Q8 + q);
+                to[0] = lo;
+                to[1] = hi;
+            }
+        }
+        asm volatile("" ::: "memory");
     }
 }
 
@@ -298,27 +363,37 @@ __global__ __launch_bounds__(256) void w16a16_sum_kernel(const float* __restrict
 // -------------------------------------------------------------------------------------------- dz and db --
 
 constexpr int kDzCols = 256;   // columns of a block: 32 threads of 8; 8 threads share a column's rows
-constexpr int kDzRows = 64;    // rows of a block
+constexpr int kDzSlices = 8;
 
-// dz = bf16(dy act'(z)), rows of ld values (N rounded up to 8, zeros behind N), and the sums of the unrounded dz over a block's rows.
+// The rows of a block: 8 a thread where that leaves eight blocks a compute unit, fewer for short batches.
+inline int dz_rows(int M, int across, int units) {
+    const long long rows = (long long)M * across / (8ll * units);
+    return kDzSlices * (int)std::max(1ll, std::min(8ll, rows / kDzSlices));
+}
+
+// dz = bf16(dy act'(z)), rows of ld values (N rounded up to 8, zeros behind N), and the sums of the unrounded dz over a block's rows.  Bound by HBM.
 __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restrict__ z, const uint16_t* __restrict__ dy, const float* __restrict__ dy32, int act,
-                                                        int M, int N, int ld, uint16_t* __restrict__ dz, float* __restrict__ sums) {
-    __shared__ float part[8][kDzCols + 8];
+                                                        int M, int N, int ld, int rows, uint16_t* __restrict__ dz, float* __restrict__ sums) {
+    __shared__ float part[kDzSlices][kDzCols + 8];
     const int across = (ld + kDzCols - 1) / kDzCols, bx = blockIdx.x % across, by = blockIdx.x / across;
     const int c = threadIdx.x % 32, n = bx * kDzCols + 8 * c, slice = threadIdx.x / 32;
-    const int m0 = by * kDzRows, m1 = min(M, m0 + kDzRows);
+    const int m0 = by * rows, m1 = min(M, m0 + rows);
+    const bool whole = N % 8 == 0;
     float sum[8] = {};
     if (n < ld) {
-        for (int m = m0 + slice; m < m1; m += 8) {
+#pragma unroll 2
+        for (int m = m0 + slice; m < m1; m += kDzSlices) {
             const size_t at = (size_t)m * N + n;
             float v[8], s[8];
-            if (N % 8 == 0) {
+            if (whole) {
+                uint4 kept;
+                if (act != QAIL_ACT_NONE) kept = *reinterpret_cast<const uint4*>(z + at);
                 if (dy) unpack8(*reinterpret_cast<const uint4*>(dy + at), v);
                 else {
                     const float4 lo = reinterpret_cast<const float4*>(dy32 + at)[0], hi = reinterpret_cast<const float4*>(dy32 + at)[1];
                     v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
                 }
-                if (act != QAIL_ACT_NONE) unpack8(*reinterpret_cast<const uint4*>(z + at), s);
+                if (act != QAIL_ACT_NONE) unpack8(kept, s);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -329,7 +404,7 @@ __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restri
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (act != QAIL_ACT_NONE) v[i] = n + i < N ? v[i] * slope(act, s[i]) : 0.f;
+                if (act != QAIL_ACT_NONE) v[i] = whole || n + i < N ? v[i] * slope(act, s[i]) : 0.f;
                 sum[i] += v[i];
             }
             if (dz) *reinterpret_cast<uint4*>(dz + (size_t)m * ld + n) = pack8(v);
@@ -343,15 +418,24 @@ __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restri
     if (col >= N) return;
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t += part[i][threadIdx.x];
+    for (int i = 0; i < kDzSlices; ++i) t += part[i][threadIdx.x];
     sums[(size_t)by * N + col] = t;
 }
 
+// The blocks' sums added up: 32 columns a block, 8 threads a column.
 __global__ __launch_bounds__(256) void w16a16_bias_kernel(const float* __restrict__ sums, int count, int N, float* __restrict__ dbias) {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
+    __shared__ float part[8][32];
+    const int c = threadIdx.x % 32, slice = threadIdx.x / 32, n = blockIdx.x * 32 + c;
     float t = 0.f;
-    for (int i = 0; i < count; ++i) t += sums[(size_t)i * N + n];
+    if (n < N) {
+#pragma unroll 8
+        for (int i = slice; i < count; i += 8) t += sums[(size_t)i * N + n];
+    }
+    part[slice][c] = t;
+    __syncthreads();
+    if (slice != 0 || n >= N) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += part[i][c];
     dbias[n] = t;
 }
 
@@ -378,9 +462,10 @@ hipError_t launch_product(ProductArgs g, float* partial, hipStream_t st) {
     g.partial = partial;
     g.e.Q = g.Q;
     hipError_t e = hipErrorInvalidValue;
+    if (g.plan.bp == 256) e = launch_tiles<256, 256, 2, 4, kTA, kTB, 2>(g, st);
     if (g.plan.bp == 128) e = launch_tiles<128, 128, 2, 2, kTA, kTB, 2>(g, st);
     if constexpr (!kTA)
-        if (g.plan.bp == 32) e = launch_tiles<32, 128, 1, 4, kTA, kTB, 4>(g, st);
+        if (g.plan.bp == 32) e = launch_tiles<32, 64, 1, 2, kTA, kTB, 4>(g, st);
     if (e != hipSuccess || g.plan.splits == 1) return e;
     const long long threads = (long long)g.P * ((g.Q + 7) / 8);
     hipLaunchKernelGGL(w16a16_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, partial, g.plan.splits, g.P, g.e);
@@ -405,13 +490,15 @@ hipError_t launch_w16a16(const qail_w16a16& d, const uint16_t* x, int M, const u
     return launch_product<false, false>(g, static_cast<float*>(ws), st);
 }
 
-// The workspace of the backward call: dz, the sums of dz over kDzRows rows each, then the shares of the two products in turn.
+// The workspace of the backward call: dz, the sums of dz over the blocks' rows, then the shares of the two products in turn.
 struct BackPlaces {
-    int ld, row_blocks;
+    int ld, across, rows, row_blocks;
     size_t sums, partial, bytes;
     BackPlaces(const qail_w16a16& d, int M) {
         ld = (d.N + 7) / 8 * 8;
-        row_blocks = (M + kDzRows - 1) / kDzRows;
+        across = (ld + kDzCols - 1) / kDzCols;
+        rows = dz_rows(M, across, device_cu_count());
+        row_blocks = (M + rows - 1) / rows;
         sums = round256((size_t)M * ld * 2);
         partial = sums + round256((size_t)row_blocks * d.N * sizeof(float));
         bytes = partial + round256(std::max(partial_bytes(M, d.K, d.N, false), partial_bytes(d.N, d.K, M, true)));
@@ -430,10 +517,9 @@ hipError_t launch_w16a16_back(const qail_w16a16& d, const uint16_t* x, const uin
     const bool as_it_is = d.activation == QAIL_ACT_NONE && dy && d.N % 8 == 0;   // dz is dy
     const bool products = dx || dweight;
     if ((products && !as_it_is) || dbias) {
-        const unsigned blocks = (unsigned)((at.ld + kDzCols - 1) / kDzCols) * (unsigned)at.row_blocks;
-        hipLaunchKernelGGL(w16a16_dz_kernel, dim3(blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, products && !as_it_is ? dz : nullptr,
+        hipLaunchKernelGGL(w16a16_dz_kernel, dim3((unsigned)at.across * (unsigned)at.row_blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, at.rows, products && !as_it_is ? dz : nullptr,
                            dbias ? sums : nullptr);
-        if (dbias) hipLaunchKernelGGL(w16a16_bias_kernel, dim3((unsigned)((d.N + 255) / 256)), dim3(256), 0, st, sums, at.row_blocks, d.N, dbias);
+        if (dbias) hipLaunchKernelGGL(w16a16_bias_kernel, dim3((unsigned)((d.N + 31) / 32)), dim3(256), 0, st, sums, at.row_blocks, d.N, dbias);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
