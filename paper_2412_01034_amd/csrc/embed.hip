@@ -3,8 +3,9 @@
 // The gradient adds up the rows of dh that belong to a token.  Atomics would add them in any order, so the tokens are sorted first (stable: a
 // token's rows stay in the order of their places), and whoever writes row v of the gradient reads its rows one after the other.  A token that comes
 // more than kPart times is added up in parts of kPart sorted places by other blocks before, whose sums are then added in their order.
-// What is sorted are pairs (token, place), 8 bits of the token at a time, in tiles of kTile: per tile the places of equal digits are
-// counted by comparing lanes, the counts of all tiles are summed up, and the pairs move.  All tokens in one tile stay in LDS for all digits.
+// What is sorted are pairs (token, place), 8 bits of the token at a time, in tiles of kTile, whose pairs stay in LDS for all digits: equal digits are found by comparing
+// lanes.  Up to kMergeTiles tiles are then merged by rank: a pair's place is its own tile's plus how many pairs of each other tile come before it, 12 probes a
+// tile.  More of them are sorted digit by digit over all tiles: their counts, the counts' sums, and the move.
 #include <algorithm>
 
 #include "qail_internal.h"
@@ -77,12 +78,16 @@ __device__ __forceinline__ void rank_digits(SortShared& sh, const uint32_t* digi
 // Per digit the counts of the waves in front; returns, in threads 0 .. 255, the tile's count of digit threadIdx.x.
 __device__ __forceinline__ uint32_t sum_waves(SortShared& sh) {
     uint32_t n = 0;
-    if (threadIdx.x < kDigits)
+    if (threadIdx.x < kDigits) {
+        uint32_t c[kSortWaves];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) c[w] = sh.count[w][threadIdx.x];
+#pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = sh.count[w][threadIdx.x];
             sh.count[w][threadIdx.x] = n;
-            n += c;
+            n += c[w];
         }
+    }
     return n;
 }
 
@@ -119,26 +124,27 @@ __device__ __forceinline__ void report(const int32_t* ids, int n, int V, uint32_
         if (ids[i] >= V) atomicAdd(errors, 1u);
 }
 
-// All tokens in one tile: every digit in one launch.
-__global__ __launch_bounds__(kSortBlock) void embed_sort_tile_kernel(const int32_t* __restrict__ ids, int T, int V, int passes, uint32_t* __restrict__ keys,
-                                                                     uint32_t* __restrict__ places, uint32_t* __restrict__ errors) {
+// Every tile by itself, all digits.
+__global__ __launch_bounds__(kSortBlock) void embed_sort_tiles_kernel(const int32_t* __restrict__ ids, int T, int V, int passes, uint32_t* __restrict__ keys,
+                                                                      uint32_t* __restrict__ places, uint32_t* __restrict__ errors) {
     __shared__ SortShared sh;
     __shared__ uint32_t start[kDigits], pair[2][kTile];
-    report(ids, T, V, errors);
+    const int first = blockIdx.x * kTile, n = min(kTile, T - first);
+    report(ids + first, n, V, errors);
     uint32_t key[kRounds], place[kRounds], digit[kRounds], rank[kRounds];
     bool held[kRounds];
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
         place[i] = place_in_tile(i);
-        held[i] = (int)place[i] < T;
-        key[i] = held[i] ? token_key(ids[place[i]], V) : 0;
+        held[i] = (int)place[i] < n;
+        key[i] = held[i] ? token_key(ids[first + place[i]], V) : 0;
     }
     for (int pass = 0; pass < passes; ++pass) {
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) digit[i] = (key[i] >> (8 * pass)) & 255u;
         rank_digits(sh, digit, held, rank);
         uint32_t all;
-        const uint32_t n = sum_waves(sh), before = sum_before(sh, n, &all);
+        const uint32_t count = sum_waves(sh), before = sum_before(sh, count, &all);
         if (threadIdx.x < kDigits) start[threadIdx.x] = before;
         __syncthreads();
 #pragma unroll
@@ -156,10 +162,39 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_tile_kernel(const int32
     }
 #pragma unroll
     for (int i = 0; i < kRounds; ++i)
-        if (held[i]) keys[place_in_tile(i)] = key[i], places[place_in_tile(i)] = place[i];
+        if (held[i]) keys[first + place_in_tile(i)] = key[i], places[first + place_in_tile(i)] = first + place[i];
 }
 
-// Several tiles, one digit: the tiles' counts, [digit][tile] ...  (keys == NULL: the first digit, of ids)
+// How many of n ascending keys are below v.
+__device__ __forceinline__ int below(const uint32_t* keys, int n, uint32_t v) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (keys[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+constexpr int kMergeTiles = 16;
+
+// Sorted tiles into one list.
+__global__ __launch_bounds__(256) void embed_merge_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ places, int T, uint32_t* __restrict__ keys_to,
+                                                          uint32_t* __restrict__ places_to) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= T) return;
+    const int tile = i / kTile, tiles = (T + kTile - 1) / kTile;
+    const uint32_t key = keys[i];
+    int to = i - tile * kTile;
+    for (int s = 0; s < tiles; ++s) {
+        const int first = s * kTile;
+        if (s != tile) to += below(keys + first, min(kTile, T - first), s < tile ? key + 1 : key);
+    }
+    keys_to[to] = key;
+    places_to[to] = places[i];
+}
+
+// Many tiles, one digit: the tiles' counts, [digit][tile] ...  (keys == NULL: the first digit, of ids)
 __global__ __launch_bounds__(kSortBlock) void embed_count_kernel(const int32_t* __restrict__ ids, const uint32_t* __restrict__ keys, int T, int V, int shift,
                                                                  uint32_t* __restrict__ counts, uint32_t* __restrict__ errors) {
     __shared__ uint32_t count[kDigits];
@@ -217,8 +252,8 @@ __global__ __launch_bounds__(kSortBlock) void embed_move_kernel(const int32_t* _
 // --------------------------------------------------------------------------------------------------- sums --
 
 constexpr int kPart = 32;       // sorted places of a part
-constexpr int kRowsEach = 64;   // rows of the gradient of a block
-constexpr int kCols = 1024;     // columns of a block: four a thread
+constexpr int kMostRows = 16;   // rows of the gradient of a block, at most: with 64, 32000 x 4096 takes 147 us instead of 129 (24577 tokens), as blocks differ in their tokens
+constexpr int kListed = 1024;   // places of a block's rows that it keeps in LDS
 
 struct SumArgs {
     const uint32_t* keys;       // sorted
@@ -228,37 +263,37 @@ struct SumArgs {
     float* parts;               // [parts][2][K]
     int T, V, K, accumulate;
     float scale;
+    int rows, lanes;            // of a block; threads that share a row, 4 columns each (a power of two)
 };
 
-// How many sorted keys are below v.
-__device__ __forceinline__ int below(const uint32_t* keys, int T, uint32_t v) {
-    int lo = 0, hi = T;
+// below() by a whole wave: 64 probes at a time, so three or four trips to memory instead of fifteen.
+__device__ __forceinline__ int below_by_wave(const uint32_t* keys, int n, uint32_t v) {
+    const int lane = threadIdx.x % kWave;
+    int lo = 0, hi = n;
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (keys[mid] < v) lo = mid + 1;
-        else hi = mid;
+        const int step = (hi - lo + kWave - 1) / kWave, at = lo + (lane + 1) * step - 1;   // the last of each of 64 runs
+        const int c = __popcll(__ballot(at < hi && keys[at < hi ? at : hi - 1] < v));
+        lo += c * step;
+        hi = min(hi, lo + step - 1);
     }
     return lo;
 }
 
-// The sum of the rows at sorted places a .. b - 1, four columns a thread, eight rows requested at a time.
-__device__ __forceinline__ float4 sum_rows(const SumArgs& g, int a, int b, int col) {
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = a; i < b; i += 8) {
+// The sum of the rows of dh at places[0 .. n), four columns a thread, eight rows requested at a time; behind the last one that row again (kFew: nothing, for
+// sums of a row or two).
+template <bool kFew, typename Places>
+__device__ __forceinline__ f32x4_t sum_rows(const SumArgs& g, Places places, int n, int col) {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i += 8) {
         uint2 v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int at = i + e < b ? i + e : b - 1;
-            v[e] = *reinterpret_cast<const uint2*>(g.dh + (size_t)g.places[at] * g.K + col);
-        }
+        for (int e = 0; e < 8; ++e)
+            if (!kFew || i + e < n) v[e] = *reinterpret_cast<const uint2*>(g.dh + (size_t)places(kFew ? i + e : min(i + e, n - 1)) * g.K + col);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (i + e < b) {
-                s.x += __builtin_bit_cast(float, v[e].x << 16);
-                s.y += __builtin_bit_cast(float, v[e].x & 0xFFFF0000u);
-                s.z += __builtin_bit_cast(float, v[e].y << 16);
-                s.w += __builtin_bit_cast(float, v[e].y & 0xFFFF0000u);
-            }
+            if (i + e < n)
+                s += f32x4_t{__builtin_bit_cast(float, v[e].x << 16), __builtin_bit_cast(float, v[e].x & 0xFFFF0000u), __builtin_bit_cast(float, v[e].y << 16),
+                             __builtin_bit_cast(float, v[e].y & 0xFFFF0000u)};
     }
     return s;
 }
@@ -266,53 +301,83 @@ __device__ __forceinline__ float4 sum_rows(const SumArgs& g, int a, int b, int c
 // Part i has sorted places kPart i .. and two sums: of the token that its first place belongs to, and of its last place's if that is another; each
 // only where the token comes more than kPart times.
 __global__ __launch_bounds__(256) void embed_parts_kernel(const SumArgs g) {
-    __shared__ int at[6];
-    const int across = (g.K + kCols - 1) / kCols, part = blockIdx.x / across;
+    const int across = (g.K + 1023) / 1024, part = blockIdx.x / across, lane = threadIdx.x % kWave;
     const int a = part * kPart, b = min(g.T, a + kPart);
-    const uint32_t head = g.keys[a], tail = g.keys[b - 1];
-    if (threadIdx.x < 4) {   // where both tokens begin and end
-        const uint32_t v = threadIdx.x < 2 ? head : tail;
-        at[threadIdx.x] = below(g.keys, g.T, v + threadIdx.x % 2);
-    }
-    __syncthreads();
-    const int col = blockIdx.x % across * kCols + 4 * threadIdx.x;
+    static_assert(kPart <= kWave, "a wave sees a part at once");
+    const uint32_t key = g.keys[min(a + lane, b - 1)], head = __builtin_amdgcn_readfirstlane(key), tail = __builtin_amdgcn_readlane(key, kPart - 1);
+    const int end = a + __popcll(__ballot(a + lane < b && key == head)), begin = b - __popcll(__ballot(a + lane < b && key == tail));   // in the part
+    // more than kPart places of one token: the part's first or last and one kPart farther on
+    const bool long_head = head < (uint32_t)g.V && ((end > kPart && g.keys[end - 1 - kPart] == head) || (a + kPart < g.T && g.keys[a + kPart] == head));
+    const bool long_tail = tail != head && tail < (uint32_t)g.V && begin + kPart < g.T && g.keys[begin + kPart] == tail;
+    const int col = blockIdx.x % across * 1024 + 4 * threadIdx.x;
     if (col >= g.K) return;
-    float4* const to = reinterpret_cast<float4*>(g.parts + (size_t)part * 2 * g.K + col);
-    if (head < (uint32_t)g.V && at[1] - at[0] > kPart) *to = sum_rows(g, a, min(b, at[1]), col);
-    if (tail != head && tail < (uint32_t)g.V && at[3] - at[2] > kPart) to[g.K / 4] = sum_rows(g, at[2], b, col);
+    const auto put = [&](int which, int from, int to) {
+        *reinterpret_cast<f32x4_t*>(g.parts + ((size_t)part * 2 + which) * g.K + col) = sum_rows<false>(g, [&](int i) { return g.places[from + i]; }, to - from, col);
+    };
+    if (long_head) put(0, a, end);
+    if (long_tail) put(1, begin, b);
 }
 
-__global__ __launch_bounds__(256) void embed_rows_kernel(const SumArgs g) {
-    __shared__ int start[kRowsEach + 1];
-    const int across = (g.K + kCols - 1) / kCols, v0 = blockIdx.x / across * kRowsEach, rows = min(kRowsEach, g.V - v0);
-    if ((int)threadIdx.x <= rows) start[threadIdx.x] = below(g.keys, g.T, (uint32_t)(v0 + threadIdx.x));
+// kStream: the gradient is written past the caches.
+template <bool kStream>
+__global__ __launch_bounds__(256, 8) void embed_rows_kernel(const SumArgs g) {
+    __shared__ int start[kMostRows + 1], ends[2];
+    __shared__ uint32_t listed[kListed];
+    const int across = (g.K + 4 * g.lanes - 1) / (4 * g.lanes), v0 = blockIdx.x / across * g.rows, rows = min(g.rows, g.V - v0);
+    // where the rows' tokens begin: the first and the last one's by two waves, the others' from the keys between
+    if (threadIdx.x < 2 * kWave) {
+        const int which = threadIdx.x / kWave, at = below_by_wave(g.keys, g.T, (uint32_t)(v0 + (which ? rows : 0)));
+        if (threadIdx.x % kWave == 0) ends[which] = at;
+    }
     __syncthreads();
-    const int col = blockIdx.x % across * kCols + 4 * threadIdx.x;
+    const int lo = ends[0], hi = ends[1];
+    if (hi - lo <= kListed) {
+        for (int i = lo + threadIdx.x; i <= hi; i += 256) {   // place i begins all rows above the key before it, up to its own
+            const int from = i == lo ? 0 : (int)g.keys[i - 1] - v0 + 1, to = i == hi ? rows : (int)g.keys[i] - v0;
+            for (int v = from; v <= to; ++v) start[v] = i;
+            if (i < hi) listed[i - lo] = g.places[i];
+        }
+    } else if ((int)threadIdx.x <= rows) {
+        start[threadIdx.x] = lo + below(g.keys + lo, hi - lo, (uint32_t)(v0 + threadIdx.x));
+    }
+    __syncthreads();
+    const int col = 4 * (blockIdx.x % across * g.lanes + (threadIdx.x & (g.lanes - 1))), groups = 256 / g.lanes;
     if (col >= g.K) return;
-    for (int i = 0; i < rows; ++i) {
+    for (int i = threadIdx.x / g.lanes; i < rows; i += groups) {
         const int a = start[i], b = start[i + 1];
         if (a == b && g.accumulate) continue;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (b - a <= kPart) {
-            s = sum_rows(g, a, b, col);
-        } else {
-            for (int part = a / kPart; part * kPart < b; ++part) {
-                const int which = part * kPart < a;   // the token begins inside the part
-                const float4 t = *reinterpret_cast<const float4*>(g.parts + ((size_t)part * 2 + which) * g.K + col);
-                s.x += t.x, s.y += t.y, s.z += t.z, s.w += t.w;
+        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+        if (b - a > kPart) {
+            const int last = (b - 1) / kPart;
+            for (int part = a / kPart; part <= last; part += 8) {
+                f32x4_t t[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = min(part + e, last), which = at * kPart < a;   // the token begins inside the part
+                    t[e] = *reinterpret_cast<const f32x4_t*>(g.parts + ((size_t)at * 2 + which) * g.K + col);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (part + e <= last) s += t[e];
             }
+        } else if (hi - lo <= kListed) {
+            s = sum_rows<true>(g, [&](int k) { return listed[a - lo + k]; }, b - a, col);
+        } else {
+            s = sum_rows<true>(g, [&](int k) { return g.places[a + k]; }, b - a, col);
         }
-        s.x *= g.scale, s.y *= g.scale, s.z *= g.scale, s.w *= g.scale;
-        float4* const to = reinterpret_cast<float4*>(g.dtable + (size_t)(v0 + i) * g.K + col);
-        if (g.accumulate) {
-            const float4 o = *to;
-            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
-        }
-        *to = s;
+        s *= g.scale;
+        f32x4_t* const to = reinterpret_cast<f32x4_t*>(g.dtable + (size_t)(v0 + i) * g.K + col);
+        if (g.accumulate) s += *to;
+        if constexpr (kStream) __builtin_nontemporal_store(s, to);
+        else *to = s;
     }
 }
 
 constexpr size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+
+// A gradient that no cache holds (256 MB) is written past them, where it would push out dh: 32000 x 4096 with 2312 tokens 114 -> 103 us, the sums of parts before it
+// 10 -> 7.
+constexpr size_t kStreamFrom = (size_t)256 << 20;
 
 struct Places {   // of the workspace
     int tiles, parts;
@@ -322,7 +387,7 @@ struct Places {   // of the workspace
         parts = T > kPart ? (T + kPart - 1) / kPart : 0;
         pairs = round256((size_t)T * 4);                              // keys, places, and both again where several tiles are sorted
         counts = pairs * (tiles > 1 ? 4 : 2);
-        sums = counts + (tiles > 1 ? round256((size_t)kDigits * tiles * 4) : 0);
+        sums = counts + (tiles > kMergeTiles ? round256((size_t)kDigits * tiles * 4) : 0);
         bytes = sums + (size_t)parts * 2 * K * 4;
     }
 };
@@ -349,10 +414,16 @@ hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, floa
     uint32_t* const counts = reinterpret_cast<uint32_t*>(w + at.counts);
     int passes = 1;
     while (passes < 4 && (V >> (8 * passes)) != 0) ++passes;   // keys are 0 .. V
-    SumArgs g = {pair[0], pair[1], dh, dtable, reinterpret_cast<float*>(w + at.sums), T, V, K, accumulate, scale};
-    if (at.tiles == 1) {
-        hipLaunchKernelGGL(embed_sort_tile_kernel, dim3(1), dim3(kSortBlock), 0, st, ids, T, V, passes, pair[0], pair[1], errors);
-    } else if (at.tiles > 1) {
+    SumArgs g = {pair[0], pair[1], dh, dtable, reinterpret_cast<float*>(w + at.sums), T, V, K, accumulate, scale, 1, 1};
+    while (4 * g.lanes < K && g.lanes < 256) g.lanes *= 2;
+    // eight blocks a compute unit, and no fewer rows than threads for them
+    const int across = (K + 4 * g.lanes - 1) / (4 * g.lanes), groups = 256 / g.lanes;
+    g.rows = (int)std::min<long long>(kMostRows, std::max<long long>(groups, (long long)V * across / (8 * device_cu_count())));
+    if (at.tiles > 0 && at.tiles <= kMergeTiles) {
+        uint32_t* const* const to = at.tiles > 1 ? pair + 2 : pair;
+        hipLaunchKernelGGL(embed_sort_tiles_kernel, dim3(at.tiles), dim3(kSortBlock), 0, st, ids, T, V, passes, to[0], to[1], errors);
+        if (at.tiles > 1) hipLaunchKernelGGL(embed_merge_kernel, dim3((T + 255) / 256), dim3(256), 0, st, to[0], to[1], T, pair[0], pair[1]);
+    } else if (at.tiles > kMergeTiles) {
         for (int pass = 0; pass < passes; ++pass) {
             const uint32_t* const keys = pass ? pair[2 * (pass & 1)] : nullptr;
             const uint32_t* const places = pass ? pair[2 * (pass & 1) + 1] : nullptr;
@@ -364,9 +435,8 @@ hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, floa
             g.keys = keys_to, g.places = places_to;
         }
     }
-    const int across = (K + kCols - 1) / kCols;
-    if (at.parts) hipLaunchKernelGGL(embed_parts_kernel, dim3((unsigned)at.parts * across), dim3(256), 0, st, g);
-    hipLaunchKernelGGL(embed_rows_kernel, dim3((unsigned)((V + kRowsEach - 1) / kRowsEach) * across), dim3(256), 0, st, g);
+    if (at.parts) hipLaunchKernelGGL(embed_parts_kernel, dim3((unsigned)at.parts * ((K + 1023) / 1024)), dim3(256), 0, st, g);
+    hipLaunchKernelGGL((size_t)V * K * sizeof(float) >= kStreamFrom ? embed_rows_kernel<true> : embed_rows_kernel<false>, dim3((unsigned)((V + g.rows - 1) / g.rows) * across), dim3(256), 0, st, g);
     return hipGetLastError();
 }
 
