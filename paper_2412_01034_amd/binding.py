@@ -194,18 +194,20 @@ def _not_plain(*args):
 
 _linear_native = _linear_batch_native = _conv_batch_native = _not_plain
 _rmsnorm_native = _rmsnorm_backward_native = _kv_append_native = _paged_attention_native = _adapters_batch_native = _not_plain
+_embed_native = _embed_backward_native = _w16a16_native = _w16a16_backward_native = _sample_native = _not_plain
 
 
 def _marshal_for() -> tuple:
     """What a module has to be built for: its layouts are compiled in."""
     return (sys.hexversion >> 16, "%s %s" % (torch.__version__, torch.version.git_version), ctypes.sizeof(qail_wdesc),
             ctypes.sizeof(qail_w4a16_item), ctypes.sizeof(qail_conv_item), ctypes.sizeof(qail_kv_cache), ctypes.sizeof(qail_requests),
-            ctypes.sizeof(qail_adapters))
+            ctypes.sizeof(qail_adapters), ctypes.sizeof(qail_w16a16), ctypes.sizeof(qail_sampling))
 
 
 def _use_native(L: ctypes.CDLL) -> None:
     global _linear_native, _linear_batch_native, _conv_batch_native
     global _rmsnorm_native, _rmsnorm_backward_native, _kv_append_native, _paged_attention_native, _adapters_batch_native
+    global _embed_native, _embed_backward_native, _w16a16_native, _w16a16_backward_native, _sample_native
     try:
         from . import _marshal
     except ImportError:
@@ -218,6 +220,9 @@ def _use_native(L: ctypes.CDLL) -> None:
                                                                            L.qail_w4a16_linear_adapters_batch)))
     _rmsnorm_native, _rmsnorm_backward_native, _kv_append_native = _marshal.rmsnorm, _marshal.rmsnorm_backward, _marshal.kv_append
     _paged_attention_native, _adapters_batch_native = _marshal.paged_attention, _marshal.adapters_batch
+    _marshal.use_ends(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.qail_embed, L.qail_embed_backward, L.qail_w16a16_linear, L.qail_w16a16_backward, L.qail_sample)))
+    _embed_native, _embed_backward_native, _w16a16_native = _marshal.embed, _marshal.embed_backward, _marshal.w16a16_linear
+    _w16a16_backward_native, _sample_native = _marshal.w16a16_backward, _marshal.sample
 
 
 def status_string(status: int) -> str:
@@ -862,6 +867,11 @@ QAIL_LOGITS_F32 = 1
 
 def qail_embed(table: torch.Tensor, ids: torch.Tensor, h: torch.Tensor, scale: float = 1.0, errors: Optional[torch.Tensor] = None) -> None:
     """table: bf16 [V, K]; ids: int32, any shape; h: bf16, K values for each id.  A row whose id is negative is left as it was."""
+    status = _embed_native(table, ids, h, scale, errors)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_embed")
+        return
     V, K = table.shape
     T = ids.numel()
     _check(lib().qail_embed(_bf16(table, V * K, "table"), V, K, _int32(ids, T, "ids"), T, scale, _bf16(h, T * K, "h"), _errors(errors), _stream()),
@@ -877,6 +887,11 @@ def qail_embed_backward_workspace(V: int, K: int, T: int) -> int:
 def qail_embed_backward(ids: torch.Tensor, dh: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
                         errors: Optional[torch.Tensor] = None) -> None:
     """ids: int32, any shape; dh: bf16, K values for each id; dtable: fp32 [V, K], overwritten or, with `accumulate`, added to."""
+    status = _embed_backward_native(ids, dh, dtable, workspace, scale, accumulate, errors)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_embed_backward")
+        return
     V, K = dtable.shape
     T = ids.numel()
     _check(lib().qail_embed_backward(_int32(ids, T, "ids"), _bf16(dh, T * K, "dh"), T, scale, V, K, int(bool(accumulate)), _fp32(dtable, V * K, "dtable"),
@@ -907,6 +922,11 @@ def _bf16_or_fp32(t: torch.Tensor, count: int, what: str) -> Tuple[Optional[int]
 def qail_w16a16_linear(linear: qail_w16a16, x: torch.Tensor, y: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                        residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None) -> None:
     """x: bf16 [M, K]; y: bf16 or fp32 [M, N]; residual, z (what the activation is applied to, for the backward call): bf16 [M, N]."""
+    status = _w16a16_native(linear, x, y, workspace, residual, z) if type(linear) is qail_w16a16 else None
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_w16a16_linear")
+        return
     M, N, K = x.shape[0], linear.N, linear.K
     half, whole = _bf16_or_fp32(y, M * N, "y")
     ws, wsb = (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
@@ -923,6 +943,11 @@ def qail_w16a16_backward_workspace(linear: qail_w16a16, M: int) -> int:
 def qail_w16a16_backward(linear: qail_w16a16, x: Optional[torch.Tensor], dy: torch.Tensor, workspace: torch.Tensor, z: Optional[torch.Tensor] = None,
                          dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None) -> None:
     """x, dx: bf16 [M, K]; dy: bf16 or fp32 [M, N]; z: bf16 [M, N]; dweight: bf16 [N, K]; dbias: fp32 [N]."""
+    status = _w16a16_backward_native(linear, x, dy, workspace, z, dx, dweight, dbias) if type(linear) is qail_w16a16 else None
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_w16a16_backward")
+        return
     M, N, K = dy.shape[0], linear.N, linear.K
     half, whole = _bf16_or_fp32(dy, M * N, "dy")
     _check(lib().qail_w16a16_backward(ctypes.byref(linear), _bf16(x, M * K, "x"), _bf16(z, M * N, "z"), half, whole, M, _bf16(dx, M * K, "dx"),
@@ -935,6 +960,11 @@ def qail_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor, logp
                 errors: Optional[torch.Tensor] = None) -> None:
     """logits: bf16 or fp32 [R, V], rows of a wider tensor among them; u: fp32 [R], in [0, 1); token: int32 [R]; logprob: fp32 [R]; temperature, top_p, min_p: fp32
     [R], top_k: int32 [R], None for off."""
+    status = _sample_native(logits, u, token, logprob, temperature, top_k, top_p, min_p, errors)
+    if status is not None:
+        if status:
+            raise QailError(status, "qail_sample")
+        return
     _typed(logits, "logits", torch.bfloat16, torch.float32)
     if not logits.is_cuda:
         raise ValueError("device tensor expected")

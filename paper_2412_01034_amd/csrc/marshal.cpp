@@ -27,6 +27,11 @@ decltype(&qail_rmsnorm_backward) g_rmsnorm_backward = nullptr;
 decltype(&qail_kv_append) g_kv_append = nullptr;
 decltype(&qail_paged_attention) g_paged_attention = nullptr;
 decltype(&qail_w4a16_linear_adapters_batch) g_adapters_batch = nullptr;
+decltype(&qail_embed) g_embed = nullptr;
+decltype(&qail_embed_backward) g_embed_backward = nullptr;
+decltype(&qail_w16a16_linear) g_w16a16 = nullptr;
+decltype(&qail_w16a16_backward) g_w16a16_backward = nullptr;
+decltype(&qail_sample) g_sample = nullptr;
 
 bool number(PyObject* o, int32_t& v) {   // an int of at least 0 that fits 32 bits
     if (!PyLong_CheckExact(o)) return false;
@@ -287,6 +292,141 @@ PyObject* adapters_batch(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// How many numbers a plain tensor of 32-bit integers has.
+bool count_of(PyObject* o, int32_t& n) {
+    if (!THPVariable_CheckExact(o) || THPVariable_Unpack(o).numel() > INT_MAX) return false;
+    n = (int32_t)THPVariable_Unpack(o).numel();
+    return true;
+}
+// bf16 or fp32, the other address NULL.
+template <typename A, typename B>
+bool either(PyObject* o, int64_t count, A*& half, B*& whole) {
+    half = nullptr;
+    whole = nullptr;
+    return typed(o, Kind::fp32, 4 * count, whole) || typed(o, Kind::bf16, 2 * count, half);
+}
+
+// (table, ids, h, scale, errors)
+PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return plainly([&]() -> PyObject* {
+        int64_t V, K;
+        int32_t T;
+        float scale;
+        const uint16_t* table;
+        const int32_t* ids;
+        uint16_t* h;
+        uint32_t* errors;
+        if (n != 5 || !g_embed || !rows_of(a[0], V, K) || !count_of(a[1], T) || !real(a[3], scale) || !typed(a[0], Kind::bf16, V * K * 2, table) ||
+            !typed(a[1], Kind::int32, (int64_t)T * 4, ids) || !typed(a[2], Kind::bf16, (int64_t)T * K * 2, h) || !optional(a[4], Kind::int32, 4, errors))
+            return nullptr;
+        void* const st = stream();
+        return call([&] { return g_embed(table, (int32_t)V, (int32_t)K, ids, T, scale, h, errors, st); });
+    });
+}
+
+// (ids, dh, dtable, workspace, scale, accumulate, errors)
+PyObject* embed_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return plainly([&]() -> PyObject* {
+        int64_t V, K;
+        int32_t T;
+        float scale;
+        const uint16_t* dh;
+        const int32_t* ids;
+        float* dtable;
+        uint32_t* errors;
+        void* ws;
+        size_t ws_bytes = 0;
+        if (n != 7 || !g_embed_backward || !rows_of(a[2], V, K) || !count_of(a[0], T) || !real(a[4], scale) || !PyBool_Check(a[5]) ||
+            !typed(a[0], Kind::int32, (int64_t)T * 4, ids) || !typed(a[1], Kind::bf16, (int64_t)T * K * 2, dh) || !typed(a[2], Kind::fp32, V * K * 4, dtable) ||
+            !tensor(a[3], 0, ws, &ws_bytes) || !optional(a[6], Kind::int32, 4, errors))
+            return nullptr;
+        const int32_t accumulate = a[5] == Py_True;
+        void* const st = stream();
+        return call([&] { return g_embed_backward(ids, dh, T, scale, (int32_t)V, (int32_t)K, accumulate, dtable, errors, ws, ws_bytes, st); });
+    });
+}
+
+// (linear, x, y, workspace, residual, z)
+PyObject* w16a16_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return plainly([&]() -> PyObject* {
+        if (n != 6 || !g_w16a16) return nullptr;
+        const Items di(a[0]);
+        const auto* d = held<qail_w16a16>(di);
+        if (!d || !THPVariable_CheckExact(a[1]) || THPVariable_Unpack(a[1]).dim() < 1 || THPVariable_Unpack(a[1]).size(0) > INT_MAX) return nullptr;
+        const int64_t M = THPVariable_Unpack(a[1]).size(0);
+        const uint16_t *x, *residual;
+        uint16_t *y, *z;
+        float* y32;
+        void* ws = nullptr;
+        size_t ws_bytes = 0;
+        if (!typed(a[1], Kind::bf16, M * d->K * 2, x) || !either(a[2], M * d->N, y, y32) || (a[3] != Py_None && !tensor(a[3], 0, ws, &ws_bytes)) ||
+            !optional(a[4], Kind::bf16, M * d->N * 2, residual) || !optional(a[5], Kind::bf16, M * d->N * 2, z))
+            return nullptr;
+        void* const st = stream();
+        return call([&] { return g_w16a16(d, x, (int32_t)M, residual, z, y, y32, ws, ws_bytes, st); });
+    });
+}
+
+// (linear, x, dy, workspace, z, dx, dweight, dbias)
+PyObject* w16a16_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return plainly([&]() -> PyObject* {
+        if (n != 8 || !g_w16a16_backward) return nullptr;
+        const Items di(a[0]);
+        const auto* d = held<qail_w16a16>(di);
+        if (!d || !THPVariable_CheckExact(a[2]) || THPVariable_Unpack(a[2]).dim() < 1 || THPVariable_Unpack(a[2]).size(0) > INT_MAX) return nullptr;
+        const int64_t M = THPVariable_Unpack(a[2]).size(0), N = d->N, K = d->K;
+        const uint16_t *x, *z, *dy;
+        const float* dy32;
+        uint16_t *dx, *dw;
+        float* db;
+        void* ws;
+        size_t ws_bytes = 0;
+        if (!optional(a[1], Kind::bf16, M * K * 2, x) || !either(a[2], M * N, dy, dy32) || !tensor(a[3], 0, ws, &ws_bytes) || !optional(a[4], Kind::bf16, M * N * 2, z) ||
+            !optional(a[5], Kind::bf16, M * K * 2, dx) || !optional(a[6], Kind::bf16, N * K * 2, dw) || !optional(a[7], Kind::fp32, N * 4, db))
+            return nullptr;
+        void* const st = stream();
+        return call([&] { return g_w16a16_backward(d, x, z, dy, dy32, (int32_t)M, dx, dw, db, ws, ws_bytes, st); });
+    });
+}
+
+// (logits, u, token, logprob, temperature, top_k, top_p, min_p, errors)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return plainly([&]() -> PyObject* {
+        if (n != 9 || !g_sample || !THPVariable_CheckExact(a[0])) return nullptr;
+        const at::Tensor& l = THPVariable_Unpack(a[0]);
+        const auto type = l.scalar_type();
+        if (!l.is_cuda() || l.dim() != 2 || (type != at::kFloat && type != at::kBFloat16) || l.size(0) > INT_MAX || l.size(1) > INT_MAX || (l.stride(1) != 1 && l.size(1) > 1))
+            return nullptr;
+        const int64_t R = l.size(0), V = l.size(1), stride = R > 1 ? l.stride(0) : V;
+        const float* u;
+        int32_t* token;
+        float* logprob;
+        qail_sampling s;
+        uint32_t* errors;
+        if (!typed(a[1], Kind::fp32, R * 4, u) || !typed(a[2], Kind::int32, R * 4, token) || !optional(a[3], Kind::fp32, R * 4, logprob) ||
+            !optional(a[4], Kind::fp32, R * 4, s.temperature) || !optional(a[5], Kind::int32, R * 4, s.top_k) || !optional(a[6], Kind::fp32, R * 4, s.top_p) ||
+            !optional(a[7], Kind::fp32, R * 4, s.min_p) || !optional(a[8], Kind::int32, 4, errors))
+            return nullptr;
+        const void* const logits = l.data_ptr();
+        void* const st = stream();
+        return call([&] {
+            return g_sample(logits, type == at::kFloat ? QAIL_LOGITS_F32 : QAIL_LOGITS_BF16, stride, (int32_t)R, (int32_t)V, &s, u, token, logprob, errors, st);
+        });
+    });
+}
+
+// Addresses of the five functions of the policy's ends, in the order above.
+PyObject* use_ends(PyObject*, PyObject* args) {
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+    g_embed = reinterpret_cast<decltype(g_embed)>(f[0]);
+    g_embed_backward = reinterpret_cast<decltype(g_embed_backward)>(f[1]);
+    g_w16a16 = reinterpret_cast<decltype(g_w16a16)>(f[2]);
+    g_w16a16_backward = reinterpret_cast<decltype(g_w16a16_backward)>(f[3]);
+    g_sample = reinterpret_cast<decltype(g_sample)>(f[4]);
+    Py_RETURN_NONE;
+}
+
 // Addresses of the five functions of serving, in the order above.
 PyObject* use_serving(PyObject*, PyObject* args) {
     unsigned long long f[5];
@@ -317,6 +457,12 @@ PyMethodDef methods[] = {
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_append)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_attention)), METH_FASTCALL, nullptr},
     {"adapters_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(adapters_batch)), METH_FASTCALL, nullptr},
+    {"use_ends", use_ends, METH_VARARGS, nullptr},
+    {"embed", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(embed)), METH_FASTCALL, nullptr},
+    {"embed_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(embed_backward)), METH_FASTCALL, nullptr},
+    {"w16a16_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(w16a16_linear)), METH_FASTCALL, nullptr},
+    {"w16a16_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(w16a16_backward)), METH_FASTCALL, nullptr},
+    {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(sample)), METH_FASTCALL, nullptr},
     {"w4a16_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(w4a16_linear)), METH_FASTCALL, nullptr},
     {"w4a16_linear_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(w4a16_linear_batch)), METH_FASTCALL, nullptr},
     {"w4a4_conv_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(w4a4_conv_batch)), METH_FASTCALL, nullptr},
@@ -328,9 +474,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 
 PyMODINIT_FUNC PyInit__marshal() {
     PyObject* m = PyModule_Create(&module);
-    PyObject* built_for = m ? Py_BuildValue("(lsnnnnnn)", (long)(PY_VERSION_HEX >> 16), QAIL_TORCH, (Py_ssize_t)sizeof(qail_wdesc),
+    PyObject* built_for = m ? Py_BuildValue("(lsnnnnnnnn)", (long)(PY_VERSION_HEX >> 16), QAIL_TORCH, (Py_ssize_t)sizeof(qail_wdesc),
                                             (Py_ssize_t)sizeof(qail_w4a16_item), (Py_ssize_t)sizeof(qail_conv_item), (Py_ssize_t)sizeof(qail_kv_cache),
-                                            (Py_ssize_t)sizeof(qail_requests), (Py_ssize_t)sizeof(qail_adapters))
+                                            (Py_ssize_t)sizeof(qail_requests), (Py_ssize_t)sizeof(qail_adapters), (Py_ssize_t)sizeof(qail_w16a16),
+                                            (Py_ssize_t)sizeof(qail_sampling))
                             : nullptr;
     if (!built_for || PyModule_AddObject(m, "built_for", built_for) < 0) {   // (takes the reference where it succeeds)
         Py_XDECREF(built_for);
