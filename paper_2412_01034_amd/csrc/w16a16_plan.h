@@ -44,9 +44,10 @@ __host__ __device__ inline TilePlace tile_place(const ProductPlan& pl, int b) {
 //
 // Up to 32 rows: tiles of 32 x 64, whose cost is the stream of the other operand; blocks for three a unit by shares of the contraction, which are
 // not worth the second launch before a tile has sixteen steps for each.
-// Beyond: the tile and the shares that cost least by what was measured (us): of 128 x 128 tiles two share a unit, 1.05 a step together and 0.62 alone, of 256 x 256 one
-// has it, 1.7 a step; beside that 5 and 12 for the way in and out of a tile, and for shares 3 for the second launch and their sums' way at 4 TB/s.  4096 x 4096 x 4096 takes 126
-// with 256 x 256 tiles and 148 with 128 x 128, 2056 x 4096 x 1024 33 with either, 289 x 4096 x 4096 25 with five shares of 128 x 128 tiles and 42 with one.
+// Beyond: the tile and the shares that cost least by what was measured (us a step, of two tiles that share a unit / of one that has it alone, and for the way in and out):
+//     128 x 128   1.0 / 0.62, 7        192 x 128 (straight)   1.4 / 0.78, 9        256 x 256   1.65, 10 (one a unit)
+// and for shares 3 for the second launch and their sums' way at 4 TB/s.  4096 x 4096 x 4096 takes 118 us with 256 x 256 tiles and 148 with 128 x 128, 2056 x 4096 x 1024 28
+// with 192 x 128 and 33 with either other, 289 x 4096 x 4096 25 with five shares of 128 x 128 tiles and 42 with one.
 inline ProductPlan plan_product(long long P, long long Q, long long R, bool turned, int units) {
     ProductPlan pl;
     pl.steps = (int)((R + kStepR - 1) / kStepR);
@@ -63,20 +64,27 @@ inline ProductPlan plan_product(long long P, long long Q, long long R, bool turn
         pl.splits = splits < 1 ? 1 : (int)splits;
         return pl;
     }
+    struct Tile {
+        int bp, bq;
+        double pair, alone, fixed;   // pair == 0: one a unit
+    };
+    const Tile kinds[] = {{128, 128, 1.0, 0.62, 7.}, {192, 128, 1.4, 0.78, 9.}, {256, 256, 0., 1.65, 10.}};
     double least = 1e300;
-    int tile = 128, shares = 1;
+    const Tile* tile = kinds;
+    int shares = 1;
     const int most = pl.steps / 4 < 1 ? 1 : pl.steps / 4 > 16 ? 16 : pl.steps / 4;
     for (int splits = 1; splits <= most; ++splits) {
         const double sums = splits == 1 ? 0. : 3. + splits * (double)P * (double)Q * 1e-6;
         const double steps = (double)((pl.steps + splits - 1) / splits);
-        const long long small = tiles_of(128, 128) * splits, large = tiles_of(256, 256) * splits;
-        const long long pairs = small / (2 * units), rest = small % (2 * units);
-        const double with_small = sums + (double)pairs * (1.05 * steps + 5.) + (rest == 0 ? 0. : rest <= units ? 0.62 * steps + 5. : 1.05 * steps + 5.);
-        const double with_large = sums + (double)((large + units - 1) / units) * (1.7 * steps + 12.);
-        if (with_small < least) least = with_small, tile = 128, shares = splits;
-        if (with_large < least) least = with_large, tile = 256, shares = splits;
+        for (const Tile& k : kinds) {
+            if (k.bp == 192 && turned) continue;
+            const long long blocks = tiles_of(k.bp, k.bq) * splits, full = k.pair > 0. ? 2ll * units : units, rounds = blocks / full, rest = blocks % full;
+            const double each = (k.pair > 0. ? k.pair : k.alone) * steps + k.fixed, alone = k.alone * steps + k.fixed;
+            const double cost = sums + (double)rounds * each + (rest == 0 ? 0. : rest <= units ? alone : each);
+            if (cost < least) least = cost, tile = &k, shares = splits;
+        }
     }
-    tiles_of(tile, tile);
+    tiles_of(tile->bp, tile->bq);
     pl.splits = shares;
     return pl;
 }
