@@ -34,7 +34,8 @@ static_assert(-kLowestBin < kBins, "bins for all parts");
 constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
 constexpr int kList = kBlock;                      // tokens of a bin that are listed: one a thread
 constexpr int kRanges = kBlock;
-constexpr int kKept = 4 * kBlock;                  // kept tokens of a group that are listed
+constexpr int kKept = 8 * kBlock;                  // kept tokens of a group that are listed
+static_assert(kGroup * kChunk <= 1 << 16, "their numbers");
 
 struct SampleArgs {
     const void* logits;
@@ -88,12 +89,13 @@ struct Shared {
     double part[kParts];                     // 2^(i / 512)
     union {
         u64 ranges[kRanges];                 // of keys
-        uint32_t list[kKept];                // numbers of tokens
+        uint32_t list[kList];                // numbers of tokens
+        uint16_t kept[kKept];                // ... from a group's first one
     };
     float wave_most[kWaves];
     u64 before;                              // what the chosen bin or segment has in front of it
-    int chosen, ties_before, listed;
-    uint32_t first;
+    int chosen, ties_before, listed, border_ties;
+    uint32_t first, border_key, equal;
 };
 
 // Inclusive sums over the block's threads in their order; `total`: of all of them.  The threads have met before.
@@ -259,8 +261,10 @@ struct Weight {
 __device__ __forceinline__ int bin_of(int part) { return -(part >> 3); }   // 0 for the largest logits
 static_assert(kBinParts == 1 << 3 && kParts == 1 << 9, "shifts");
 
-// The numbers of the tokens that a wave's threads have chosen from a group (Row::select) into list[0 .. most), in any order; sh.listed counts them all.
-__device__ __forceinline__ void append(Shared& sh, uint32_t* list, int most, int first, uint32_t bits) {
+// The numbers of the tokens that a wave's threads have chosen from a group (Row::select), counted from chunk `origin` on, into list[0 .. most), in any order; sh.listed
+// counts them all.
+template <typename Number>
+__device__ __forceinline__ void append(Shared& sh, Number* list, int most, int first, int origin, uint32_t bits) {
     const int lane = threadIdx.x % kWave, mine = __popc(bits);
     const int upto = (int)wave_scan((u64)mine), total = __builtin_amdgcn_readlane(upto, kWave - 1);
     if (total == 0) return;
@@ -270,7 +274,7 @@ __device__ __forceinline__ void append(Shared& sh, uint32_t* list, int most, int
     for (; bits != 0; ++at) {
         const int i = __clz(bits);
         bits &= ~(0x80000000u >> i);
-        if (at < most) list[at] = ((first + i / kPiece) * kBlock + threadIdx.x) * kPiece + i % kPiece;
+        if (at < most) list[at] = (Number)(((first - origin + i / kPiece) * kBlock + threadIdx.x) * kPiece + i % kPiece);
     }
 }
 
@@ -302,6 +306,36 @@ __device__ __forceinline__ Border border_by_keys(Shared& sh, Each each, uint32_t
     }
 }
 
+// The same of n <= kList listed tokens, one a thread.
+template <bool kCount>
+__device__ __forceinline__ Border border_of_list(Shared& sh, int n, bool held, uint32_t key, u64 mine, uint32_t base, uint32_t low, u64 aim, const Weight& weight) {
+    if (n > kWave)
+        return border_by_keys(
+            sh,
+            [&](auto f) __attribute__((always_inline)) {
+                if (held) f(key, kCount ? 1 : mine);
+            },
+            base, low, aim, [&](uint32_t k) { return kCount ? 1 : weight(value_of(k)); });
+    // few: the first wave compares them with each other, which saves the meetings of a search (one row of 32000 20.7 -> 18.3 us)
+    if (threadIdx.x < kWave) {
+        u64 front = 0;                                // what lies above
+        uint32_t equal = 0;
+        const u64 adds = !held ? 0 : kCount ? 1 : mine;
+        const int whose = held ? (int)key : 0;
+        for (int i = 0; i < n; ++i) {
+            const uint32_t other = (uint32_t)__builtin_amdgcn_readlane(whose, i);
+            const u64 w = lane_of(adds, i);
+            front += other > key ? w : 0;
+            equal += other == key;
+        }
+        if (held && front < aim && aim <= front + equal * adds) sh.border_key = key, sh.border_ties = (int)((aim - front - 1) / adds + 1);   // all of one value say the same
+    }
+    __syncthreads();
+    const Border b = {value_of(sh.border_key), sh.border_ties};
+    __syncthreads();
+    return b;
+}
+
 // The border in a bin of weights, whose tokens are to count (kCount) or weigh `aim` > 0; ahead: what those up to the border weigh (with kWeigh).  false: the bin has
 // more than about kList tokens.
 template <bool kCount, bool kWeigh, typename R>
@@ -313,7 +347,7 @@ __device__ __forceinline__ bool border_in_bin(Shared& sh, const R& row, int bin,
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
     for (int g = 0; g < row.chunks; g += kGroup)
-        append(sh, sh.list, kList, g, row.select(g, [&](float x) { return __builtin_amdgcn_fmed3f(x, from, to) == x; }));
+        append(sh, sh.list, kList, g, 0, row.select(g, [&](float x) { return __builtin_amdgcn_fmed3f(x, from, to) == x; }));
     __syncthreads();
     const int n = sh.listed;
     if (n > kList) {
@@ -333,12 +367,7 @@ __device__ __forceinline__ bool border_in_bin(Shared& sh, const R& row, int bin,
         mine = weight.of(part, rest);
     }
     __syncthreads();                                  // the list has been read: the ranges lie there as well
-    b = border_by_keys(
-        sh,
-        [&](auto f) __attribute__((always_inline)) {
-            if (held) f(key, kCount ? 1 : mine);
-        },
-        key_of(to), key_of(from), aim, [&](uint32_t k) { return kCount ? 1 : weight(value_of(k)); });
+    b = border_of_list<kCount>(sh, n, held, key, mine, key_of(to), key_of(from), aim, weight);
     if constexpr (kWeigh) {
         block_scan(sh, held && key > key_of(b.value) ? mine : 0, ahead);
         ahead += (u64)b.ties * weight(b.value);
@@ -401,16 +430,27 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     const bool by_count = top_k > 0 && top_k < V, by_share = top_p < 1.f;
     Border b = {-__builtin_inff(), 0};
     u64 kept = 0;                      // what the first top_k weigh
-    const auto all_keys = [&](bool weigh) {   // of the row, for where a bin has too many tokens
-        return [&, weigh](auto f) __attribute__((always_inline)) {
+    const auto weigh = [&]() __attribute__((always_inline)) {   // from the row itself
+        u64 some = 0;
+        row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int i = 0; i < kPiece; ++i)
+                if (x[i] > b.value) some += weight(x[i]);
+        });
+        block_scan(sh, some, kept);
+        kept += (u64)b.ties * weight(b.value);
+    };
+    const auto all_keys = [&](bool weights) {   // of the row, for where a bin has too many tokens
+        return [&, weights](auto f) __attribute__((always_inline)) {
             row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
 #pragma unroll 1
                 for (int i = 0; i < kPiece; ++i)
-                    if (x[i] >= weight.low) f(key_of(x[i]), weigh ? weight(x[i]) : 1);
+                    if (x[i] >= weight.low) f(key_of(x[i]), weights ? weight(x[i]) : 1);
             });
         };
     };
-    if (by_share) {
+    // the tokens' weights in bins
+    const auto fill = [&]() __attribute__((always_inline)) {
         row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < kPiece; ++i)
@@ -421,7 +461,10 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
                     atomicAdd(&sh.bins[bin_of(n)], weight.of(n, rest));
                 }
         });
-    }
+        __syncthreads();
+    };
+    const bool few = by_count && top_k <= kList;       // top_p's border is then looked for among the first top_k alone
+    if (by_share && !few) fill();
     if (by_count) {
         row.each([&](int, const float* x) __attribute__((always_inline)) {
 #pragma unroll
@@ -441,18 +484,10 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
             const int bin = sh.chosen;
             const u64 aim = (u64)top_k - sh.before;
             __syncthreads();
-            if (!(by_share ? border_in_bin<true, true>(sh, row, bin, weight, aim, b, kept) : border_in_bin<true, false>(sh, row, bin, weight, aim, b, kept))) {
+            if (!(by_share && !few ? border_in_bin<true, true>(sh, row, bin, weight, aim, b, kept) : border_in_bin<true, false>(sh, row, bin, weight, aim, b, kept))) {
                 b = border_by_keys(sh, all_keys(false), key_of(m), kLowest, (u64)top_k, [&](uint32_t) { return 1; });
-                u64 some = 0;
-                if (by_share)
-                    row.each_again(0, row.chunks, [&](int, const float* x) __attribute__((always_inline)) {
-#pragma unroll 1
-                        for (int i = 0; i < kPiece; ++i)
-                            if (x[i] > b.value) some += weight(x[i]);
-                    });
-                block_scan(sh, some, kept);
-                kept += (u64)b.ties * weight(b.value);
-            } else if (by_share) {
+                if (by_share && !few) weigh();
+            } else if (by_share && !few) {
                 u64 some = 0, front;
                 for (int i = threadIdx.x; i < bin; i += kBlock) some += sh.bins[i];
                 block_scan(sh, some, front);
@@ -462,7 +497,31 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
             __syncthreads();
         }
     }
-    if (by_share) {
+    bool by_list = false;
+    if (by_share && few) {
+        if (b.ties > 0) {
+            if (threadIdx.x == 0) sh.listed = 0;
+            __syncthreads();
+            for (int g = 0; g < row.chunks; g += kGroup) append(sh, sh.list, kList, g, 0, row.select(g, [&](float x) { return x >= b.value; }));
+            __syncthreads();
+            const int n = sh.listed;
+            by_list = n <= kList;                       // else many are equal to the last one
+            if (by_list) {
+                const bool held = (int)threadIdx.x < n;
+                const float x = held ? row.at(sh.list[threadIdx.x]) : 0.f;
+                const u64 mine = held ? weight(x) : 0;
+                block_scan(sh, x > b.value ? mine : 0, kept);   // (nobody writes the list before all have read it)
+                kept += (u64)b.ties * weight(b.value);
+                const double share = ceil((double)top_p * (double)kept);
+                b = border_of_list<false>(sh, n, held, key_of(x), mine, key_of(m), key_of(b.value), share > 1.0 ? (u64)share : 1, weight);
+            } else {
+                __syncthreads();
+                weigh();
+            }
+        }
+        if (!by_list) fill();
+    }
+    if (by_share && !by_list) {
         u64 aim = 0, none;
         find<kBins / kBlock>(sh, [&](int i) { return sh.bins[i]; }, [&](u64 total) {
             const double share = ceil((double)top_p * (double)(b.ties > 0 ? kept : total));
@@ -486,18 +545,19 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     const float from = on > 0 ? fminf(low, b.value) : low;   // (between them there may be what min_p does not keep)
     const int segments = row.chunks * kWaves;           // at most 512: one a thread
     if ((int)threadIdx.x < segments) sh.segment[threadIdx.x] = 0, sh.ties[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.equal = 0;
     for (int g = 0; g < row.chunks; g += kGroup) {
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
-        if (filtered) append(sh, sh.list, kKept, g, row.select(g, [&](float x) { return x >= from; }));
+        if (filtered) append(sh, sh.kept, kKept, g, g, row.select(g, [&](float x) { return x >= from; }));
         __syncthreads();
         const int listed = sh.listed;
         if (filtered && listed <= kKept) {
             for (int i = threadIdx.x; i < listed; i += kBlock) {
-                const uint32_t number = sh.list[i], at = number / (kWave * kPiece);
+                const uint32_t number = g * kChunk + sh.kept[i], at = number / (kWave * kPiece);
                 const float x = row.at(number);
                 if (x < low) {
-                    atomicAdd(&sh.ties[at], x == b.value ? 1u : 0u);
+                    if (x == b.value) atomicAdd(&sh.ties[at], 1u), atomicAdd(&sh.equal, 1u);
                 } else if (weight.down(x) >= least) {
                     atomicAdd(&sh.segment[at], weight(x));
                 }
@@ -519,7 +579,11 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
 #pragma unroll
                 for (int c = 0; c < kGroup; ++c) four |= (u64)__popc(bits >> (24 - kPiece * c) & 0xFFu) << (16 * c);
                 four = lane_of(wave_scan(four), kWave - 1);
-                if (lane < kGroup && g + lane < row.chunks) sh.ties[(g + lane) * kWaves + wave] = four >> (16 * lane) & 0xFFFF;
+                if (lane < kGroup && g + lane < row.chunks) {
+                    const uint32_t c = four >> (16 * lane) & 0xFFFF;
+                    sh.ties[(g + lane) * kWaves + wave] = c;
+                    if (c > 0) atomicAdd(&sh.equal, c);
+                }
             }
         }
         __syncthreads();
@@ -527,7 +591,9 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     const bool held = (int)threadIdx.x < segments;
     const u64 above = held ? sh.segment[threadIdx.x] : 0, room = b.ties;
     u64 ties_front = 0, here = above, all;
-    if (b.ties > 0) {                                   // else nobody asks
+    if (sh.equal <= room) {                             // all of them are kept
+        here += held ? sh.ties[threadIdx.x] * on : 0;
+    } else if (b.ties > 0) {
         const u64 equal = held ? sh.ties[threadIdx.x] : 0, ties_upto = block_scan(sh, equal, all);
         ties_front = ties_upto - equal;
         here += (min(ties_upto, room) - min(ties_front, room)) * on;
