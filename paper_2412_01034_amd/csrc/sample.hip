@@ -22,7 +22,7 @@ namespace {
 constexpr int kBlock = 1024, kWaves = kBlock / kWave;
 constexpr int kPiece = 8;                          // neighbouring tokens of a thread
 constexpr int kChunk = kBlock * kPiece;            // tokens of a pass over the block
-constexpr int kMostChunks = (1 << 18) / kChunk;
+constexpr int kMostChunks = (1 << 18) / kChunk + 1;   // (a row may begin inside a piece)
 constexpr int kGroup = 4;                          // chunks that are looked at together
 static_assert(kGroup * kPiece == 32, "a bit for each of a thread's tokens of a group");
 constexpr int kBins = 3 * kBlock;
@@ -134,15 +134,17 @@ __device__ __forceinline__ u64 find(Shared& sh, Get get, Aim aim_of) {
 }
 
 // The values of a row, 8 neighbouring tokens of a thread in each of its chunks; minus infinity behind the row.  kChunks of them stay in registers; 0: none.
-template <bool kBf16, bool kAligned, int kChunks>
+// A row that begins inside 16 bytes is read from their beginning on, so that all loads but the last are wide: its tokens are numbered from there (`skip` is the first one's
+// number), and the values in front of it, which are those of the row before, are minus infinity as well.
+template <bool kBf16, int kChunks>
 struct Row {
     const uint8_t* p;
-    int V, chunks;
+    int end, skip, chunks;
     float kept[kChunks > 0 ? kChunks : 1][kPiece];
 
     __device__ __forceinline__ void values(int c, float* f) const {
         const int j = (c * kBlock + threadIdx.x) * kPiece;
-        if (kAligned && j + kPiece <= V) {
+        if (j + kPiece <= end) {
             if constexpr (kBf16) {
                 unpack8(*reinterpret_cast<const uint4*>(p + 2ll * j), f);
             } else {
@@ -151,13 +153,19 @@ struct Row {
             }
         } else {
 #pragma unroll
+            for (int i = 0; i < kPiece; ++i) f[i] = j + i >= end ? -__builtin_inff() : at(j + i);
+        }
+        if (j < skip) {   // (a row that is shorter than its skip has no piece but this)
+#pragma unroll
             for (int i = 0; i < kPiece; ++i)
-                f[i] = j + i >= V ? -__builtin_inff()
-                       : kBf16    ? bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p)[j + i])
-                                  : reinterpret_cast<const float*>(p)[j + i];
+                if (i < skip) f[i] = -__builtin_inff();
         }
     }
-    __device__ __forceinline__ explicit Row(const void* at, int V_) : p(static_cast<const uint8_t*>(at)), V(V_), chunks((V_ + kChunk - 1) / kChunk) {
+    __device__ __forceinline__ Row(const uint8_t* first, int V) {
+        skip = (int)(reinterpret_cast<uintptr_t>(first) & 15u) / (kBf16 ? 2 : 4);
+        p = first - skip * (kBf16 ? 2 : 4);
+        end = V + skip;
+        chunks = (end + kChunk - 1) / kChunk;
         static_assert(kChunks <= 4, "one by one: a loop is unrolled too late for registers");
         if constexpr (kChunks > 0) values(0, kept[0]);
         if constexpr (kChunks > 1) values(1, kept[1]);
@@ -375,11 +383,11 @@ __device__ __forceinline__ bool border_in_bin(Shared& sh, const R& row, int bin,
     return true;
 }
 
-template <bool kBf16, bool kAligned, int kChunks>
+template <bool kBf16, int kChunks>
 __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     __shared__ Shared sh;
     const int r = blockIdx.x, V = a.V, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const Row<kBf16, kAligned, kChunks> row(static_cast<const uint8_t*>(a.logits) + (long long)r * a.stride * (kBf16 ? 2 : 4), V);
+    const Row<kBf16, kChunks> row(static_cast<const uint8_t*>(a.logits) + (long long)r * a.stride * (kBf16 ? 2 : 4), V);
     const float temperature = a.s.temperature ? a.s.temperature[r] : 1.f, top_p = a.s.top_p ? a.s.top_p[r] : 1.f, min_p = a.s.min_p ? a.s.min_p[r] : 0.f;
     const float u = a.u[r];
     const int top_k = a.s.top_k ? a.s.top_k[r] : 0;
@@ -420,7 +428,7 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
         }
         __syncthreads();
         if (threadIdx.x == 0) {
-            a.token[r] = (int32_t)sh.first;
+            a.token[r] = (int32_t)sh.first - row.skip;
             if (a.logprob) a.logprob[r] = 0.f;
         }
         return;
@@ -621,7 +629,7 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < kPiece; ++i) {
         if (at <= aim && aim < at + w[i]) {              // one token
-            a.token[r] = (c * kBlock + threadIdx.x) * kPiece + i;
+            a.token[r] = (c * kBlock + threadIdx.x) * kPiece + i - row.skip;
             if (a.logprob) a.logprob[r] = (float)(weight.down(x[i]) - log((double)all / kOne));
         }
         at += w[i];
@@ -634,9 +642,10 @@ hipError_t launch_sample(const void* logits, int type, int64_t stride, int R, in
                          uint32_t* errors, hipStream_t st) {
     const SampleArgs a = {logits, stride, V, s, u, token, logprob, errors};
     const bool aligned = stride % (type == QAIL_LOGITS_BF16 ? 8 : 4) == 0 || R == 1;
+    const int length = V + (aligned ? 0 : kPiece - 1);   // with what a row may skip
     const auto of_type = [&](auto bf16) {
         constexpr bool kBf16 = decltype(bf16)::value;
-        return !aligned ? sample_kernel<kBf16, false, 0> : V <= kChunk ? sample_kernel<kBf16, true, 1> : V <= 4 * kChunk ? sample_kernel<kBf16, true, 4> : sample_kernel<kBf16, true, 0>;
+        return length <= kChunk ? sample_kernel<kBf16, 1> : length <= 4 * kChunk ? sample_kernel<kBf16, 4> : sample_kernel<kBf16, 0>;
     };
     const auto kernel = type == QAIL_LOGITS_BF16 ? of_type(std::true_type{}) : of_type(std::false_type{});
     hipLaunchKernelGGL(kernel, dim3((unsigned)R), dim3(kBlock), 0, st, a);
