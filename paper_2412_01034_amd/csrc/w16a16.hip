@@ -188,8 +188,9 @@ __device__ __forceinline__ void copy16_from(const void* p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 
-// One operand's part of a step in LDS: kB rows (p or q) of 64 r.  Straight: kB rows of 128 bytes, piece s (16 bytes) of row i at s ^ (i & 7), so
-// that 8 consecutive rows' reads of one s hit 8 places.  Turned: 64 rows (r) of 2 kB bytes, piece s of row i at s ^ ((i & 3) << 2): a transposed read takes
+// One operand's part of a step in LDS: kB rows (p or q) of 64 r.  Straight: kB rows of 128 bytes, piece s (16 bytes) of row i at s ^ (i & 7) ^ (i / 8 & 1),
+// so that the 16 lanes that are served together, 16 consecutive rows of one s, hit 16 places of 256 bytes (with i & 7 alone rows 8 apart met: four cycles a read, 4096 x 11008 x
+// 4096 took WAS us instead of IS).  Turned: 64 rows (r) of 2 kB bytes, piece s of row i at s ^ ((i & 3) << 2): a transposed read takes
 // 64 bytes of each of four rows, which lie in four places of 256 bytes then (of 128, two rows, where kB is 64).
 template <int kB, bool kTurned, int kThreads>
 struct Operand {
@@ -197,7 +198,9 @@ struct Operand {
     static constexpr int kLoads = kBytes / 16 / kThreads;
     static constexpr int kPieces = kTurned ? kB / 8 : kStepR / 8;   // of a row
     static_assert(kLoads * 16 * kThreads == kBytes && (!kTurned || kB >= 64), "whole loads, whole swizzles");
-    __device__ static __forceinline__ int place(int row, int piece) { return piece ^ (!kTurned ? row & 7 : kB == 64 ? (row & 2) << 1 : (row & 3) << 2); }
+    __device__ static __forceinline__ int place(int row, int piece) {
+        return piece ^ (!kTurned ? (row & 7) ^ (row >> 3 & 1) : kB == 64 ? (row & 2) << 1 : (row & 3) << 2);
+    }
 
     const uint16_t* base;     // row 0 of the tile (straight) or its column 0 in row 0 (turned), at r = 0
     long long ld;
