@@ -222,3 +222,93 @@ def test_the_example_trains_its_embeddings(S):
     assert abs(loss - want.item()) <= 2.0 ** -7 * want.item()
     assert ((dtable.double() - table.grad).norm() / table.grad.norm()).item() <= 6 * 2.0 ** -8
     assert dtable.abs().amax(1).count_nonzero().item() == 7
+
+
+def test_large_tiles_captured(B):
+    """Products whose tiles need the opt-in for large LDS blocks, and shares of the contraction that pass through the workspace, in a graph."""
+    cases = [(2056, 1024, 512), (1030, 2048, 2048), (700, 256, 4096)]
+    held = []
+    for i, (M, N, K) in enumerate(cases):
+        w, b = normal((N, K), i, K ** -0.5), normal((N,), i + 1)
+        d = B.make_w16a16(w, b, "silu")
+        x, dy = normal((M, K), i + 2), normal((M, N), i + 3)
+        out = dict(y=torch.empty((M, N), dtype=BF16, device="cuda"), z=torch.empty((M, N), dtype=BF16, device="cuda"), dx=torch.empty_like(x),
+                   dweight=torch.empty((N, K), dtype=BF16, device="cuda"), dbias=torch.empty(N, device="cuda"))
+        held.append(((d, w, b), x, dy, out, space(max(B.qail_w16a16_workspace(d, M), B.qail_w16a16_backward_workspace(d, M)))))
+
+    def run():
+        for (d, *_), x, dy, o, ws in held:
+            B.qail_w16a16_linear(d, x, o["y"], ws, z=o["z"])
+            B.qail_w16a16_backward(d, x, dy, ws, z=o["z"], dx=o["dx"], dweight=o["dweight"], dbias=o["dbias"])
+
+    run()
+    want = [{k: v.clone() for k, v in h[3].items()} for h in held]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        for h in held:
+            for v in h[3].values():
+                v.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(h[3][k], w[k]) for h, w in zip(held, want) for k in w)
+
+
+def test_infinities_stay_in_their_rows(B):
+    """An infinity or NaN in a row of x, or in a row of W, reaches that row (column) of the outputs alone, behind the end of K and N too."""
+    for M, N, K in ((5, 70, 72), (130, 257, 264), (300, 72, 1000)):
+        x, w = normal((M, K), 1), normal((N, K), 2)
+        x[3, K - 1], w[7, K - 2] = float("inf"), float("nan")
+        d = B.make_w16a16(w)
+        y = torch.empty((M, N), device="cuda")
+        B.qail_w16a16_linear(d, x, y, space(B.qail_w16a16_workspace(d, M)))
+        bad = ~y.isfinite()
+        assert bad[3].all() and bad[:, 7].all() and bad.sum().item() == N + M - 1
+        dy = normal((M, N), 3)
+        dy[2, N - 1] = float("inf")
+        w = normal((N, K), 2)
+        d = B.make_w16a16(w)
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device="cuda")
+        x = normal((M, K), 1)
+        B.qail_w16a16_backward(d, x, dy, space(B.qail_w16a16_backward_workspace(d, M)), dx=dx, dweight=dw, dbias=db)
+        assert (~dx.isfinite()).sum().item() == K and not dx[2].isfinite().any()
+        assert (~dw.isfinite()).sum().item() == K and not dw[N - 1].isfinite().any()
+        assert (~db.isfinite()).nonzero().flatten().tolist() == [N - 1]
+
+
+def test_far_rows(B):
+    """Tensors beyond 2^32 bytes: a table and its gradient, logits whose rows lie 2^31 values apart, and rows of a linear."""
+    V, K = 70001, 32768
+    table = torch.empty((V, K), dtype=BF16, device="cuda")
+    for v in (0, 40000, 65535, 65536, V - 1):
+        table[v] = normal((K,), v)
+    ids = torch.tensor([V - 1, 0, 65536, 40000, 65535], dtype=torch.int32, device="cuda")
+    h = torch.empty((5, K), dtype=BF16, device="cuda")
+    B.qail_embed(table, ids, h)
+    assert torch.equal(h, table[ids.long()])
+    del table
+    dtable = torch.empty((V, K), device="cuda")
+    dtable[V - 2:] = 7
+    B.qail_embed_backward(ids, h, dtable, space(B.qail_embed_backward_workspace(V, K, 5)))
+    assert torch.equal(dtable[ids.long()], h.float()) and dtable[V - 2].abs().max() == 0
+    del dtable
+    wide = torch.empty((1 << 31) + (1 << 10), dtype=BF16, device="cuda")
+    logits = wide.as_strided((2, 1000), (1 << 31, 1))
+    logits.copy_(normal((2, 1000), 3))
+    token, u = torch.empty(2, dtype=torch.int32, device="cuda"), torch.tensor([0.3, 0.6], device="cuda")
+    B.qail_sample(logits, u, token)
+    near = torch.empty_like(token)
+    B.qail_sample(logits.contiguous(), u, near)
+    assert torch.equal(token, near)
+    del wide, logits
+    M, K, N = (1 << 20) + 100, 4096, 8
+    x, w = torch.zeros((M, K), dtype=BF16, device="cuda"), normal((N, K), 4, K ** -0.5)
+    x[-200:] = normal((200, K), 5)
+    d = B.make_w16a16(w)
+    y = torch.empty((M, N), device="cuda")
+    B.qail_w16a16_linear(d, x, y, space(B.qail_w16a16_workspace(d, M)))
+    want = x[-200:].double() @ w.double().t()
+    assert (y[-200:].double() - want).abs().max().item() <= (K + 2) * 2.0 ** -23 * (x[-200:].double().abs() @ w.double().abs().t()).max().item()
+    assert y[:-200].abs().max() == 0
