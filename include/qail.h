@@ -532,7 +532,8 @@ int qail_w4a16_linear_adapters_batch(const qail_w4a16_item* items, const qail_ad
 
 /* ------------------------------------------------- the policy's ends, in 16 bits --
  * Sec. 5.4 and the appendix "Analysis" quantise the backbone's linears; the table of embeddings, the head, the projector and the vision
- * side stay in 16 bits.  These calls are what a policy does before its first decoder layer and after its last one. */
+ * side stay in 16 bits.  These calls are what a policy does before its first decoder layer and after its last one.  Their workspaces carry
+ * nothing between calls; calls that share one must be ordered on one stream. */
 
 /* Rows of a table: h[t][k] = bf16(scale * table[ids[t]][k]), one rounding.
  *   table  bf16 [V][K]; ids int32 [T]; h bf16 [T][K] (not the table); scale finite
@@ -560,7 +561,7 @@ typedef enum {
 
 /* A linear whose weights stay in 16 bits: W bf16 [N][K], bias bf16 [N] or NULL; device memory, 16-byte aligned. */
 typedef struct {
-    int32_t N, K;             /* N >= 1; K a multiple of 8 */
+    int32_t N, K;             /* N >= 1; K >= 8, a multiple of 8 */
     int32_t activation;       /* qail_activation */
     const uint16_t* weight;
     const uint16_t* bias;
@@ -570,8 +571,8 @@ typedef struct {
  *     y[m][n] = act(z[m][n]) + residual[m][n]              fp32, rounded once
  *   x          bf16 [M][K]; residual bf16 [M][N] or NULL
  *   y, y_f32   bf16 or fp32 [M][N], exactly one of them; y may be the residual itself
- *   z_out      bf16 [M][N], the rounded z for the backward call, or NULL; not y or the residual
- * M, N, K <= 2^22, M * N, M * K and N * K <= 2^33.  The workspace (256-byte aligned; may be NULL where the query says 0) holds partial sums
+ *   z_out      bf16 [M][N], the rounded z for the backward call, or NULL
+ * No output may be an input otherwise, or another output.  M >= 1; M, N, K <= 2^22, M * N, M * K and N * K <= 2^33.  The workspace (256-byte aligned; may be NULL where the query says 0) holds partial sums
  * of output tiles whose K is divided among blocks. */
 int qail_w16a16_workspace(const qail_w16a16* d, int32_t M, size_t* bytes);
 int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const uint16_t* residual, uint16_t* z_out, uint16_t* y, float* y_f32,

@@ -1,5 +1,7 @@
 // C entry points of the policy's ends in 16 bits: argument checks and dispatch.  As in api.hip, every check is done on the host before the
 // first HIP call.
+#include <initializer_list>
+
 #include "qail_internal.h"
 
 using namespace qail;
@@ -27,6 +29,18 @@ int check_linear(const qail_w16a16* d, int32_t M) {
     if (M > (1 << 22) || d->N > (1 << 22) || d->K > (1 << 22) || (long long)M * d->N > kMost || (long long)M * d->K > kMost || (long long)d->N * d->K > kMost)
         return QAIL_ERR_UNSUPPORTED;
     return QAIL_OK;
+}
+
+// No output is an input or another output (NULL is neither).
+bool apart(std::initializer_list<const void*> in, std::initializer_list<const void*> out) {
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        if (!*o) continue;
+        for (const void* i : in)
+            if (i == *o) return false;
+        for (auto p = out.begin(); p != o; ++p)
+            if (*p == *o) return false;
+    }
+    return true;
 }
 
 }  // namespace
@@ -79,7 +93,7 @@ int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const
     if (e != QAIL_OK) return e;
     if (!d->weight || !x || !y == !y_f32) return QAIL_ERR_NULL;
     if (!aligned(d->weight) || !aligned(d->bias) || !aligned(x) || !aligned(residual) || !aligned(z_out) || !aligned(y) || !aligned(y_f32)) return QAIL_ERR_ALIGN;
-    if ((z_out && (z_out == y || z_out == residual || z_out == x || static_cast<void*>(z_out) == y_f32)) || y == x) return QAIL_ERR_SHAPE;
+    if (!apart({x, residual, d->weight, d->bias}, {z_out, y == residual ? nullptr : y, y_f32}) || (z_out && z_out == y)) return QAIL_ERR_SHAPE;
     const size_t need = w16a16_workspace(*d, M);
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return QAIL_ERR_WORKSPACE;
@@ -103,13 +117,7 @@ int qail_w16a16_backward(const qail_w16a16* d, const uint16_t* x, const uint16_t
     if (!d->weight || !dy == !dy_f32 || (!dx && !dweight && !dbias) || (dweight && !x) || (d->activation != QAIL_ACT_NONE && !z)) return QAIL_ERR_NULL;
     if (!aligned(d->weight) || !aligned(x) || !aligned(z) || !aligned(dy) || !aligned(dy_f32) || !aligned(dx) || !aligned(dweight) || !aligned(dbias))
         return QAIL_ERR_ALIGN;
-    const void* const in[] = {x, z, dy, dy_f32, d->weight};
-    const void* const out[] = {dx, dweight, dbias};
-    for (int i = 0; i < 3; ++i) {
-        for (const void* p : in)
-            if (p && p == out[i]) return QAIL_ERR_SHAPE;
-        if (out[i] && out[i] == out[(i + 1) % 3]) return QAIL_ERR_SHAPE;
-    }
+    if (!apart({x, z, dy, dy_f32, d->weight}, {dx, dweight, dbias})) return QAIL_ERR_SHAPE;
     if (!workspace || workspace_bytes < w16a16_back_workspace(*d, M)) return QAIL_ERR_WORKSPACE;
     if (!aligned<256>(workspace)) return QAIL_ERR_ALIGN;
     return hip_status(launch_w16a16_back(*d, x, z, dy, dy_f32, M, dx, dweight, dbias, workspace, static_cast<hipStream_t>(stream)));

@@ -69,12 +69,13 @@ def test_linear_refusals(B):
         return B.lib().qail_w16a16_linear(None if none else ctypes.byref(linear(B, **d)), *a.values(), None)
 
     expect(B.QAIL_ERR_SHAPE, call, dict(M=0), dict(M=-1), dict(d=dict(N=0)), dict(d=dict(K=0)), dict(d=dict(K=60)), dict(y=OK), dict(z=0x20000),
-           dict(z=0x30000, residual=0x30000), dict(z=OK))
+           dict(z=0x30000, residual=0x30000), dict(z=OK), dict(y=None, y32=0x30000, residual=0x30000), dict(y=None, y32=OK), dict(y=None, y32=0x30000, z=0x30000))
     expect(B.QAIL_ERR_UNSUPPORTED, call, dict(d=dict(activation=5)), dict(d=dict(activation=-1)), dict(M=(1 << 22) + 1), dict(d=dict(N=(1 << 22) + 8)),
            dict(d=dict(K=(1 << 22) + 8)), dict(M=1 << 22, d=dict(N=4096)), dict(M=1 << 22, d=dict(K=4096)), dict(d=dict(N=1 << 20, K=1 << 14)))
     expect(B.QAIL_ERR_NULL, call, dict(none=True), dict(x=None), dict(y=None), dict(y32=OK), dict(d=dict(weight=None)))
     expect(B.QAIL_ERR_ALIGN, call, dict(x=ODD), dict(y=0x20008), dict(y=None, y32=ODD), dict(residual=ODD), dict(z=ODD), dict(d=dict(weight=ODD)), dict(d=dict(bias=ODD)))
     big = dict(N=4096, K=4096)                    # few tiles: K is divided
+    assert call(d=big, y=0x30000, residual=0x30000, ws=None) == B.QAIL_ERR_WORKSPACE    # in place: gets past the pointers
     n = B.qail_w16a16_workspace(linear(B, **big), 4)
     assert n >= 2 * 4 * 4096 * 4
     expect(B.QAIL_ERR_WORKSPACE, call, dict(d=big, ws=None), dict(d=big, bytes=n - 1))

@@ -150,7 +150,7 @@ def test_rows_of_wider_tensors(B, dtype):
     check(B, odd, randoms(5, 2), [0.8] * 5, None, [0.9] * 5)
     check(B, odd[:, :999], randoms(5, 3))
     check(B, wide[::2, :777], randoms(3, 4), None, [20] * 3)
-    for V in (1, 3, 5, 8187, 8189, 8193, 32763, 32767, 40003):   # rows that skip 0 to 7 values, whose neighbours would be drawn
+    for V in (1, 3, 5, 8187, 8189, 8193, 32763, 32767, 40003, (1 << 18) - 1):   # rows that skip 0 to 7 values, whose neighbours would be drawn
         x = rows(9, V, V, dtype)
         x[4] += 30
         check(B, x, randoms(9, V), [1.0] * 8 + [0.0], [0, 7, 0, V, 2, 0, 0, 1, 0], [1.0, 0.9, 0.8, 1.0, 1.0, 0.99, 1.0, 1.0, 1.0], [0.0] * 6 + [0.1, 0.0, 0.0])
