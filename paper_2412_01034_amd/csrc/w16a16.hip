@@ -118,17 +118,31 @@ struct Epilogue {
     int act, Q;
 };
 
-// Outputs p, q .. q + 7 from their sums.  Rows of Q % 8 == 0 start on 16 bytes; others go value by value.
+// 8 values at any address that their type allows, in loads and stores of 16 bytes all the same (rows of an odd number of values; value by value the kernel of dz took
+// 67 us for 3468 x 5073, now 34, and 310 x 4096 x 14905 96 us, 17 more than 14904).
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef u32x4_t any_half8_t __attribute__((aligned(2)));
+typedef f32x4_t any_float4_t __attribute__((aligned(4)));
+__device__ __forceinline__ void load8(const uint16_t* p, float* v) {
+    const u32x4_t t = *reinterpret_cast<const any_half8_t*>(p);
+    unpack8(make_uint4(t.x, t.y, t.z, t.w), v);
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
+    const uint4 t = pack8(v);
+    *reinterpret_cast<any_half8_t*>(p) = u32x4_t{t.x, t.y, t.z, t.w};
+}
+
+// Outputs p, q .. q + 7 from their sums; the last ones of a row, fewer than 8, value by value.
 __device__ __forceinline__ void finish8(const Epilogue& e, long long p, int q, float* v) {
     const size_t at = (size_t)p * e.Q + q;
-    if (e.Q % 8 == 0) {
+    if (q + 8 <= e.Q) {
         float t[8];
         if (e.bias) {
-            unpack8(*reinterpret_cast<const uint4*>(e.bias + q), t);
+            load8(e.bias + q, t);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += t[i];
         }
-        if (e.z) *reinterpret_cast<uint4*>(e.z + at) = pack8(v);
+        if (e.z) store8(e.z + at, v);
         if (e.act != QAIL_ACT_NONE) {
             if (e.y) {
 #pragma unroll
@@ -139,15 +153,15 @@ __device__ __forceinline__ void finish8(const Epilogue& e, long long p, int q, f
             }
         }
         if (e.residual) {
-            unpack8(*reinterpret_cast<const uint4*>(e.residual + at), t);
+            load8(e.residual + at, t);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += t[i];
         }
         if (e.y) {
-            *reinterpret_cast<uint4*>(e.y + at) = pack8(v);
+            store8(e.y + at, v);
         } else {
-            reinterpret_cast<float4*>(e.y32 + at)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(e.y32 + at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            reinterpret_cast<any_float4_t*>(e.y32 + at)[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<any_float4_t*>(e.y32 + at)[1] = f32x4_t{v[4], v[5], v[6], v[7]};
         }
         return;
     }
@@ -332,7 +346,7 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
     multiply(1);
 
     // Out through LDS, 32 rows of a wave at a time: the lanes then have 8 neighbouring outputs of a row, a row's lanes lie beside each other, and the
-    // epilogue is a loop (unrolled over the registers its code was ten times the instruction cache).  Piece c (16 bytes) of row p lies at c ^ (p & 15).
+    // epilogue is a loop (unrolled over the registers its code is far longer than the instruction cache).  Piece c (16 bytes) of row p lies at c ^ (p & 15).
     constexpr int kRow = 32 * FQ, kPiecesOut = kRow / 4, kLanes = kRow / 8;   // floats and pieces of a row; lanes that share one
     static_assert(kWP * kWQ * 32 * kRow * 4 <= kSlots * kSlot && kPiecesOut >= 8, "the waves' rows fit the ring");
     constexpr int kMask = kPiecesOut < 16 ? kPiecesOut - 1 : 15;
@@ -373,11 +387,20 @@ __global__ __launch_bounds__(256) void w16a16_sum_kernel(const float* __restrict
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x, all = (long long)P * n8;
     if (i >= all) return;
     float v[8] = {};
-    const float4* from = reinterpret_cast<const float4*>(partial) + 2 * i;
-    for (int s = 0; s < splits; ++s, from += 2 * all) {
-        const float4 lo = from[0], hi = from[1];
-        v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w;
-        v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+    const float4* const from = reinterpret_cast<const float4*>(partial) + 2 * i;
+    for (int s = 0; s < splits; s += 4) {   // four shares requested at a time; behind the last one that one again
+        float4 lo[4], hi[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const float4* const share = from + 2 * all * min(s + t, splits - 1);
+            lo[t] = share[0], hi[t] = share[1];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (s + t < splits) {
+                v[0] += lo[t].x, v[1] += lo[t].y, v[2] += lo[t].z, v[3] += lo[t].w;
+                v[4] += hi[t].x, v[5] += hi[t].y, v[6] += hi[t].z, v[7] += hi[t].w;
+            }
     }
     finish8(e, i / n8, (int)(i % n8) * 8, v);
 }
@@ -400,36 +423,41 @@ __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restri
     const int across = (ld + kDzCols - 1) / kDzCols, bx = blockIdx.x % across, by = blockIdx.x / across;
     const int c = threadIdx.x % 32, n = bx * kDzCols + 8 * c, slice = threadIdx.x / 32;
     const int m0 = by * rows, m1 = min(M, m0 + rows);
-    const bool whole = N % 8 == 0;
     float sum[8] = {};
-    if (n < ld) {
+    const auto add = [&](int m, float* v, const float* s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (act != QAIL_ACT_NONE) v[i] *= slope(act, s[i]);
+            sum[i] += v[i];
+        }
+        if (dz) *reinterpret_cast<uint4*>(dz + (size_t)m * ld + n) = pack8(v);
+    };
+    if (n + 8 <= N) {
 #pragma unroll 2
         for (int m = m0 + slice; m < m1; m += kDzSlices) {
             const size_t at = (size_t)m * N + n;
             float v[8], s[8];
-            if (whole) {
-                uint4 kept;
-                if (act != QAIL_ACT_NONE) kept = *reinterpret_cast<const uint4*>(z + at);
-                if (dy) unpack8(*reinterpret_cast<const uint4*>(dy + at), v);
-                else {
-                    const float4 lo = reinterpret_cast<const float4*>(dy32 + at)[0], hi = reinterpret_cast<const float4*>(dy32 + at)[1];
-                    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-                }
-                if (act != QAIL_ACT_NONE) unpack8(kept, s);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool in = n + i < N;
-                    v[i] = !in ? 0.f : dy ? bf16_bits_to_f32(dy[at + i]) : dy32[at + i];
-                    s[i] = in && act != QAIL_ACT_NONE ? bf16_bits_to_f32(z[at + i]) : 0.f;
-                }
+            u32x4_t kept;
+            if (act != QAIL_ACT_NONE) kept = *reinterpret_cast<const any_half8_t*>(z + at);
+            if (dy) load8(dy + at, v);
+            else {
+                const f32x4_t lo = reinterpret_cast<const any_float4_t*>(dy32 + at)[0], hi = reinterpret_cast<const any_float4_t*>(dy32 + at)[1];
+                v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
             }
+            if (act != QAIL_ACT_NONE) unpack8(make_uint4(kept.x, kept.y, kept.z, kept.w), s);
+            add(m, v, s);
+        }
+    } else if (n < N) {
+        for (int m = m0 + slice; m < m1; m += kDzSlices) {
+            const size_t at = (size_t)m * N + n;
+            float v[8], s[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (act != QAIL_ACT_NONE) v[i] = whole || n + i < N ? v[i] * slope(act, s[i]) : 0.f;
-                sum[i] += v[i];
+                const bool in = n + i < N;
+                v[i] = !in ? 0.f : dy ? bf16_bits_to_f32(dy[at + i]) : dy32[at + i];
+                s[i] = in && act != QAIL_ACT_NONE ? bf16_bits_to_f32(z[at + i]) : 0.f;
             }
-            if (dz) *reinterpret_cast<uint4*>(dz + (size_t)m * ld + n) = pack8(v);
+            add(m, v, s);   // (slopes at 0 are finite: what lies behind N stays 0)
         }
     }
     if (!sums) return;
@@ -470,7 +498,7 @@ hipError_t launch_tiles(const ProductArgs& g, hipStream_t st) {
     constexpr int lds = kSlots * (kBP + kBQ) * 2 * kStepR;
     static_assert(lds <= 160 * 1024, "the ring fits LDS");
     const auto kernel = w16a16_product_kernel<kBP, kBQ, kWP, kWQ, kTA, kTB, kSlots>;
-    if (lds > 64 * 1024) {
+    if (lds > 64 * 1024) {   // needs an opt-in, on every device
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
@@ -485,9 +513,12 @@ hipError_t launch_product(ProductArgs g, float* partial, hipStream_t st) {
     g.e.Q = g.Q;
     hipError_t e = hipErrorInvalidValue;
     if (g.plan.bp == 256) e = launch_tiles<256, 256, 2, 4, kTA, kTB, 2>(g, st);
-    if (g.plan.bp == 128) e = launch_tiles<128, 128, 2, 2, kTA, kTB, 2>(g, st);
+    // A tile that has its unit to itself may keep four steps in LDS, which cover the way from memory: 3468 x 64 x 5072 (a gradient) 14.8 -> 12.8 us, 310 x 4096 x 14904 81 -> 73;
+    // not where many row tiles share a column's lines, which the first of them brings into L2: 1500 x 4096 x 4096, eight of 192, 58 -> 61.
+    const bool deep = g.plan.blocks() <= device_cu_count() && (g.plan.bp == 128 || g.plan.tiles_p <= 4);
+    if (g.plan.bp == 128) e = deep ? launch_tiles<128, 128, 2, 2, kTA, kTB, 4>(g, st) : launch_tiles<128, 128, 2, 2, kTA, kTB, 2>(g, st);
     if constexpr (!kTA)
-        if (g.plan.bp == 192) e = launch_tiles<192, 128, 2, 2, kTA, kTB, 2>(g, st);
+        if (g.plan.bp == 192) e = deep ? launch_tiles<192, 128, 2, 2, kTA, kTB, 4>(g, st) : launch_tiles<192, 128, 2, 2, kTA, kTB, 2>(g, st);
     if constexpr (!kTA)
         if (g.plan.bp == 32) e = launch_tiles<32, 64, 1, 2, kTA, kTB, 4>(g, st);
     if (e != hipSuccess || g.plan.splits == 1) return e;

@@ -82,7 +82,8 @@ def check_gradient(B, ids, V, K, scale, seed, accumulate=False):
 @pytest.mark.parametrize("T, V, K, scale, holes", [
     (1, 1, 8, 1.0, 0), (1, 255, 8, 1.0, 0), (5, 256, 72, 2.0, 1), (32, 3, 1024, 1.0, 0), (33, 1, 1032, 1.0, 0), (63, 2, 64, -0.5, 0), (64, 2, 64, 1.0, 3),
     (1000, 7, 200, 1.0, 100), (4096, 65, 64, 1.0, 0), (4096, 70000, 16, 1.0, 9), (4097, 65, 64, 0.25, 11), (4097, 300, 40, 1.0, 0), (9000, 70000, 8, 1.0, 0),
-    (12289, 5, 136, 1.0, 12000), (30000, 2000, 48, 3.0, 17), (65536, 300, 8, 1.0, 0), (65537, 300, 8, 1.0, 5), (70001, 70000, 8, 1.0, 5), (257, 1000, 4104, 1.0, 0), (5000, 1, 8, 1.0, 4999)])
+    (12289, 5, 136, 1.0, 12000), (30000, 2000, 48, 3.0, 17), (65536, 300, 8, 1.0, 0), (65537, 300, 8, 1.0, 5), (70001, 70000, 8, 1.0, 5), (257, 1000, 4104, 1.0, 0), (5000, 1, 8, 1.0, 4999),
+    (2, 1, 8, 1.0, 1), (255, 3, 72, 1.0, 0), (256, 40, 264, 1.0, 100), (256, 1 << 23, 8, 1.0, 3)])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient(B, T, V, K, scale, holes, accumulate):
     check_gradient(B, numbers(T, V, T + V, holes), V, K, scale, 5, accumulate)

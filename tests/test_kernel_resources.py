@@ -64,5 +64,5 @@ def test_kernels_of_the_policys_ends_use_no_scratch():
     """Sums, fragments and a row of logits lie in registers."""
     names = ("embed_", "w16a16_", "sample_kernel")
     found = {k[".name"]: (k[".private_segment_fixed_size"], k[".vgpr_spill_count"]) for k in kernels(ensure_built().LIB_PATH) if any(n in k[".name"] for n in names)}
-    assert len(found) == 28, sorted(found)   # lookup, 5 of the sort, parts, 2 of the rows; 10 products and 3 beside them; 6 of the sampling
+    assert len(found) == 34, sorted(found)   # lookup, 6 of the sort, parts, 2 of the rows; 15 products and 3 beside them; 6 of the sampling
     assert {n: v for n, v in found.items() if v != (0, 0)} == {}
