@@ -3,9 +3,10 @@
 // The gradient adds up the rows of dh that belong to a token.  Atomics would add them in any order, so the tokens are sorted first (stable: a
 // token's rows stay in the order of their places), and whoever writes row v of the gradient reads its rows one after the other.  A token that comes
 // more than kPart times is added up in parts of kPart sorted places by other blocks before, whose sums are then added in their order.
-// What is sorted are pairs (token, place), 8 bits of the token at a time, in tiles of kTile, whose pairs stay in LDS for all digits: equal digits are found by comparing
-// lanes; up to kFew pairs are compared with each other instead.  Up to kMergeTiles tiles are then merged by rank: a pair's place is its own tile's plus how many pairs of each other tile come before it, 12 probes a
-// tile.  More of them are sorted digit by digit over all tiles: their counts, the counts' sums, and the move.
+// What is sorted are pairs (token, place).  Up to kTile of them are ranked by comparing each with all others, a wave a pair, over the whole chip (2312 tokens 4.8 us, 4096 6.2; by digits
+// in one block 9.8 and 10.8).  More of them are sorted in tiles of kTile, 8 bits of the token at a time, whose pairs stay in LDS for all digits: equal digits are found by
+// comparing lanes.  Up to kMergeTiles tiles are then merged by rank: a pair's place is its own tile's plus how many pairs of each other tile come before it, 12 probes a
+// tile (24577 tokens: 11.7 and 6.1 us).  More of them are sorted digit by digit over all tiles: their counts, the counts' sums, and the move.
 #include <algorithm>
 
 #include "qail_internal.h"
@@ -165,27 +166,25 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_tiles_kernel(const int3
         if (held[i]) keys[first + place_in_tile(i)] = key[i], places[first + place_in_tile(i)] = first + place[i];
 }
 
-constexpr int kFew = 256;
-
-// Up to kFew pairs: each is compared with all others, by four threads, so that nobody waits for a digit (44 tokens of 13716 7.7 us by digits).
-__global__ __launch_bounds__(4 * kFew) void embed_sort_few_kernel(const int32_t* __restrict__ ids, int T, int V, uint32_t* __restrict__ keys, uint32_t* __restrict__ places,
-                                                                  uint32_t* __restrict__ errors) {
-    static_assert(4 * kFew == kSortBlock, "report() counts a block's ids");
-    __shared__ __attribute__((aligned(16))) uint32_t all[kFew];
-    report(ids, T, V, errors);
-    if (threadIdx.x < kFew) all[threadIdx.x] = (int)threadIdx.x < T ? token_key(ids[threadIdx.x], V) : 0xFFFFFFFFu;
+// One tile: a wave compares a pair with all others.  Bound by the vector unit: T^2 comparisons of two instructions.
+__global__ __launch_bounds__(kSortBlock) void embed_rank_kernel(const int32_t* __restrict__ ids, int T, int V, uint32_t* __restrict__ keys, uint32_t* __restrict__ places,
+                                                                uint32_t* __restrict__ errors) {
+    __shared__ __attribute__((aligned(16))) uint32_t all[kTile];
+    if (blockIdx.x == 0) report(ids, T, V, errors);
+    for (int i = threadIdx.x; i < (T + 3) / 4 * 4; i += kSortBlock) all[i] = i < T ? token_key(ids[i], V) : 0xFFFFFFFFu;
     __syncthreads();
-    const int i = threadIdx.x / 4, quarter = threadIdx.x % 4;
+    const int i = blockIdx.x * kSortWaves + threadIdx.x / kWave, lane = threadIdx.x % kWave;
     if (i >= T) return;
     const uint32_t key = all[i];
-    int to = 0;
-    for (int j = 4 * quarter; j < T; j += 16) {   // places behind T hold the largest number
+    uint32_t to = 0;
+#pragma unroll 2
+    for (int j = 4 * lane; j < T; j += 4 * kWave) {   // what stands in front counts if it is no larger, what stands behind if it is smaller
         const uint4 k = *reinterpret_cast<const uint4*>(&all[j]);
-        to += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) + (k.z < key || (k.z == key && j + 2 < i)) + (k.w < key || (k.w == key && j + 3 < i));
+        to += (k.x < key + (j < i)) + (k.y < key + (j + 1 < i)) + (k.z < key + (j + 2 < i)) + (k.w < key + (j + 3 < i));
     }
-    to += __shfl_xor(to, 1, kWave);
-    to += __shfl_xor(to, 2, kWave);
-    if (quarter == 0) keys[to] = key, places[to] = i;
+#pragma unroll
+    for (int o = 1; o < kWave; o *= 2) to += __shfl_xor(to, o, kWave);
+    if (lane == 0) keys[to] = key, places[to] = i;
 }
 
 // How many of n ascending keys are below v.
@@ -201,20 +200,18 @@ __device__ __forceinline__ int below(const uint32_t* keys, int n, uint32_t v) {
 
 constexpr int kMergeTiles = 16;
 
-// Sorted tiles into one list.
+// Sorted tiles into one list: kMergeTiles lanes a pair, each with a tile of its own, so that a pair waits for 12 trips to the L2 and not for as many per tile (24577 tokens
+// 13.4 -> 6.1 us).
 __global__ __launch_bounds__(256) void embed_merge_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ places, int T, uint32_t* __restrict__ keys_to,
                                                           uint32_t* __restrict__ places_to) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
+    const int i = blockIdx.x * (256 / kMergeTiles) + threadIdx.x / kMergeTiles, s = threadIdx.x % kMergeTiles;
     if (i >= T) return;
-    const int tile = i / kTile, tiles = (T + kTile - 1) / kTile;
+    const int tile = i / kTile, first = s * kTile;
     const uint32_t key = keys[i];
-    int to = i - tile * kTile;
-    for (int s = 0; s < tiles; ++s) {
-        const int first = s * kTile;
-        if (s != tile) to += below(keys + first, min(kTile, T - first), s < tile ? key + 1 : key);
-    }
-    keys_to[to] = key;
-    places_to[to] = places[i];
+    int to = s == tile ? i - first : first < T ? below(keys + first, min(kTile, T - first), s < tile ? key + 1 : key) : 0;
+#pragma unroll
+    for (int o = 1; o < kMergeTiles; o *= 2) to += __shfl_xor(to, o, kWave);
+    if (s == 0) keys_to[to] = key, places_to[to] = places[i];
 }
 
 // Many tiles, one digit: the tiles' counts, [digit][tile] ...  (keys == NULL: the first digit, of ids)
@@ -442,12 +439,11 @@ hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, floa
     // eight blocks a compute unit, and no fewer rows than threads for them
     const int across = (K + 4 * g.lanes - 1) / (4 * g.lanes), groups = 256 / g.lanes;
     g.rows = (int)std::min<long long>(kMostRows, std::max<long long>(groups, (long long)V * across / (8 * device_cu_count())));
-    if (T > 0 && T <= kFew) {
-        hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(4 * kFew), 0, st, ids, T, V, pair[0], pair[1], errors);
-    } else if (at.tiles > 0 && at.tiles <= kMergeTiles) {
-        uint32_t* const* const to = at.tiles > 1 ? pair + 2 : pair;
-        hipLaunchKernelGGL(embed_sort_tiles_kernel, dim3(at.tiles), dim3(kSortBlock), 0, st, ids, T, V, passes, to[0], to[1], errors);
-        if (at.tiles > 1) hipLaunchKernelGGL(embed_merge_kernel, dim3((T + 255) / 256), dim3(256), 0, st, to[0], to[1], T, pair[0], pair[1]);
+    if (at.tiles == 1) {
+        hipLaunchKernelGGL(embed_rank_kernel, dim3((T + kSortWaves - 1) / kSortWaves), dim3(kSortBlock), 0, st, ids, T, V, pair[0], pair[1], errors);
+    } else if (at.tiles > 1 && at.tiles <= kMergeTiles) {
+        hipLaunchKernelGGL(embed_sort_tiles_kernel, dim3(at.tiles), dim3(kSortBlock), 0, st, ids, T, V, passes, pair[2], pair[3], errors);
+        hipLaunchKernelGGL(embed_merge_kernel, dim3((T * kMergeTiles + 255) / 256), dim3(256), 0, st, pair[2], pair[3], T, pair[0], pair[1]);
     } else if (at.tiles > kMergeTiles) {
         for (int pass = 0; pass < passes; ++pass) {
             const uint32_t* const keys = pass ? pair[2 * (pass & 1)] : nullptr;
