@@ -546,7 +546,7 @@ int qail_embed(const uint16_t* table, int32_t V, int32_t K, const int32_t* ids, 
 /* Its gradient: dtable[v][k] = scale * sum of dh[t][k] over the t with ids[t] == v, fp32 [V][K], in an order that depends on ids alone, so
  * that the same call always gives the same bits; accumulate != 0 adds it to what dtable holds and leaves the rows without a token alone,
  * 0 overwrites all of it.  Negative ids and ids >= V have no row; the latter are counted as above.  What dh holds in their rows is not used.
- * Sizes as above, T = 0 among them (with accumulate == 0 the gradient is zero).  The workspace is 256-byte aligned. */
+ * dtable is neither dh nor ids.  Sizes as above, T = 0 among them (with accumulate == 0 the gradient is zero).  The workspace is 256-byte aligned. */
 int qail_embed_backward_workspace(int32_t V, int32_t K, int32_t T, size_t* bytes);
 int qail_embed_backward(const int32_t* ids, const uint16_t* dh, int32_t T, float scale, int32_t V, int32_t K, int32_t accumulate, float* dtable,
                         uint32_t* errors, void* workspace, size_t workspace_bytes, void* stream);
@@ -572,8 +572,8 @@ typedef struct {
  *   x          bf16 [M][K]; residual bf16 [M][N] or NULL
  *   y, y_f32   bf16 or fp32 [M][N], exactly one of them; y may be the residual itself
  *   z_out      bf16 [M][N], the rounded z for the backward call, or NULL
- * No output may be an input otherwise, or another output.  M >= 1; M, N, K <= 2^22, M * N, M * K and N * K <= 2^33.  The workspace (256-byte aligned; may be NULL where the query says 0) holds partial sums
- * of output tiles whose K is divided among blocks. */
+ * No output may be an input otherwise, or another output.  M >= 1; M, N, K <= 2^22, M * N, M * K and N * K <= 2^33.  The workspace (256-byte
+ * aligned; may be NULL where the query says 0) holds partial sums of output tiles whose K is divided among blocks. */
 int qail_w16a16_workspace(const qail_w16a16* d, int32_t M, size_t* bytes);
 int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const uint16_t* residual, uint16_t* z_out, uint16_t* y, float* y_f32,
                        void* workspace, size_t workspace_bytes, void* stream);

@@ -73,6 +73,7 @@ int qail_embed_backward(const int32_t* ids, const uint16_t* dh, int32_t T, float
     if (!finite(scale)) return QAIL_ERR_SHAPE;
     if (!dtable || (T > 0 && (!ids || !dh))) return QAIL_ERR_NULL;
     if (!aligned<4>(ids) || !aligned(dh) || !aligned(dtable) || !aligned<4>(errors)) return QAIL_ERR_ALIGN;
+    if (T > 0 && !apart({ids, dh}, {dtable})) return QAIL_ERR_SHAPE;
     if (T == 0 && accumulate) return QAIL_OK;
     if (!workspace || workspace_bytes < embed_back_workspace(K, T)) return QAIL_ERR_WORKSPACE;
     if (!aligned<256>(workspace)) return QAIL_ERR_ALIGN;

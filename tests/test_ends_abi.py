@@ -41,11 +41,11 @@ def test_embed_backward_refusals(B):
     n = B.qail_embed_backward_workspace(100, 64, 5000)
 
     def call(**change):
-        a = dict(ids=OK, dh=OK, T=5000, scale=1.0, V=100, K=64, accumulate=0, dtable=OK, errors=None, ws=OK, bytes=n)
+        a = dict(ids=OK, dh=OK, T=5000, scale=1.0, V=100, K=64, accumulate=0, dtable=OK + 4096, errors=None, ws=OK, bytes=n)
         a.update(change)
         return B.lib().qail_embed_backward(*a.values(), None)
 
-    expect(B.QAIL_ERR_SHAPE, call, dict(V=0), dict(K=12), dict(T=-1), dict(scale=NAN))
+    expect(B.QAIL_ERR_SHAPE, call, dict(V=0), dict(K=12), dict(T=-1), dict(scale=NAN), dict(dtable=OK))
     expect(B.QAIL_ERR_UNSUPPORTED, call, dict(K=65544), dict(V=1 << 24), dict(T=1 << 24))
     expect(B.QAIL_ERR_NULL, call, dict(ids=None), dict(dh=None), dict(dtable=None))
     expect(B.QAIL_ERR_ALIGN, call, dict(ids=OK + 2), dict(dh=ODD), dict(dtable=ODD), dict(ws=OK + 16), dict(errors=OK + 1))
