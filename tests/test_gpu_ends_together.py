@@ -312,3 +312,48 @@ def test_far_rows(B):
     want = x[-200:].double() @ w.double().t()
     assert (y[-200:].double() - want).abs().max().item() <= (K + 2) * 2.0 ** -23 * (x[-200:].double().abs() @ w.double().abs().t()).max().item()
     assert y[:-200].abs().max() == 0
+
+
+def test_plain_calls_give_the_same_by_either_way(B, monkeypatch):
+    """The calls as C++ marshals them and as Python does, with every optional tensor; and what neither of them takes."""
+    m = Model(B, 301, 64, 72, 40, 8)
+    prepare_training(B, m)
+    choice, z = choices(40, 4), torch.empty((8, 64), dtype=BF16, device="cuda")
+    dp, dbias, dx = torch.empty_like(m.projector), torch.empty(64, device="cuda"), torch.empty_like(m.features)
+    errors = torch.zeros(1, dtype=torch.int32, device="cuda")
+    back = space(B.qail_w16a16_backward_workspace(m.p, 8))
+
+    def everything():
+        for t in (m.h, m.y, m.logits, m.token, m.logprob, z, dp, dbias, dx, m.dtable):
+            t.fill_(3)
+        m.set(9)
+        m.ids[-2:] = torch.tensor([301, -7], dtype=torch.int32)
+        errors.zero_()
+        B.qail_w16a16_linear(m.p, m.features, m.h[:8], m.ws, residual=m.table[:8], z=z)
+        B.qail_embed(m.table, m.ids, m.h, scale=2, errors=errors)
+        B.qail_rmsnorm(m.h, m.norm, EPS, y=m.y)
+        B.qail_w16a16_linear(m.d, m.y, m.logits, m.ws)
+        B.qail_sample(m.logits, m.u, m.token, logprob=m.logprob, errors=errors, **choice)
+        B.qail_w16a16_backward(m.p, m.features, m.h[:8], back, z=z, dx=dx, dweight=dp, dbias=dbias)
+        B.qail_embed_backward(m.ids, m.h, m.dtable, m.train_ws, scale=0.5, accumulate=True, errors=errors)
+        return [t.clone() for t in (m.h, m.logits, m.token, m.logprob, z, dp, dbias, dx, m.dtable, errors)]
+
+    native = everything()
+    assert native[-1].item() >= 2 and (m.token >= 0).all()
+    for name in ("_embed_native", "_embed_backward_native", "_w16a16_native", "_w16a16_backward_native", "_sample_native"):
+        assert getattr(B, name) is not B._not_plain
+        monkeypatch.setattr(B, name, B._not_plain)
+    assert all(torch.equal(a, b) for a, b in zip(native, everything()))
+    for undo in (False, True):
+        if undo:
+            monkeypatch.undo()
+        with pytest.raises(ValueError):
+            B.qail_embed(m.table, m.ids, m.h.t().contiguous().t())
+        with pytest.raises(ValueError):
+            B.qail_embed_backward(m.ids, m.h[:-1], m.dtable, m.train_ws)
+        with pytest.raises(ValueError):
+            B.qail_w16a16_linear(m.d, m.y, m.logits.cpu(), m.ws)
+        with pytest.raises(ValueError):
+            B.qail_w16a16_backward(m.p, m.features.float(), m.h[:8], back, z=z, dweight=dp)
+        with pytest.raises(ValueError):
+            B.qail_sample(m.logits.t(), m.u, m.token)
