@@ -1,11 +1,11 @@
 // Rows of a table of embeddings, and the gradient of that lookup.
 //
-// The gradient adds up the rows of dh that belong to a token.  Atomics would add them in any order, so the tokens are sorted first (stable: a
-// token's rows stay in the order of their places), and whoever writes row v of the gradient reads its rows one after the other.  A token that comes
-// more than kPart times is added up in parts of kPart sorted places by other blocks before, whose sums are then added in their order.
-// What is sorted are pairs (token, place).  Up to kTile of them are ranked by comparing each with all others, a wave a pair, over the whole chip (2312 tokens 4.8 us, 4096 6.2; by digits
-// in one block 9.8 and 10.8).  More of them are sorted in tiles of kTile, 8 bits of the token at a time, whose pairs stay in LDS for all digits: equal digits are found by
-// comparing lanes.  Up to kMergeTiles tiles are then merged by rank: a pair's place is its own tile's plus how many pairs of each other tile come before it, 12 probes a
+// The gradient adds up the rows of dh that belong to a token.  Atomics would add them in any order, so the tokens are sorted first (stable: a token's rows stay
+// in the order of their places), and whoever writes row v of the gradient reads its rows one after the other.  A token that comes more than kPart times is
+// added up in parts of kPart sorted places by other blocks before, whose sums are then added in their order. What is sorted are pairs (token, place).  Up to
+// kTile of them are ranked by comparing each with all others, a wave a pair, over the whole chip (2312 tokens 4.8 us, 4096 6.2; by digits in one block 9.8 and
+// 10.8).  More of them are sorted in tiles of kTile, 8 bits of the token at a time, whose pairs stay in LDS for all digits: equal digits are found by comparing
+// lanes.  Up to kMergeTiles tiles are then merged by rank: a pair's place is its own tile's plus how many pairs of each other tile come before it, 12 probes a
 // tile (24577 tokens: 11.7 and 6.1 us).  More of them are sorted digit by digit over all tiles: their counts, the counts' sums, and the move.
 #include <algorithm>
 
@@ -338,8 +338,8 @@ __global__ __launch_bounds__(256) void embed_parts_kernel(const SumArgs g) {
     if (long_tail) put(1, begin, b);
 }
 
-// A block writes `rows` rows, whose tokens it finds by itself.  Bound by HBM: 32000 x 4096 with 2312 tokens in 100 us (5.4 TB/s), with 24577 in 128.  kStream: the gradient is written past
-// the caches.
+// A block writes `rows` rows, whose tokens it finds by itself.  Bound by HBM: 32000 x 4096 with 2312 tokens in 100 us (5.4 TB/s), with 24577 in 128.  kStream:
+// the gradient is written past the caches.
 template <bool kStream>
 __global__ __launch_bounds__(256, 8) void embed_rows_kernel(const SumArgs g) {
     __shared__ int start[kMostRows + 1], ends[2];
@@ -458,7 +458,8 @@ hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, floa
         }
     }
     if (at.parts) hipLaunchKernelGGL(embed_parts_kernel, dim3((unsigned)at.parts * ((K + 1023) / 1024)), dim3(256), 0, st, g);
-    hipLaunchKernelGGL((size_t)V * K * sizeof(float) >= kStreamFrom ? embed_rows_kernel<true> : embed_rows_kernel<false>, dim3((unsigned)((V + g.rows - 1) / g.rows) * across), dim3(256), 0, st, g);
+    const auto rows_kernel = (size_t)V * K * sizeof(float) >= kStreamFrom ? embed_rows_kernel<true> : embed_rows_kernel<false>;
+    hipLaunchKernelGGL(rows_kernel, dim3((unsigned)((V + g.rows - 1) / g.rows) * across), dim3(256), 0, st, g);
     return hipGetLastError();
 }
 

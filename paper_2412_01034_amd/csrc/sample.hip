@@ -10,9 +10,9 @@
 // exact arithmetic but for those 2^-44.  In 32 bits the sums would be off by 2^-24 or so of themselves, and of 32000 tokens without a filter one row in some thousands
 // would get a neighbouring one.  An exponential is a table of 512 and a polynomial; 64 bits cost no more cycles than 32 here.
 //
-// One block a row, whose values stay in registers up to 32768 tokens; a longer row is read again in every pass, and lies in L2 by then.  Several blocks a row would have to
-// meet in memory, which this call has none of.  Bound by instructions and by the meetings of the 16 waves, not by memory: one row of 32000 takes 18 us (15.6 of 40 thousand cycles are the
-// exponentials of top-p, thirty instructions each), 256 rows 33, 48 rows of 131072 94.
+// One block a row, whose values stay in registers up to 32768 tokens; a longer row is read again in every pass, and lies in L2 by then.  Several blocks a row
+// would have to meet in memory, which this call has none of.  Bound by instructions and by the meetings of the 16 waves, not by memory: one row of 32000 takes
+// 18 us (15.6 of 40 thousand cycles are the exponentials of top-p, thirty instructions each), 256 rows 33, 48 rows of 131072 94.
 #include <type_traits>
 
 #include "qail_internal.h"
@@ -174,7 +174,8 @@ struct Row {
         if constexpr (kChunks > 2) values(2, kept[2]);
         if constexpr (kChunks > 3) values(3, kept[3]);
     }
-    // f(chunk, values) for the kGroup chunks from `first` on, those behind the row among them (minus infinity): unrolled, the loads in front.  For passes that do little with a value.
+    // f(chunk, values) for the kGroup chunks from `first` on, those behind the row among them (minus infinity): unrolled, the loads in front.  For passes that
+    // do little with a value.
     template <typename F>
     __device__ __forceinline__ void group(int first, F f) const {
         if constexpr (kChunks > 0) {

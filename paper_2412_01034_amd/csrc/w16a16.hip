@@ -272,10 +272,10 @@ struct Operand {
     }
 };
 
-// kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied.
-// The matrix cores get B's rows as rows: a lane then has one p and groups of four neighbouring q.  Bound by power and LDS where the chip is full (a 4096 x 4096 x 4096 gradient 115 to 125 us,
-// 1100 to 1200 TFLOP/s of 1450 that a library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s), by the epilogue
-// with short contractions (2056 x 4096 x 1024 with GELU, z and bias 40 us, 28 without them).
+// kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied. The matrix cores get B's rows
+// as rows: a lane then has one p and groups of four neighbouring q.  Bound by power and LDS where the chip is full (a 4096 x 4096 x 4096 gradient 115 to 125
+// us, 1100 to 1200 TFLOP/s of 1450 that a library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s),
+// by the epilogue with short contractions (2056 x 4096 x 1024 with GELU, z and bias 40 us, 28 without them).
 template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
 __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a16_product_kernel(const ProductArgs g) {
     constexpr int kThreads = kWP * kWQ * kWave, FP = kBP / kWP / 32, FQ = kBQ / kWQ / 32;
@@ -575,8 +575,8 @@ hipError_t launch_w16a16_back(const qail_w16a16& d, const uint16_t* x, const uin
     const bool as_it_is = d.activation == QAIL_ACT_NONE && dy && d.N % 8 == 0;   // dz is dy
     const bool products = dx || dweight;
     if ((products && !as_it_is) || dbias) {
-        hipLaunchKernelGGL(w16a16_dz_kernel, dim3((unsigned)at.across * (unsigned)at.row_blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, at.rows, products && !as_it_is ? dz : nullptr,
-                           dbias ? sums : nullptr);
+        hipLaunchKernelGGL(w16a16_dz_kernel, dim3((unsigned)at.across * (unsigned)at.row_blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, at.rows,
+                           products && !as_it_is ? dz : nullptr, dbias ? sums : nullptr);
         if (dbias) hipLaunchKernelGGL(w16a16_bias_kernel, dim3((unsigned)((d.N + 31) / 32)), dim3(256), 0, st, sums, at.row_blocks, d.N, dbias);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
