@@ -565,6 +565,7 @@ typedef struct {
     int32_t activation;       /* qail_activation */
     const uint16_t* weight;
     const uint16_t* bias;
+    int32_t round_dz;         /* of the gradients, below: 0 or not */
 } qail_w16a16;
 
 /*     z[m][n] = sum_k x[m][k] W[n][k] + bias[n]           fp32
@@ -579,7 +580,9 @@ int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const
                        void* workspace, size_t workspace_bytes, void* stream);
 
 /* Its gradients, at the rounded z:
- *     dz = dy * act'(z)                     fp32; rounded to bf16 for the products
+ *     dz = dy * act'(z)                     fp32; enters the products in two bf16 parts (2^-16 of itself), or with round_dz != 0 rounded to
+ *                                           bf16, which takes little more than half their time and costs the gradients as much as their own rounding;
+ *                                           a bf16 dy without an activation or with RELU is exact either way
  *     dx[m][k] = sum_n dz[m][n] W[n][k]     fp32 sums, rounded once; bf16 [M][K] or NULL
  *     dweight[n][k] = sum_m dz[m][n] x[m][k]   likewise; bf16 [N][K] or NULL
  *     dbias[n] = sum_m dz[m][n]             of the unrounded dz, a fixed order of summation; fp32 [N] or NULL

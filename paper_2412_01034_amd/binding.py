@@ -100,7 +100,8 @@ class qail_adapters(ctypes.Structure):
 
 
 class qail_w16a16(ctypes.Structure):
-    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("activation", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+    _fields_ = [("N", ctypes.c_int32), ("K", ctypes.c_int32), ("activation", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("round_dz", ctypes.c_int32)]
 
 
 class qail_sampling(ctypes.Structure):
@@ -898,13 +899,13 @@ def qail_embed_backward(ids: torch.Tensor, dh: torch.Tensor, dtable: torch.Tenso
                                      _errors(errors), _ptr(workspace), workspace.nbytes, _stream()), "qail_embed_backward")
 
 
-def make_w16a16(weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none") -> qail_w16a16:
-    """weight: bf16 [N, K]; bias: bf16 [N]; activation: a key of ACTIVATIONS.  The result can be passed to any number of calls (the tensors must be
-    kept alive by the caller)."""
+def make_w16a16(weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none", round_dz: bool = False) -> qail_w16a16:
+    """weight: bf16 [N, K]; bias: bf16 [N]; activation: a key of ACTIVATIONS; round_dz: the gradients' products have dz rounded to bf16, in little more than half the time.
+    The result can be passed to any number of calls (the tensors must be kept alive by the caller)."""
     N, K = weight.shape
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation: one of {', '.join(ACTIVATIONS)} expected, {activation!r} given")
-    return qail_w16a16(N, K, ACTIVATIONS[activation], _bf16(weight, N * K, "weight"), _bf16(bias, N, "bias"))
+    return qail_w16a16(N, K, ACTIVATIONS[activation], _bf16(weight, N * K, "weight"), _bf16(bias, N, "bias"), int(bool(round_dz)))
 
 
 def qail_w16a16_workspace(linear: qail_w16a16, M: int) -> int:

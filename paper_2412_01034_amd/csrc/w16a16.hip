@@ -4,6 +4,10 @@
 // All three products are C[p][q] = sum_r A(p, r) B(q, r), whose operands either have r contiguous ("straight": x and W of the
 // forward product, dz of dx) or lie row by row of r ("turned": W of dx, dz and x of dW).  One kernel computes them: 64 r at a time go from
 // memory straight into LDS, and a turned operand is read from there transposed by the hardware, so that nothing is transposed in memory.
+//
+// dz is computed in fp32 and the matrix cores take bf16: it enters its products as the sum of two bf16 numbers, which takes about twice as long as rounding it once (289 x 4096 x
+// 4096 77 us for 54, 4096 x 4096 x 4096 500 for 270) and leaves the gradients their own rounding alone (0.0017 of their norm from 64 bits; 0.0023 with dz rounded).  The
+// caller may ask for the rounded one; where dz has 8 bits anyway (a bf16 dy, no activation or RELU) there is one part.
 #include <algorithm>
 
 #include "qail_internal.h"
@@ -184,6 +188,7 @@ struct ProductArgs {
     const uint16_t* a;      // straight: [P][lda], turned: [R][lda] (lda >= P rounded up to 8)
     const uint16_t* b;      // likewise with Q
     long long lda, ldb;
+    long long low;          // where a's second parts begin, elements from a; 0: it has none.  Their steps come first, and the plan has them
     int P, Q, R;            // R: of a straight operand a multiple of 8 that its rows have
     ProductPlan plan;
     float* partial;         // [splits][P][Q rounded up to 8], where splits > 1
@@ -235,10 +240,10 @@ struct Operand {
             }
         }
     }
-    // Step `step` into LDS at `lds` (of the block); what lies beyond R is zero.
-    __device__ __forceinline__ void load(int step, uint32_t lds) const {
+    // Step `step` of the matrix that begins `part` elements farther on into LDS at `lds` (of the block); what lies beyond R is zero.
+    __device__ __forceinline__ void load(int step, uint32_t lds, long long part) const {
         const int r0 = step * kStepR;
-        const uint16_t* const from = base + (kTurned ? (long long)r0 * ld : (long long)r0);
+        const uint16_t* const from = base + part + (kTurned ? (long long)r0 * ld : (long long)r0);
         const uint32_t to = lds + (threadIdx.x / kWave) * (16 * kWave);
         if (r0 + kStepR <= R) {
 #pragma unroll
@@ -274,7 +279,7 @@ struct Operand {
 
 // kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied. The matrix cores get B's rows
 // as rows: a lane then has one p and groups of four neighbouring q.  Bound by power and LDS where the chip is full (a 4096 x 4096 x 4096 gradient 115 to 125
-// us, 1100 to 1200 TFLOP/s of 1450 that a library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s),
+// us with dz in one part, 242 to 264 in two: 1040 to 1200 TFLOP/s of 1450 that a library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s),
 // by the epilogue with short contractions (2056 x 4096 x 1024 with GELU, z and bias 40 us, 28 without them).
 template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
 __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a16_product_kernel(const ProductArgs g) {
@@ -293,10 +298,12 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
 
     f32x16_t acc[FP][FQ] = {};
     bf16x8_t fa[2][FP] = {}, fb[2][FQ] = {};
+    // The gradients' products (B turned) have dz in two parts, whose sum it is: first the steps of the second parts, then the same ones of the first parts.
+    const int low_steps = kTB && g.low != 0 ? g.plan.steps / 2 : 0, low = kTB ? max(0, min(low_steps - first, steps)) : 0;   // in all, and of this block's
     auto load = [&](int i) {
-        const int slot = i % kSlots;
-        a.load(first + i, lds + slot * kSlot);
-        b.load(first + i, lds + slot * kSlot + A::kBytes);
+        const int slot = i % kSlots, step = first + i - (i < low ? 0 : low_steps);
+        a.load(step, lds + slot * kSlot, i < low ? g.low : 0);
+        b.load(step, lds + slot * kSlot + A::kBytes, 0);
     };
     // All of the steps up to i have arrived (at most kSlots - 1 later ones are on their way), and nobody reads the step in front of them.
     auto wait_for = [&](int i, int issued) {
@@ -314,6 +321,16 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
 #pragma unroll
             for (int y = 0; y < FQ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][y], fa[set][x], acc[x][y], 0, 0, 0);
     };
+    // The second parts add 2^-8 of the sums at most.  Where an infinity or NaN of B met them the sum is the first parts' alone: of opposite infinities, or of an infinity and
+    // the 0 that an exact dz has for its second part, it would be NaN where the product's is infinite.
+    auto drop = [&]() {
+#pragma unroll
+        for (int x = 0; x < FP; ++x)
+#pragma unroll
+            for (int y = 0; y < FQ; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[x][y][e] = fabsf(acc[x][y][e]) <= 3.4028235e38f ? acc[x][y][e] : 0.f;
+    };
 #pragma unroll
     for (int i = 0; i < kSlots; ++i)
         if (i < steps) load(i);
@@ -321,6 +338,14 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
     // The fragments of 16 r are read while those before them are multiplied, the first ones of a step beside the last products of the step before
     // (zeros at the beginning), so that the matrix cores do not wait for the barrier's reads.
     for (int i = 0; i < steps; ++i) {
+        if (kTB && i == low && low > 0) {
+            multiply(1);
+            drop();
+#pragma unroll
+            for (int j = 0; j < FP; ++j) fa[1][j] = bf16x8_t{};
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fb[1][j] = bf16x8_t{};
+        }
         const uint8_t* const sa = ring + i % kSlots * kSlot;
         const uint8_t* const sb = sa + A::kBytes;
 #pragma unroll
@@ -346,6 +371,7 @@ __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a
         }
     }
     multiply(1);
+    if (kTB && low == steps) drop();
 
     // Out through LDS, 32 rows of a wave at a time: the lanes then have 8 neighbouring outputs of a row, a row's lanes lie beside each other, and the
     // epilogue is a loop (unrolled over the registers its code is far longer than the instruction cache).  Piece c (16 bytes) of row p lies at c ^ (p & 15).
@@ -411,6 +437,7 @@ __global__ __launch_bounds__(256) void w16a16_sum_kernel(const float* __restrict
 
 constexpr int kDzCols = 256;   // columns of a block: 32 threads of 8; 8 threads share a column's rows
 constexpr int kDzSlices = 8;
+constexpr float kMostHalf = 3.38953139e38f;   // the largest number of bf16
 
 // The rows of a block: 8 a thread where that leaves eight blocks a compute unit, fewer for short batches.
 inline int dz_rows(int M, int across, int units) {
@@ -418,10 +445,10 @@ inline int dz_rows(int M, int across, int units) {
     return kDzSlices * (int)std::max(1ll, std::min(8ll, rows / kDzSlices));
 }
 
-// dz = bf16(dy act'(z)), rows of ld values (N rounded up to 8, zeros behind N), and the sums of the unrounded dz over a block's rows.  Bound by
-// HBM and, with either GELU, as much by its slope: 4096 x 4096 in 28 us (3.6 TB/s).
+// dz = bf16(dy act'(z)), or that and bf16 of what it leaves over (low), rows of ld values (N rounded up to 8, zeros behind N), and the sums of the unrounded dz over a
+// block's rows.  Bound by HBM and, with either GELU, as much by its slope: 4096 x 4096 in two parts in 32 us (4.1 TB/s), in one in 26.
 __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restrict__ z, const uint16_t* __restrict__ dy, const float* __restrict__ dy32, int act,
-                                                        int M, int N, int ld, int rows, uint16_t* __restrict__ dz, float* __restrict__ sums) {
+                                                        int M, int N, int ld, int rows, uint16_t* __restrict__ dz, uint16_t* __restrict__ low, float* __restrict__ sums) {
     __shared__ float part[kDzSlices][kDzCols + 8];
     const int across = (ld + kDzCols - 1) / kDzCols, bx = blockIdx.x % across, by = blockIdx.x / across;
     const int c = threadIdx.x % 32, n = bx * kDzCols + 8 * c, slice = threadIdx.x / 32;
@@ -433,7 +460,21 @@ __global__ __launch_bounds__(256) void w16a16_dz_kernel(const uint16_t* __restri
             if (act != QAIL_ACT_NONE) v[i] *= slope(act, s[i]);
             sum[i] += v[i];
         }
-        if (dz) *reinterpret_cast<uint4*>(dz + (size_t)m * ld + n) = pack8(v);
+        if (!dz) return;
+        const size_t at = (size_t)m * ld + n;
+        if (!low) {
+            *reinterpret_cast<uint4*>(dz + at) = pack8(v);
+            return;
+        }
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = fabsf(v[i]) <= 3.4028235e38f ? __builtin_amdgcn_fmed3f(v[i], -kMostHalf, kMostHalf) : v[i];
+        const uint4 high = pack8(t);
+        *reinterpret_cast<uint4*>(dz + at) = high;
+        unpack8(high, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = fabsf(v[i]) <= 3.4028235e38f ? v[i] - t[i] : 0.f;   // an infinity has no second part
+        *reinterpret_cast<uint4*>(low + at) = pack8(t);
     };
     if (n + 8 <= N) {
 #pragma unroll 2
@@ -511,7 +552,7 @@ hipError_t launch_tiles(const ProductArgs& g, hipStream_t st) {
 
 template <bool kTA, bool kTB>
 hipError_t launch_product(ProductArgs g, float* partial, hipStream_t st) {
-    g.plan = plan_product(g.P, g.Q, g.R, kTA, device_cu_count());
+    g.plan = plan_product(g.P, g.Q, g.R, kTA, device_cu_count(), g.low != 0 ? 2 : 1);
     g.partial = partial;
     g.e.Q = g.Q;
     hipError_t e = hipErrorInvalidValue;
@@ -530,8 +571,8 @@ hipError_t launch_product(ProductArgs g, float* partial, hipStream_t st) {
     return hipGetLastError();
 }
 
-size_t partial_bytes(long long P, long long Q, long long R, bool turned) {
-    const ProductPlan pl = plan_product(P, Q, R, turned, device_cu_count());
+size_t partial_bytes(long long P, long long Q, long long R, bool turned, int parts = 1) {
+    const ProductPlan pl = plan_product(P, Q, R, turned, device_cu_count(), parts);
     return pl.splits == 1 ? 0 : (size_t)pl.splits * P * ((Q + 7) / 8 * 8) * sizeof(float);
 }
 
@@ -548,18 +589,22 @@ hipError_t launch_w16a16(const qail_w16a16& d, const uint16_t* x, int M, const u
     return launch_product<false, false>(g, static_cast<float*>(ws), st);
 }
 
-// The workspace of the backward call: dz, the sums of dz over the blocks' rows, then the shares of the two products in turn.
+// The workspace of the backward call: dz and its second parts, the sums of dz over the blocks' rows, then the shares of the two products in turn.
 struct BackPlaces {
     int ld, across, rows, row_blocks;
-    size_t sums, partial, bytes;
+    size_t low, sums, partial, bytes;
     BackPlaces(const qail_w16a16& d, int M) {
         ld = (d.N + 7) / 8 * 8;
         across = (ld + kDzCols - 1) / kDzCols;
         rows = dz_rows(M, across, device_cu_count());
         row_blocks = (M + rows - 1) / rows;
-        sums = round256((size_t)M * ld * 2);
+        low = round256((size_t)M * ld * 2);
+        sums = d.round_dz ? low : 2 * low;
         partial = sums + round256((size_t)row_blocks * d.N * sizeof(float));
-        bytes = partial + round256(std::max(partial_bytes(M, d.K, d.N, false), partial_bytes(d.N, d.K, M, true)));
+        size_t shares = 0;   // in either number of parts, which the type of dy decides
+        for (int parts = 1; parts <= (d.round_dz ? 1 : 2); ++parts)
+            shares = std::max({shares, partial_bytes(M, d.K, d.N, false, parts), partial_bytes(d.N, d.K, M, true, parts)});
+        bytes = partial + round256(shares);
     }
 };
 
@@ -574,15 +619,18 @@ hipError_t launch_w16a16_back(const qail_w16a16& d, const uint16_t* x, const uin
     float* const partial = reinterpret_cast<float*>(w + at.partial);
     const bool as_it_is = d.activation == QAIL_ACT_NONE && dy && d.N % 8 == 0;   // dz is dy
     const bool products = dx || dweight;
+    // dz has no more than 8 bits where dy has no more and the slopes are 0 and 1
+    const bool two_parts = !d.round_dz && (dy_f32 || (d.activation != QAIL_ACT_NONE && d.activation != QAIL_ACT_RELU));
     if ((products && !as_it_is) || dbias) {
         hipLaunchKernelGGL(w16a16_dz_kernel, dim3((unsigned)at.across * (unsigned)at.row_blocks), dim3(256), 0, st, z, dy, dy_f32, d.activation, M, d.N, at.ld, at.rows,
-                           products && !as_it_is ? dz : nullptr, dbias ? sums : nullptr);
+                           products && !as_it_is ? dz : nullptr, products && two_parts ? dz + at.low / 2 : nullptr, dbias ? sums : nullptr);
         if (dbias) hipLaunchKernelGGL(w16a16_bias_kernel, dim3((unsigned)((d.N + 31) / 32)), dim3(256), 0, st, sums, at.row_blocks, d.N, dbias);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     const uint16_t* const from = as_it_is ? dy : dz;
     ProductArgs g = {};
+    g.low = two_parts ? (long long)(at.low / 2) : 0;
     if (dx) {
         g.a = from, g.lda = at.ld, g.b = d.weight, g.ldb = d.K;
         g.P = M, g.Q = d.K, g.R = d.N;

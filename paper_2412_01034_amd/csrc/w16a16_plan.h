@@ -40,7 +40,7 @@ __host__ __device__ inline TilePlace tile_place(const ProductPlan& pl, int b) {
     return t;
 }
 
-// turned: the operand of P lies row by row of r.
+// turned: the operand of P lies row by row of r; parts: it is the sum of so many matrices, which the steps go through in turn.
 //
 // Up to 32 rows: tiles of 32 x 64, whose cost is the stream of the other operand; blocks for three a unit by shares of the contraction, which are
 // not worth the second launch before a tile has sixteen steps for each.
@@ -48,9 +48,9 @@ __host__ __device__ inline TilePlace tile_place(const ProductPlan& pl, int b) {
 //     128 x 128   1.0 / 0.62, 7        192 x 128 (straight)   1.4 / 0.78, 9        256 x 256   1.65, 10 (one a unit)
 // and for shares 3 for the second launch and their sums' way at 4 TB/s.  4096 x 4096 x 4096 takes 118 us with 256 x 256 tiles and 148 with 128 x 128, 2056 x 4096 x 1024 28
 // with 192 x 128 and 33 with either other, 289 x 4096 x 4096 25 with five shares of 128 x 128 tiles and 42 with one.
-inline ProductPlan plan_product(long long P, long long Q, long long R, bool turned, int units) {
+inline ProductPlan plan_product(long long P, long long Q, long long R, bool turned, int units, int parts = 1) {
     ProductPlan pl;
-    pl.steps = (int)((R + kStepR - 1) / kStepR);
+    pl.steps = parts * (int)((R + kStepR - 1) / kStepR);
     const auto tiles_of = [&](int bp, int bq) {
         pl.bp = bp, pl.bq = bq;
         pl.tiles_p = (int)((P + bp - 1) / bp);
