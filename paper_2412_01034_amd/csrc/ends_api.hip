@@ -94,7 +94,7 @@ int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const
     if (e != QAIL_OK) return e;
     if (!d->weight || !x || !y == !y_f32) return QAIL_ERR_NULL;
     if (!aligned(d->weight) || !aligned(d->bias) || !aligned(x) || !aligned(residual) || !aligned(z_out) || !aligned(y) || !aligned(y_f32)) return QAIL_ERR_ALIGN;
-    if (!apart({x, residual, d->weight, d->bias}, {z_out, y == residual ? nullptr : y, y_f32}) || (z_out && z_out == y)) return QAIL_ERR_SHAPE;
+    if (!apart({x, d->weight, d->bias}, {z_out, y, y_f32}) || !apart({residual}, {z_out, y_f32})) return QAIL_ERR_SHAPE;   // y may be the residual
     const size_t need = w16a16_workspace(*d, M);
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return QAIL_ERR_WORKSPACE;

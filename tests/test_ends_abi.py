@@ -82,6 +82,19 @@ def test_linear_refusals(B):
     expect(B.QAIL_ERR_ALIGN, call, dict(d=big, ws=OK + 16))
 
 
+def test_an_output_in_place_of_the_residual_is_no_other_input(B):
+    """x + f(x) in place would have blocks read rows of x that others have overwritten.  (Sizes that need a workspace, which is missing: no call gets as far as a launch.)"""
+    def call(d={}, **change):
+        a = dict(x=OK, M=4, residual=0x30000, z=None, y=0x30000, y32=None, ws=None, bytes=0)
+        a.update(change)
+        d = dict(dict(N=4096, K=4096, weight=0x50000, bias=0x60000), **d)
+        return B.lib().qail_w16a16_linear(ctypes.byref(linear(B, **d)), *a.values(), None)
+
+    expect(B.QAIL_ERR_WORKSPACE, call, dict())
+    expect(B.QAIL_ERR_SHAPE, call, dict(x=0x30000), dict(d=dict(weight=0x30000)), dict(d=dict(bias=0x30000)), dict(z=0x30000), dict(z=OK), dict(z=0x50000), dict(z=0x60000),
+           dict(y=None, y32=0x30000), dict(y=None, y32=0x60000), dict(y=None, y32=0x70000, z=0x30000))
+
+
 def test_linear_backward_refusals(B):
     n = B.qail_w16a16_backward_workspace(linear(B), 4)
 
