@@ -77,8 +77,8 @@ __device__ __forceinline__ float activated(int act, float z) {
         case QAIL_ACT_RELU: return z < 0.f ? 0.f : z;
         case QAIL_ACT_GELU: {
             float bell;
-            const float h = normal_tail<kShort>(fminf(fabsf(z), 20.f), bell);
-            return z > 0.f ? fmaf(-z, h, z) : z * h;
+            const float x = fminf(fabsf(z), 20.f), h = normal_tail<kShort>(x, bell);
+            return z > 0.f ? fmaf(-x, h, z) : z * h;   // (h is 0 from 14 on: not -z, or infinity would meet it)
         }
         case QAIL_ACT_GELU_TANH: return z * __builtin_amdgcn_rcpf(1.f + exp_of(-gelu_tanh_argument(z)));
         case QAIL_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
