@@ -914,6 +914,16 @@ def qail_w16a16_workspace(linear: qail_w16a16, M: int) -> int:
     return b.value
 
 
+def _rows(t: torch.Tensor, n: int, what: str) -> int:
+    """How many rows of n values a tensor has: its last dimension is a row, the others count them (single values may come without that dimension)."""
+    if t.shape[-1:] != (n,) and (n != 1 or t.dim() != 1):
+        raise ValueError(f"{what}: rows of {n} values expected, a tensor of {tuple(t.shape)} given")
+    rows = t.numel() // max(n, 1)
+    if rows > 0x7FFFFFFF:
+        raise ValueError(f"{what}: {rows} rows given")
+    return rows
+
+
 def _bf16_or_fp32(t: torch.Tensor, count: int, what: str) -> Tuple[Optional[int], Optional[int]]:
     """(address as bf16, address as fp32), one of them None."""
     _typed(t, what, torch.bfloat16, torch.int16, torch.float32)
@@ -922,13 +932,15 @@ def _bf16_or_fp32(t: torch.Tensor, count: int, what: str) -> Tuple[Optional[int]
 
 def qail_w16a16_linear(linear: qail_w16a16, x: torch.Tensor, y: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                        residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None) -> None:
-    """x: bf16 [M, K]; y: bf16 or fp32 [M, N]; residual, z (what the activation is applied to, for the backward call): bf16 [M, N]."""
+    """x: bf16 [M, K], M in any number of dimensions; y: bf16 or fp32 [M, N]; residual, z (what the activation is applied to, for the backward call): bf16
+    [M, N]."""
     status = _w16a16_native(linear, x, y, workspace, residual, z) if type(linear) is qail_w16a16 else None
     if status is not None:
         if status:
             raise QailError(status, "qail_w16a16_linear")
         return
-    M, N, K = x.shape[0], linear.N, linear.K
+    N, K = linear.N, linear.K
+    M = _rows(x, K, "x")
     half, whole = _bf16_or_fp32(y, M * N, "y")
     ws, wsb = (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
     _check(lib().qail_w16a16_linear(ctypes.byref(linear), _bf16(x, M * K, "x"), M, _bf16(residual, M * N, "residual"), _bf16(z, M * N, "z"), half, whole,
@@ -943,13 +955,14 @@ def qail_w16a16_backward_workspace(linear: qail_w16a16, M: int) -> int:
 
 def qail_w16a16_backward(linear: qail_w16a16, x: Optional[torch.Tensor], dy: torch.Tensor, workspace: torch.Tensor, z: Optional[torch.Tensor] = None,
                          dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None) -> None:
-    """x, dx: bf16 [M, K]; dy: bf16 or fp32 [M, N]; z: bf16 [M, N]; dweight: bf16 [N, K]; dbias: fp32 [N]."""
+    """dy: bf16 or fp32 [M, N], M in any number of dimensions; x, dx: bf16 [M, K]; z: bf16 [M, N]; dweight: bf16 [N, K]; dbias: fp32 [N]."""
     status = _w16a16_backward_native(linear, x, dy, workspace, z, dx, dweight, dbias) if type(linear) is qail_w16a16 else None
     if status is not None:
         if status:
             raise QailError(status, "qail_w16a16_backward")
         return
-    M, N, K = dy.shape[0], linear.N, linear.K
+    N, K = linear.N, linear.K
+    M = _rows(dy, N, "dy")
     half, whole = _bf16_or_fp32(dy, M * N, "dy")
     _check(lib().qail_w16a16_backward(ctypes.byref(linear), _bf16(x, M * K, "x"), _bf16(z, M * N, "z"), half, whole, M, _bf16(dx, M * K, "dx"),
                                       _bf16(dweight, N * K, "dweight"), _fp32(dbias, N, "dbias"), _ptr(workspace), workspace.nbytes, _stream()),

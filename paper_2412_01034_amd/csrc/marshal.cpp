@@ -298,6 +298,14 @@ bool count_of(PyObject* o, int32_t& n) {
     n = (int32_t)THPVariable_Unpack(o).numel();
     return true;
 }
+// How many rows of n values a plain tensor has: its last dimension is a row, the others count them (single values may come without that dimension).
+bool rows_by(PyObject* o, int64_t n, int64_t& M) {
+    if (!THPVariable_CheckExact(o) || n < 1) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.dim() < 1 || (t.size(-1) != n && (n != 1 || t.dim() != 1))) return false;
+    M = t.numel() / n;
+    return M <= INT_MAX;
+}
 // bf16 or fp32, the other address NULL.
 template <typename A, typename B>
 bool either(PyObject* o, int64_t count, A*& half, B*& whole) {
@@ -352,8 +360,8 @@ PyObject* w16a16_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 6 || !g_w16a16) return nullptr;
         const Items di(a[0]);
         const auto* d = held<qail_w16a16>(di);
-        if (!d || !THPVariable_CheckExact(a[1]) || THPVariable_Unpack(a[1]).dim() < 1 || THPVariable_Unpack(a[1]).size(0) > INT_MAX) return nullptr;
-        const int64_t M = THPVariable_Unpack(a[1]).size(0);
+        int64_t M;
+        if (!d || !rows_by(a[1], d->K, M)) return nullptr;
         const uint16_t *x, *residual;
         uint16_t *y, *z;
         float* y32;
@@ -373,8 +381,9 @@ PyObject* w16a16_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 8 || !g_w16a16_backward) return nullptr;
         const Items di(a[0]);
         const auto* d = held<qail_w16a16>(di);
-        if (!d || !THPVariable_CheckExact(a[2]) || THPVariable_Unpack(a[2]).dim() < 1 || THPVariable_Unpack(a[2]).size(0) > INT_MAX) return nullptr;
-        const int64_t M = THPVariable_Unpack(a[2]).size(0), N = d->N, K = d->K;
+        int64_t M;
+        if (!d || !rows_by(a[2], d->N, M)) return nullptr;
+        const int64_t N = d->N, K = d->K;
         const uint16_t *x, *z, *dy;
         const float* dy32;
         uint16_t *dx, *dw;

@@ -146,6 +146,23 @@ def test_the_binding_refuses_what_is_not_what_it_says(B):
         B.qail_sample(whole, torch.zeros(4), number)
 
 
+def test_the_binding_counts_rows_by_the_last_dimension(B):
+    new = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)  # noqa: E731
+    d, one = B.qail_w16a16(40, 64, 0, OK, None), B.qail_w16a16(1, 64, 0, OK, None)
+    for x in (new(4, 128), new(64, 4), new(4), new(4, 64, 1), new(256)):
+        with pytest.raises(ValueError, match="x: rows of 64 values expected"):
+            B.qail_w16a16_linear(d, x, new(256, 40))
+    for dy in (new(4, 80), new(40, 4), new(5)):
+        with pytest.raises(ValueError, match="dy: rows of 40 values expected"):
+            B.qail_w16a16_backward(d, None, dy, None, dx=new(256, 64))
+    with pytest.raises(ValueError, match="dy: rows of 1 values expected"):
+        B.qail_w16a16_backward(one, None, new(3, 5), None, dx=new(256, 64))
+    for t, n, rows in ((new(3, 5, 64), 64, 15), (new(64), 64, 1), (new(7), 1, 7), (new(7, 1), 1, 7), (new(1), 1, 1), (new(0, 64), 64, 0), (new(2, 0, 64), 64, 0)):
+        assert B._rows(t, n, "x") == rows
+    with pytest.raises(ValueError, match="y: 1120 bytes given, 1200 needed"):     # 15 rows, not 3
+        B.qail_w16a16_linear(d, new(3, 5, 64), new(14, 40))
+
+
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not found")
 def test_division_of_products_on_the_host(tmp_path):
     exe = str(tmp_path / "host_products_driver")

@@ -357,3 +357,34 @@ def test_plain_calls_give_the_same_by_either_way(B, monkeypatch):
             B.qail_w16a16_backward(m.p, m.features.float(), m.h[:8], back, z=z, dweight=dp)
         with pytest.raises(ValueError):
             B.qail_sample(m.logits.t(), m.u, m.token)
+
+
+@pytest.mark.parametrize("plain", [True, False])
+def test_linears_take_rows_in_any_number_of_dimensions(B, monkeypatch, plain):
+    """Frames x patches x width is that many rows, by either way of marshalling."""
+    if not plain:
+        for name in ("_w16a16_native", "_w16a16_backward_native"):
+            monkeypatch.setattr(B, name, B._not_plain)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    F, P, K, N = 3, 17, 64, 40
+    x, w, b, dy = new(F, P, K), new(N, K), new(N), new(F, P, N)
+    d = B.make_w16a16(w, b, "silu")
+
+    def run(x, dy):
+        M = F * P
+        y, z = (torch.full((*x.shape[:-1], N), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        ws = torch.empty(max(B.qail_w16a16_workspace(d, M), B.qail_w16a16_backward_workspace(d, M)), dtype=torch.uint8, device="cuda")
+        B.qail_w16a16_linear(d, x, y, ws, z=z)
+        out = [torch.full_like(x, float("nan")), torch.full_like(w, float("nan")), torch.full((N,), float("nan"), device="cuda")]
+        B.qail_w16a16_backward(d, x, dy, ws, z=z, dx=out[0], dweight=out[1], dbias=out[2])
+        return [y, z, *out]
+
+    for a, e in zip(run(x, dy), run(x.view(F * P, K), dy.view(F * P, N))):
+        assert torch.equal(a.flatten(), e.flatten()) and torch.isfinite(a).all()
+    one = B.make_w16a16(w[:1].contiguous())       # one output: its gradient may be a list of numbers
+    dx, flat = torch.empty((F * P, K), dtype=torch.bfloat16, device="cuda"), torch.empty((F * P, K), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.qail_w16a16_backward_workspace(one, F * P), dtype=torch.uint8, device="cuda")
+    B.qail_w16a16_backward(one, None, dy[..., :1].contiguous(), ws, dx=dx)
+    B.qail_w16a16_backward(one, None, dy[..., 0].flatten().contiguous(), ws, dx=flat)
+    assert torch.equal(dx, flat)
