@@ -175,7 +175,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, long long p, int q, f
         float t = v[i];
         if (e.bias) t += bf16_bits_to_f32(e.bias[q + i]);
         if (e.z) e.z[at + i] = (uint16_t)f32x2_to_bf16x2_rne(t, 0.f);
-        if (e.act != QAIL_ACT_NONE) t = activated<false>(e.act, t);
+        if (e.act != QAIL_ACT_NONE) t = e.y ? activated<true>(e.act, t) : activated<false>(e.act, t);   // the same function as in whole groups
         if (e.residual) t += bf16_bits_to_f32(e.residual[at + i]);
         if (e.y) e.y[at + i] = (uint16_t)f32x2_to_bf16x2_rne(t, 0.f);
         else e.y32[at + i] = t;

@@ -56,3 +56,33 @@ def test_an_infinity_is_what_the_function_makes_of_it(B, activation, out, how):
         assert torch.equal(y[torch.isinf(want)].double(), want[torch.isinf(want)]) and torch.isfinite(y[torch.isfinite(want)]).all(), activation
         off = (2.0 ** -7 if out == BF16 else 2.0 ** -20) * want.abs() + 2.0 ** -24
         assert ((y.double() - want).abs() <= off)[torch.isfinite(want)].all(), activation
+
+
+# Of the function's value, far from 0: the exact GELU for bf16 outputs takes a tail good to 2^-14.7 and an exponential of an argument in one part, up to 126 with three roundings of 2^-24 of
+# itself (2^-16.5 of the exponential); the argument of tanh-GELU's exponential, up to 88, has four (2^-15.5).
+GOOD_TO = {"gelu": 2.0 ** -20, "gelu_tanh": 2.0 ** -15, "silu": 2.0 ** -20}
+
+
+@pytest.mark.parametrize("activation, low", [("gelu", -14.0), ("gelu_tanh", -10.5), ("silu", -95.0)])
+@pytest.mark.parametrize("out", [BF16, torch.float32])
+def test_small_values_are_good_to_a_share_of_themselves(B, activation, low, out):
+    """Down to 2^-119: below, reciprocals and exponentials have no normal numbers.  All columns of a row are the same sum, and the last seven, which are written one by one, have the
+    values of the first eight."""
+    z = torch.cat((torch.linspace(low, 8, 6001), -torch.logspace(-30, 1, 500))).cuda().to(BF16)
+    M, N = z.numel(), 15
+    w = torch.zeros((N, 8), dtype=BF16, device="cuda")
+    w[:, 0] = 1
+    x = torch.zeros((M, 8), dtype=BF16, device="cuda")
+    x[:, 0] = z
+    y = torch.full((M, N), NAN, dtype=out, device="cuda")
+    d = B.make_w16a16(w, None, activation)
+    B.qail_w16a16_linear(d, x, y, space(B.qail_w16a16_workspace(d, M)))
+    assert torch.equal(y, y[:, :1].expand(-1, N))
+    t = z.double()
+    if activation == "gelu":
+        want = t * torch.erfc(-t / math.sqrt(2)) / 2
+    else:
+        want = t / (1 + torch.exp(-t if activation == "silu" else -math.sqrt(8 / math.pi) * (t + 0.044715 * t ** 3)))
+    good = 2.0 ** -14 if activation == "gelu" and out == BF16 else GOOD_TO[activation]
+    off = (good + (2.0 ** -8 if out == BF16 else 2.0 ** -24)) * want.abs() + 2.0 ** -119
+    assert ((y[:, 0].double() - want).abs() <= off).all()
