@@ -437,7 +437,7 @@ hipError_t launch_embed_back(const int32_t* ids, const uint16_t* dh, int T, floa
     while (passes < 4 && (V >> (8 * passes)) != 0) ++passes;   // keys are 0 .. V
     SumArgs g = {pair[0], pair[1], dh, dtable, reinterpret_cast<float*>(w + at.sums), T, V, K, accumulate, scale, 1, 1};
     while (4 * g.lanes < K && g.lanes < 256) g.lanes *= 2;
-    // eight blocks a compute unit, and no fewer rows than threads for them
+    // eight blocks a compute unit, and a row for each group of threads that shares one (below K = 64 there are more groups than rows: the others' threads have none)
     const int across = (K + 4 * g.lanes - 1) / (4 * g.lanes), groups = 256 / g.lanes;
     g.rows = (int)std::min<long long>(kMostRows, std::max<long long>(groups, (long long)V * across / (8 * device_cu_count())));
     if (at.tiles == 1) {

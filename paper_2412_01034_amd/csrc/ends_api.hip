@@ -14,7 +14,7 @@ int hip_status(hipError_t e) { return e == hipSuccess ? QAIL_OK : QAIL_ERR_HIP; 
 
 int check_embed(int32_t V, int32_t K, int32_t T) {
     if (V < 1 || K < 8 || K % 8 != 0 || T < 0) return QAIL_ERR_SHAPE;
-    // 256 threads a token or for 64 rows of the table stay below 2^32
+    // 256 threads a token, or for 16 rows of the table and 1024 columns, stay below 2^32
     if (K > 65536 || V >= (1 << 24) || T >= (1 << 24) || (long long)V * K > (1ll << 36) || (long long)T * K > (1ll << 36)) return QAIL_ERR_UNSUPPORTED;
     return QAIL_OK;
 }
@@ -24,9 +24,11 @@ int check_linear(const qail_w16a16* d, int32_t M) {
     if (!d) return QAIL_ERR_NULL;
     if (d->activation < QAIL_ACT_NONE || d->activation > QAIL_ACT_SILU) return QAIL_ERR_UNSUPPORTED;
     if (M < 1 || d->N < 1 || d->K < 8 || d->K % 8 != 0) return QAIL_ERR_SHAPE;
-    // 128 rows of an operand are reached by 32-bit offsets, and 256 threads for 8 outputs, or for a tile, stay below 2^32
+    // 256 rows of an operand are reached by 32-bit offsets, and 256 threads for 8 outputs, or for a tile, stay below 2^32
+    constexpr int kMostSize = 1 << 22;
     constexpr long long kMost = 1ll << 33;
-    if (M > (1 << 22) || d->N > (1 << 22) || d->K > (1 << 22) || (long long)M * d->N > kMost || (long long)M * d->K > kMost || (long long)d->N * d->K > kMost)
+    static_assert(257ll * kMostSize * (int)sizeof(uint16_t) < (1ll << 32), "offsets of a tile's rows");
+    if (M > kMostSize || d->N > kMostSize || d->K > kMostSize || (long long)M * d->N > kMost || (long long)M * d->K > kMost || (long long)d->N * d->K > kMost)
         return QAIL_ERR_UNSUPPORTED;
     return QAIL_OK;
 }

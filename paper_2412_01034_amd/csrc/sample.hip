@@ -554,7 +554,8 @@ __global__ __launch_bounds__(kBlock) void sample_kernel(const SampleArgs a) {
     float low = fmaxf(weight.low, b.ties > 0 ? value_of(key_of(b.value) + 1) : b.value);   // what is kept beside the ties; of min_p's border two steps below for its rounding
     if (min_p > 0.f) low = fmaxf(low, value_of(max(key_of((float)(weight.most + least * (double)temperature)), kLowest + 3) - 2));
     const float from = on > 0 ? fminf(low, b.value) : low;   // (between them there may be what min_p does not keep)
-    const int segments = row.chunks * kWaves;           // at most 512: one a thread
+    const int segments = row.chunks * kWaves;           // at most 528
+    static_assert(kMostChunks * kWaves <= kBlock, "one a thread");
     if ((int)threadIdx.x < segments) sh.segment[threadIdx.x] = 0, sh.ties[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.equal = 0;
     for (int g = 0; g < row.chunks; g += kGroup) {

@@ -27,9 +27,10 @@ __host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4
 // ------------------------------------------------------------------------------------------------ activations --
 
 // A tile has as many outputs as its waves have cycles to spare, so these are short: products and sums with one rounding, the hardware's 2^x and 1 / x
-// (1 ulp each).  Relative errors are about 2^-21 everywhere; the arguments of exponentials are kept in two parts, since 2^x loses 2^-24 x.
+// (1 ulp each).  The arguments of exponentials are kept in two parts, since 2^x loses 2^-24 x.  Relative errors are below 2^-20, but for the short GELU (2^-14.3, below) and
+// tanh-GELU of far negative z (2^-15.5: its argument has 2^-22 of itself, which is 88 there).  Results below 2^-119 may be 0: the hardware's 2^x and 1 / x have no subnormal ones.
 
-// exp(x); 0 and infinity beyond 126.
+// exp(x): 0 below -87.3, infinity beyond 88.7.  (The argument's clamp is farther out: it keeps infinities out of `lo`.)
 __device__ __forceinline__ float exp_of(float x) {
     constexpr float k = 1.44269504f, k_lo = 1.92596299e-8f;   // log2(e)
     x = __builtin_amdgcn_fmed3f(x, -126.f, 126.f);
@@ -38,8 +39,8 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 
 // x = |z| <= 20: exp(-z^2 / 2), and beside it erfc(x / sqrt(2)) / 2, the share of the normal distribution beyond x.  erfc(v) exp(v^2) is t P(t), t = 1 / (1 + 0.3 v), with
-// a polynomial that is fitted to v <= 10 with the least largest relative error: of degree 8 (2^-25.6), or where the result is rounded to bf16 of degree 5 (2^-14.7), the
-// argument of the exponential in one part.  The shorter form saves a quarter of an epilogue's instructions with the exact GELU (2056 x 4096 x 1024: 51.7 -> 49.8 us).
+// a polynomial that is fitted to v <= 10 with the least largest relative error: of degree 8 (2^-25.6), or where the result is rounded to bf16 (2^-8) of degree 5 (2^-14.7), the
+// argument of the exponential in one part (2^-16.5).  The shorter form saves a quarter of an epilogue's instructions with the exact GELU (2056 x 4096 x 1024: 51.7 -> 49.8 us).
 template <bool kShort>
 __device__ __forceinline__ float normal_tail(float x, float& bell) {
     constexpr float k = -0.721347520f, k_lo = -9.62981495e-9f;   // -log2(e) / 2

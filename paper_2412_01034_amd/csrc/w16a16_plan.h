@@ -43,7 +43,7 @@ __host__ __device__ inline TilePlace tile_place(const ProductPlan& pl, int b) {
 // turned: the operand of P lies row by row of r; parts: it is the sum of so many matrices, which the steps go through in turn.
 //
 // Up to 32 rows: tiles of 32 x 64, whose cost is the stream of the other operand; blocks for three a unit by shares of the contraction, which are
-// not worth the second launch before a tile has sixteen steps for each.
+// not worth the second launch before a tile has eight steps for each.
 // Beyond: the tile and the shares that cost least by what was measured (us a step, of two tiles that share a unit / of one that has it alone, and for the way in and out):
 //     128 x 128   1.0 / 0.62, 7        192 x 128 (straight)   1.4 / 0.78, 9        256 x 256   1.65, 10 (one a unit)
 // and for shares 3 for the second launch and their sums' way at 4 TB/s.  4096 x 4096 x 4096 takes 118 us with 256 x 256 tiles and 148 with 128 x 128, 2056 x 4096 x 1024 28
