@@ -581,7 +581,7 @@ int qail_w16a16_linear(const qail_w16a16* d, const uint16_t* x, int32_t M, const
 
 /* Its gradients, at the rounded z:
  *     dz = dy * act'(z)                     fp32; enters the products in two bf16 parts (2^-16 of itself), or with round_dz != 0 rounded to
- *                                           bf16, which takes little more than half their time and costs the gradients as much as their own rounding;
+ *                                           bf16, which takes 0.54 to 0.65 of the call's time and costs the gradients as much as their own rounding;
  *                                           a bf16 dy without an activation or with RELU is exact either way
  *     dx[m][k] = sum_n dz[m][n] W[n][k]     fp32 sums, rounded once; bf16 [M][K] or NULL
  *     dweight[n][k] = sum_m dz[m][n] x[m][k]   likewise; bf16 [N][K] or NULL

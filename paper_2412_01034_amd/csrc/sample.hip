@@ -12,7 +12,8 @@
 //
 // One block a row, whose values stay in registers up to 32768 tokens; a longer row is read again in every pass, and lies in L2 by then.  Several blocks a row
 // would have to meet in memory, which this call has none of.  Bound by instructions and by the meetings of the 16 waves, not by memory: one row of 32000 takes
-// 18 us (15.6 of 40 thousand cycles are the exponentials of top-p, thirty instructions each), 256 rows 33, 48 rows of 131072 94.
+// 18 us (15.6 of 40 thousand cycles are the exponentials of top-p, thirty instructions each), 256 rows 33, 48 rows of 131072 63 to 92: as
+// the slowest of them, 35 to 50 us where little is kept and 90 where top-p keeps nearly all of a flat row, whose exponentials are computed twice.
 #include <type_traits>
 
 #include "qail_internal.h"

@@ -279,8 +279,9 @@ struct Operand {
 };
 
 // kWP x kWQ waves share a tile of kBP x kBQ; kSlots steps lie in LDS, all but one of them on their way while one is multiplied. The matrix cores get B's rows
-// as rows: a lane then has one p and groups of four neighbouring q.  Bound by power and LDS where the chip is full (a 4096 x 4096 x 4096 gradient 115 to 125
-// us with dz in one part, 242 to 264 in two: 1040 to 1200 TFLOP/s of 1450 that a library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s),
+// as rows: a lane then has one p and groups of four neighbouring q.  Where the chip is full bound by the matrix pipe (61 to 66 % busy) and by what runs beside no product, a tile's way in and its
+// epilogue, as a unit has one tile at a time (a 4096 x 4096 x 4096 gradient 115 to 125 us with dz in one part, 224 to 264 in two: 1040 to 1230 TFLOP/s of 1450 that a
+// library product reaches), by the other operand's way from memory with few rows (16 x 4096 x 32000: 55 us, 4.8 TB/s),
 // by the epilogue with short contractions (2056 x 4096 x 1024 with GELU, z and bias 40 us, 28 without them).
 template <int kBP, int kBQ, int kWP, int kWQ, bool kTA, bool kTB, int kSlots>
 __global__ __launch_bounds__(kWP* kWQ* kWave, (kWP * kWQ > 4 ? 2 : 1)) void w16a16_product_kernel(const ProductArgs g) {
